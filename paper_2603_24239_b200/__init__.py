@@ -16,8 +16,13 @@ _BINDING_NAMES = (
     "lib", "LIB_PATH",
 )
 
+_SERVING_NAMES = ("encode_paging", "encode_rotary", "encode_attention", "last_attention_kernel")
+
 
 def __getattr__(name):
+    if name == "serving" or name in _SERVING_NAMES:
+        s = importlib.import_module(".serving", __name__)
+        return s if name == "serving" else getattr(s, name)
     if name == "binding" or name in _BINDING_NAMES:
         b = importlib.import_module(".binding", __name__)
         return b if name == "binding" else getattr(b, name)

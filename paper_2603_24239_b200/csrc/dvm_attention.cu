@@ -1,0 +1,103 @@
+// Attention meta-kernel: host launch, and the kernel without tensor cores.
+//
+// dvm_attention_plain_kernel takes any type, stride and head size: one warp per row and head walks the visible tokens.
+// It is what inputs get that the tensor-core kernels cannot load (fp32, odd head sizes, odd strides or pointers).
+#include <cuda_runtime.h>
+
+#include "dvm_attention.cuh"
+#include "dvm_launch.h"
+
+namespace dvm {
+namespace att {
+
+constexpr int PLAIN_WARPS = 8;
+
+template <class T>
+__global__ void __launch_bounds__(PLAIN_WARPS * 32) dvm_attention_plain_kernel(const __grid_constant__ Args a) {
+  const long long item = (long long)blockIdx.x * PLAIN_WARPS + (threadIdx.x >> 5);
+  if (item >= (long long)a.rows * a.hq) return;
+  const int row = (int)(item / a.hq), head = (int)(item % a.hq);
+  int lo = 0, hi = a.n + 1;  // first i with starts[i] > row
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (a.starts[mid] > row) hi = mid; else lo = mid + 1;
+  }
+  const int i = lo - 1;
+  if (i < 0 || i >= a.n) return;
+  const Request r = request_at(a, i);
+  const int j = row - r.s0;
+  if (j < 0 || j >= min(r.q_len, a.max_q)) return;
+  attend_row<T>(a, i, r.pos0 + j, row, head);
+}
+
+}  // namespace att
+}  // namespace dvm
+
+static thread_local int t_last_kernel = -1;
+
+extern "C" int dvm_last_attention_kernel(int* kernel) {
+  if (!kernel || t_last_kernel < 0) return DVM_ERR_INVALID_ARG;
+  *kernel = t_last_kernel;
+  return DVM_OK;
+}
+
+int dvm_launch_attention(const dvm_attention_desc& d, void* const* t, cudaStream_t stream) {
+  using namespace dvm::att;
+  DvmDeviceInfo dev;
+  int st = dvm_device_state(&dev);
+  if (st != DVM_OK) return st;
+  Args a = {};
+  a.q = t[AT_Q]; a.k = t[AT_K]; a.v = t[AT_V];
+  a.table = (const int*)t[AT_TABLE]; a.starts = (const int*)t[AT_STARTS]; a.lengths = (const int*)t[AT_LENGTHS];
+  a.out = t[AT_OUT]; a.ws = (float*)t[AT_WS]; a.status = dev.scratch;
+  for (int i = 0; i < 2; ++i) { a.qs[i] = d.q_stride[i]; a.os[i] = d.out_stride[i]; }
+  for (int i = 0; i < 3; ++i) { a.ks[i] = d.k_stride[i]; a.vs[i] = d.v_stride[i]; }
+  a.n = (int)d.requests; a.rows = (int)d.rows; a.hq = (int)d.q_heads; a.hk = (int)d.kv_heads; a.group = a.hq / a.hk; a.D = (int)d.head_dim;
+  a.pages = (int)d.pages; a.max_blocks = (int)d.max_blocks;
+  while ((1ll << a.page_log) < d.page_size) ++a.page_log;
+  a.window = (int)d.window; a.sinks = (int)d.sinks; a.max_q = (int)d.max_q; a.out_bf16 = d.out_dtype == DVM_BF16; a.scale = d.scale;
+  const int64_t items = d.rows * d.q_heads, grid = (items + PLAIN_WARPS - 1) / PLAIN_WARPS;
+  if (grid >= (1ll << 31)) return DVM_ERR_TOO_LARGE;
+  if (d.dtype == DVM_BF16) dvm_attention_plain_kernel<__nv_bfloat16><<<(int)grid, PLAIN_WARPS * 32, 0, stream>>>(a);
+  else dvm_attention_plain_kernel<float><<<(int)grid, PLAIN_WARPS * 32, 0, stream>>>(a);
+  DVM_CUDA(cudaGetLastError());
+  dvm_count_launch();
+  t_last_kernel = 0;
+  return DVM_OK;
+}
+
+// ---- dvm_launch's entry for the serving codes (verified) ----
+int dvm_launch_serving(const uint32_t* w, void* const* tensors, int n_tensors, cudaStream_t stream) {
+  const int nt = w[DVM_H_COUNTS] & 0xff;
+  if (n_tensors != nt) return DVM_ERR_INVALID_ARG;
+  if (w[DVM_H_N_TILES] == 0) return DVM_OK;
+  int64_t need[DVM_MAX_TENSORS];
+  dvm_extents_serving(w, need);
+  for (int i = 0; i < nt; ++i)
+    if (need[i] > 0 && !tensors[i]) return DVM_ERR_INVALID_ARG;
+  const uint32_t type = w[DVM_H_KERNEL_TYPE];
+  auto aligned = [&](int slot, int dtype) { return slot < 0 || ((uintptr_t)tensors[slot] & (dtype == DVM_BF16 ? 1 : 3)) == 0; };
+  if (type == DVM_KERNEL_PAGING) {
+    dvm_paging_desc d;
+    dvm_serving_desc(w, &d);
+    for (int i = 0; i < PG_N; ++i)
+      if (!aligned(i, DVM_F32)) return DVM_ERR_INVALID_ARG;
+    return dvm_launch_paging(d, tensors, stream);
+  }
+  if (type == DVM_KERNEL_ROTARY) {
+    dvm_rotary_desc d;
+    dvm_serving_desc(w, &d);
+    const RotarySlots s = dvm_rotary_slots(d);
+    if (!aligned(s.q, d.dtype) || !aligned(s.k, d.dtype) || !aligned(s.v, d.dtype) || !aligned(s.wq, d.weight_dtype) || !aligned(s.wk, d.weight_dtype) ||
+        !aligned(s.angles, DVM_F32) || !aligned(s.positions, DVM_F32) || !aligned(s.slots, DVM_F32) || !aligned(s.q_out, d.out_dtype) ||
+        !aligned(s.k_out, d.out_dtype) || !aligned(s.v_out, d.out_dtype))
+      return DVM_ERR_INVALID_ARG;
+    return dvm_launch_rotary(d, tensors, stream);
+  }
+  dvm_attention_desc d;
+  dvm_serving_desc(w, &d);
+  if (!aligned(AT_Q, d.dtype) || !aligned(AT_K, d.dtype) || !aligned(AT_V, d.dtype) || !aligned(AT_TABLE, DVM_F32) || !aligned(AT_STARTS, DVM_F32) ||
+      !aligned(AT_LENGTHS, DVM_F32) || !aligned(AT_OUT, d.out_dtype) || (need[AT_WS] > 0 && ((uintptr_t)tensors[AT_WS] & 15)))
+    return DVM_ERR_INVALID_ARG;
+  return dvm_launch_attention(d, tensors, stream);
+}

@@ -12,6 +12,7 @@
 #include "dvm_format.h"
 #include "dvm_internal.h"
 #include "dvm_launch.h"
+#include "dvm_serving.h"
 #include "dvm_vm.cuh"
 #include "dvm_vm_variants.h"
 #include "dvm_link.h"
@@ -815,6 +816,13 @@ extern "C" int dvm_launch(const void* code, size_t code_size, void* const* tenso
   const uint32_t* w = (const uint32_t*)code;
   if (w[DVM_H_KERNEL_TYPE] == DVM_KERNEL_MATMUL)
     return dvm_launch_matmul(w, code_size / 4, tensors, n_tensors, (cudaStream_t)cuda_stream);
+  if (dvm_is_serving(w[DVM_H_KERNEL_TYPE])) {
+    st = dvm_launch_serving(w, tensors, n_tensors, (cudaStream_t)cuda_stream);
+    if (st != DVM_OK || !debug_mode()) return st;
+    int status = DVM_OK;
+    st = dvm_last_device_status(cuda_stream, &status);
+    return st != DVM_OK ? st : status;
+  }
   const void* codes[1] = {code};
   void* const* tl[1] = {tensors};
   return launch_vec(1, codes, tl, &n_tensors, false, nullptr, (cudaStream_t)cuda_stream);
@@ -902,6 +910,7 @@ extern "C" int dvm_run_host(const void* code, size_t code_size, void* const* hos
   int st = dvm_verify(code, code_size);
   if (st != DVM_OK) return st;
   const uint32_t* w = (const uint32_t*)code;
+  if (dvm_is_serving(w[DVM_H_KERNEL_TYPE])) return DVM_ERR_UNSUPPORTED;  // (their tables and caches live on the device between launches)
   const uint32_t counts = w[DVM_H_COUNTS];
   const int nt = counts & 0xff, n_in = (counts >> 8) & 0xff;
   if (n_tensors != nt || nt > DVM_MAX_TENSORS) return DVM_ERR_INVALID_ARG;

@@ -38,6 +38,7 @@
 #include "dvm_launch.h"
 #include "dvm_math.cuh"
 #include "dvm_program.h"
+#include "dvm_sm100.cuh"
 
 // =================================================================================================
 // Host: encode
@@ -511,6 +512,8 @@ int dvm_disassemble_matmul(const uint32_t* w, size_t n_words, char* buf, size_t 
 namespace dvm {
 namespace mm {
 
+using namespace sm100;
+
 constexpr int BLOCK_M = DVM_MM_BLOCK_M, BLOCK_K = DVM_MM_BLOCK_K, CHUNK = DVM_MM_CHUNK;
 constexpr int ACC_COLS = 256;                       // accumulator columns of one tile (one UMMA N)
 constexpr uint32_t STAGE_A = BLOCK_M * BLOCK_K * 2; // 16 KB: 128 rows of 128 bytes
@@ -523,9 +526,6 @@ constexpr uint32_t BAR_BYTES = 256;                  // barriers and flags behin
 constexpr uint32_t TMP_BYTES = 128 * CHUNK * 4;     // one epilogue temporary: 16 KB
 constexpr int THREADS = 192;
 constexpr uint32_t TMEM_COLS = 512;
-constexpr unsigned long long WAIT_NS = 2000000000ull;   // limit of one wait: 2 s
-constexpr unsigned long long DRAIN_NS = 200000000ull;   // limit of a wait for work in flight after an abort
-constexpr uint32_t WAIT_SPINS = 1u << 27;
 
 // Tail split (split_s >= 2): the tiles [split_first, split_first + split_r) -- the last, partial wave of the
 // launch -- are shared along k.  Their k blocks form one line, tile a at [a * split_kbp, a * split_kbp + k_blocks);
@@ -553,66 +553,6 @@ struct MMParams {
 constexpr uint32_t MAX_SPLIT = 4;                    // parts of a tail tile at most
 constexpr size_t PART_FLOATS = (size_t)BLOCK_M * ACC_COLS;  // one partial accumulator: 128 KB
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ unsigned long long gtimer() {
-  unsigned long long t;
-  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-  return t;
-}
-// Bounded wait: gives up after limit_ns (or WAIT_SPINS polls), raising the CTA's abort flag; with
-// heed_abort it also gives up as soon as another role has raised the flag.
-__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag,
-                                            unsigned long long limit_ns, bool heed_abort) {
-  const unsigned long long t0 = gtimer();
-  for (uint32_t spin = 0; spin < WAIT_SPINS; ++spin) {
-    if (mbar_try(bar, parity)) return true;
-    if (heed_abort && *abort_flag) return false;
-    if (gtimer() - t0 > limit_ns) break;
-  }
-  *abort_flag = 1;
-  return false;
-}
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag) {
-  if (mbar_try(bar, parity)) return true;
-  return mbar_wait_slow(bar, parity, abort_flag, WAIT_NS, true);
-}
-
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y)
-      : "memory");
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void umma_bf16(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-// mbarrier arrive once every tcgen05.mma issued so far by this thread has completed
-__device__ __forceinline__ void umma_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
 // ---- the CTA-pair forms (tcgen05 cta_group::2: two CTAs of a cluster, one MMA over both their shared memories) ----
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -649,42 +589,6 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-
-// 32 consecutive accumulator columns of this thread's tensor-memory lane
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[CHUNK]) {
-  uint32_t r[CHUNK];
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr)
-      : "memory");
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-  for (int i = 0; i < CHUNK; ++i) v[i] = __uint_as_float(r[i]);
-}
-
-// the same 32 columns written back (the caller waits with tmem_st_wait before it reads them again)
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[CHUNK]) {
-  uint32_t r[CHUNK];
-#pragma unroll
-  for (int i = 0; i < CHUNK; ++i) r[i] = __float_as_uint(v[i]);
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
-      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]),
-        "r"(taddr)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Bounded wait of a tile's owner for the n flags (`stride` words apart) of its other parts (each becomes `epoch` once that part's
 // accumulators are in the workspace); like mbar_wait_slow it raises the CTA's abort flag when it gives up.
