@@ -20,10 +20,10 @@ _SERVING_NAMES = ("encode_paging", "encode_rotary", "encode_attention", "last_at
 
 
 def __getattr__(name):
-    if name == "serving" or name in _SERVING_NAMES:
-        s = importlib.import_module(".serving", __name__)
-        return s if name == "serving" else getattr(s, name)
-    if name == "binding" or name in _BINDING_NAMES:
-        b = importlib.import_module(".binding", __name__)
-        return b if name == "binding" else getattr(b, name)
+    for module, names in (("serving", _SERVING_NAMES), ("binding", _BINDING_NAMES)):
+        if name == module or name in names:
+            m = importlib.import_module("." + module, __name__)
+            value = m if name == module else getattr(m, name)
+            globals()[name] = value   # found without this function from now on
+            return value
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

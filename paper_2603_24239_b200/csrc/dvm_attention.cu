@@ -4,7 +4,10 @@
 // It is what inputs get that the tensor-core kernels cannot load (fp32, odd head sizes, odd strides or pointers).
 #include <cuda_runtime.h>
 
+#include <atomic>
+
 #include "dvm_attention.cuh"
+#include "dvm_attention_launch.h"
 #include "dvm_launch.h"
 
 namespace dvm {
@@ -35,6 +38,44 @@ __global__ void __launch_bounds__(PLAIN_WARPS * 32) dvm_attention_plain_kernel(c
 
 static thread_local int t_last_kernel = -1;
 
+namespace {
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+int encode_map(CUtensorMap* map, const void* ptr, const cuuint64_t (&dims)[4], const cuuint64_t (&strides)[3], const cuuint32_t (&box)[4]) {
+  static std::atomic<EncodeTiledFn> cached{nullptr};
+  EncodeTiledFn fn = cached.load();
+  if (!fn) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found);
+    if (e != cudaSuccess || found != cudaDriverEntryPointSuccess || !p) {
+      dvm_note_cuda_error(e != cudaSuccess ? (int)e : (int)cudaErrorNotSupported);
+      return DVM_ERR_CUDA;
+    }
+    fn = (EncodeTiledFn)p;
+    cached.store(fn);
+  }
+  const cuuint32_t one[4] = {1, 1, 1, 1};
+  if (fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
+    dvm_note_cuda_error((int)cudaErrorInvalidValue);
+    return DVM_ERR_CUDA;
+  }
+  return DVM_OK;
+}
+
+// (the stride of a dim of size 1 is never walked: any legal one)
+inline cuuint64_t map_stride(int64_t size, int64_t stride) { return size > 1 ? (cuuint64_t)stride * 2 : 16; }
+}  // namespace
+
+int dvm_cache_map(const dvm_attention_desc& d, const int64_t* stride, const void* ptr, int most, CUtensorMap* map) {
+  const cuuint64_t dims[4] = {(cuuint64_t)d.head_dim, (cuuint64_t)d.page_size, (cuuint64_t)d.kv_heads, (cuuint64_t)d.pages};
+  const cuuint64_t strides[3] = {map_stride(d.page_size, stride[1]), map_stride(d.kv_heads, stride[2]), map_stride(d.pages, stride[0])};
+  const cuuint32_t box[4] = {64, (cuuint32_t)(d.page_size < most ? d.page_size : most), 1, 1};
+  return encode_map(map, ptr, dims, strides, box);
+}
+
 extern "C" int dvm_last_attention_kernel(int* kernel) {
   if (!kernel || t_last_kernel < 0) return DVM_ERR_INVALID_ARG;
   *kernel = t_last_kernel;
@@ -56,6 +97,12 @@ int dvm_launch_attention(const dvm_attention_desc& d, void* const* t, cudaStream
   a.pages = (int)d.pages; a.max_blocks = (int)d.max_blocks;
   while ((1ll << a.page_log) < d.page_size) ++a.page_log;
   a.window = (int)d.window; a.sinks = (int)d.sinks; a.max_q = (int)d.max_q; a.out_bf16 = d.out_dtype == DVM_BF16; a.scale = d.scale;
+  const bool aligned = (((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v) & 15) == 0;
+  if (aligned && dvm_attention_tensor_cores(d) && dvm_attention_single(d)) {
+    st = dvm_launch_attention_single(d, a, stream);
+    if (st == DVM_OK) t_last_kernel = 1;
+    return st;
+  }
   const int64_t items = d.rows * d.q_heads, grid = (items + PLAIN_WARPS - 1) / PLAIN_WARPS;
   if (grid >= (1ll << 31)) return DVM_ERR_TOO_LARGE;
   if (d.dtype == DVM_BF16) dvm_attention_plain_kernel<__nv_bfloat16><<<(int)grid, PLAIN_WARPS * 32, 0, stream>>>(a);

@@ -148,7 +148,7 @@ RotarySlots dvm_rotary_slots(const dvm_rotary_desc& d) {
 
 bool dvm_attention_tensor_cores(const dvm_attention_desc& d) {
   if (d.dtype != DVM_BF16 || d.head_dim % 8 || d.head_dim > 128 || d.pages == 0) return false;
-  auto ok = [](int64_t size, int64_t stride) { return size <= 1 || (stride > 0 && stride % 8 == 0); };
+  auto ok = [](int64_t size, int64_t stride) { return size <= 1 || (stride > 0 && stride % 8 == 0 && stride < (1ll << 39)); };  // (a tile copy's strides: multiples of 16 bytes below 2^40)
   return ok(d.rows, d.q_stride[0]) && ok(d.q_heads, d.q_stride[1]) && ok(d.pages, d.k_stride[0]) && ok(d.page_size, d.k_stride[1]) &&
          ok(d.kv_heads, d.k_stride[2]) && ok(d.pages, d.v_stride[0]) && ok(d.page_size, d.v_stride[1]) && ok(d.kv_heads, d.v_stride[2]);
 }

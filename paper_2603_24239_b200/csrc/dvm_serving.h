@@ -39,10 +39,11 @@ bool dvm_attention_tensor_cores(const dvm_attention_desc& d);
 inline bool dvm_attention_single(const dvm_attention_desc& d) { return d.max_q == 1 && d.q_heads / d.kv_heads <= 16; }
 
 // bytes of the workspace of a single-token code: every CTA leaves at most two parts of a head group (its range of tiles may
-// start and end inside one), each a row of head_dim sums, a maximum and a sum of weights per query head
+// start and end inside one), each a row of head_dim sums, a maximum and a sum of weights per query head, and 16 bytes
+// that say which
 inline int64_t dvm_attention_workspace(const dvm_attention_desc& d) {
   if (!d.requests || !d.rows || !dvm_attention_tensor_cores(d) || !dvm_attention_single(d)) return 0;
-  return (int64_t)DVM_ATT_UNITS * 2 * (d.q_heads / d.kv_heads) * (d.head_dim + 2) * 4;
+  return (int64_t)DVM_ATT_UNITS * (16 + 2 * (d.q_heads / d.kv_heads) * (d.head_dim + 2) * 4);
 }
 
 int dvm_launch_paging(const dvm_paging_desc& d, void* const* t, cudaStream_t stream);

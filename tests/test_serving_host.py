@@ -133,7 +133,7 @@ def test_extents():
     st, buf, size = _encode(binding.lib.dvm_encode_attention, attention())
     assert dvm.tensor_extents(binding.Code(buf, size, [])) == [2 * 20 * 512, 2 * 11 * 2048, 2 * 11 * 2048, 48, 16, 12, 2 * 20 * 512, 0]
     st, buf, size = _encode(binding.lib.dvm_encode_attention, attention(max_q=1))
-    assert dvm.tensor_extents(binding.Code(buf, size, []))[-1] == 296 * 2 * 4 * (64 + 2) * 4
+    assert dvm.tensor_extents(binding.Code(buf, size, []))[-1] == 296 * (16 + 2 * 4 * (64 + 2) * 4)
     st, buf, size = _encode(binding.lib.dvm_encode_attention, attention(rows=0))
     assert dvm.tensor_extents(binding.Code(buf, size, [])) == [0] * 8
 
