@@ -94,9 +94,12 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 }
 __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(WARPS * 32) : "memory"); }
 
-// Per CTA in the workspace: the pair whose last part in this CTA continues in later ones ({request, kv head, parts, slot}),
-// then two slots of parts: slot 0 the part at the start of the CTA's range, slot 1 a later one.
-__device__ __forceinline__ int4* head_of(const Args& a, int cta) { return (int4*)a.ws + cta; }
+// The workspace: DVM_ATT_UNITS heads {request, first CTA, parts, slot of the first part}, then two slots of parts per CTA:
+// slot 0 the part at the start of the CTA's range (the last one of a pair that began earlier, or the only one), slot 1 a
+// later one.  With at most DVM_ATT_UNITS pairs there is a head per pair, written where the pair begins; with more, one per
+// CTA, for the pair that continues beyond its range.
+__device__ __forceinline__ int4* head_of(const Args& a, int i) { return (int4*)a.ws + i; }
+__host__ __device__ __forceinline__ bool heads_by_pair(const Args& a) { return (long long)a.n * a.hk <= DVM_ATT_UNITS; }
 __device__ __forceinline__ float* slot_of(const Args& a, int cta, int slot) {
   return a.ws + 4 * DVM_ATT_UNITS + ((long long)cta * 2 + slot) * a.group * (a.D + 2);
 }
@@ -160,7 +163,7 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
   const long long chunk = max((total + DVM_ATT_UNITS - 1) / DVM_ATT_UNITS, (long long)MIN_TILES);
   const long long begin = min(total, blockIdx.x * chunk), stop = min(total, begin + chunk);
   if (begin == stop) {
-    if (threadIdx.x == 0) *head_of(a, blockIdx.x) = make_int4(0, 0, 0, 0);
+    if (threadIdx.x == 0 && !heads_by_pair(a)) *head_of(a, blockIdx.x) = make_int4(0, 0, 0, 0);
     return;
   }
   // the thread whose requests hold tile `begin` walks to it
@@ -390,14 +393,14 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
           if (d == 0) { part[a.group * a.D + head] = top; part[a.group * (a.D + 1) + head] = all; }
         }
       }
-      if (w.base + w.p.count >= stop) {  // the last pair of the range: does it continue, and does it start here?
-        if (threadIdx.x == 0) {
-          const long long after = w.base + w.p.count;
-          const int parts = w.j0 == 0 && after > stop ? (int)((after - 1) / chunk) - (int)blockIdx.x + 1 : 0;
-          *head_of(a, blockIdx.x) = make_int4(w.request, w.kvh, parts, slot);
-        }
-        break;
+      const long long after = w.base + w.p.count;
+      if (threadIdx.x == 0) {
+        const bool by_pair = heads_by_pair(a);
+        const int parts = w.j0 == 0 && after > stop ? (int)((after - 1) / chunk) - (int)blockIdx.x + 1 : 0;
+        if (by_pair ? w.j0 == 0 : after >= stop)
+          *head_of(a, by_pair ? w.request * a.hk + w.kvh : (int)blockIdx.x) = make_int4(w.request * a.hk + w.kvh, blockIdx.x, parts, slot);
       }
+      if (after >= stop) break;
       consumers_sync();  // the sums and statistics have been read
       w.next(a, begin, stop);
     }
@@ -405,28 +408,62 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
   if (*abort_flag && lane == 0) atomicMax(a.status, (unsigned int)ST_TIMEOUT);
 }
 
-// Joins the parts of the pairs that span several ranges: the CTA of a pair's first part adds them up in their order.
-constexpr int JOIN_THREADS = 256;
-__global__ void __launch_bounds__(JOIN_THREADS) dvm_attention_join_kernel(const __grid_constant__ Args a) {
+// Joins the parts of a pair that spans several ranges: one CTA per head (grid x) and query head of the pair (grid y).
+// The parts' maxima and sums first, then every warp adds up every JOIN_WARPS-th part, then the warps' sums in their order.
+constexpr int JOIN_WARPS = 8;
+__global__ void __launch_bounds__(JOIN_WARPS * 32) dvm_attention_join_kernel(const __grid_constant__ Args a) {
+  __shared__ float weight[DVM_ATT_UNITS];
+  __shared__ float stat[2][JOIN_WARPS];
+  __shared__ float sums[JOIN_WARPS][128];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y;
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (heads_by_pair(a) && request_at(a, blockIdx.x / a.hk).q_len == 0) return;  // (no row: no CTA wrote this head)
   const int4 head = *head_of(a, blockIdx.x);
   const int parts = head.z;
   if (parts < 2) return;
   const float c = a.scale * 1.4426950408889634f;
-  const int row = request_at(a, head.x).s0, size = a.group * a.D;
-  for (int x = threadIdx.x; x < size; x += JOIN_THREADS) {
-    const int h = x / a.D, d = x - h * a.D;
-    float m = -INFINITY, l = 0.f, v = 0.f;
-    for (int k = 0; k < parts; ++k) {
-      const float* part = slot_of(a, blockIdx.x + k, k ? 0 : head.w);
-      const float pm = part[size + h], pl = part[size + a.group + h], pv = part[x];
-      const float top = fmaxf(m, pm);
-      const float keep = m == -INFINITY ? 1.f : exp2f((m - top) * c), add = pm == -INFINITY ? 1.f : exp2f((pm - top) * c);
-      l = l * keep + pl * add;
-      v = v * keep + pv * add;
-      m = top;
-    }
-    put(a.out, a.out_bf16, row * a.os[0] + ((long long)head.y * a.group + h) * a.os[1] + d, l == 0.f ? 0.f : v / l);
+  const int size = a.group * a.D;
+  auto part = [&](int k) -> const float* { return slot_of(a, head.y + k, k ? 0 : head.w); };
+  float m = -INFINITY, l = 0.f;
+  for (int k = threadIdx.x; k < parts; k += JOIN_WARPS * 32) {
+    weight[k] = part(k)[size + h];
+    m = fmaxf(m, weight[k]);
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  if (lane == 0) stat[0][warp] = m;
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < JOIN_WARPS; ++x) m = fmaxf(m, stat[0][x]);
+  for (int k = threadIdx.x; k < parts; k += JOIN_WARPS * 32) {
+    weight[k] = weight[k] == -INFINITY ? 0.f : exp2f((weight[k] - m) * c);  // (a part that saw nothing is all zeros)
+    l += part(k)[size + a.group + h] * weight[k];
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+  if (lane == 0) stat[1][warp] = l;
+  __syncthreads();
+  float v[4] = {};
+#pragma unroll 4
+  for (int k = warp; k < parts; k += JOIN_WARPS) {
+    const float* p = part(k) + h * a.D;
+    const float f = weight[k];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (lane + 32 * e < a.D) v[e] = fmaf(p[lane + 32 * e], f, v[e]);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) sums[warp][lane + 32 * e] = v[e];
+  __syncthreads();
+  l = 0.f;
+#pragma unroll
+  for (int x = 0; x < JOIN_WARPS; ++x) l += stat[1][x];
+  if (threadIdx.x < a.D) {
+    float all = 0.f;
+#pragma unroll
+    for (int x = 0; x < JOIN_WARPS; ++x) all += sums[x][threadIdx.x];
+    const int request = head.x / a.hk, kvh = head.x - request * a.hk;
+    put(a.out, a.out_bf16, request_at(a, request).s0 * a.os[0] + ((long long)kvh * a.group + h) * a.os[1] + threadIdx.x, l == 0.f ? 0.f : all / l);
   }
 }
 
@@ -453,7 +490,7 @@ int dvm_launch_attention_single(const dvm_attention_desc& d, const dvm::att::Arg
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3(DVM_ATT_UNITS); cfg.blockDim = dim3(JOIN_THREADS); cfg.stream = stream; cfg.attrs = at; cfg.numAttrs = 1;
+  cfg.gridDim = dim3(heads_by_pair(a) ? a.n * a.hk : DVM_ATT_UNITS, a.group); cfg.blockDim = dim3(JOIN_WARPS * 32); cfg.stream = stream; cfg.attrs = at; cfg.numAttrs = 1;
   DVM_CUDA(cudaLaunchKernelEx(&cfg, dvm_attention_join_kernel, a));
   dvm_count_launch();
   return DVM_OK;
