@@ -82,6 +82,14 @@ extern "C" int dvm_last_attention_kernel(int* kernel) {
   return DVM_OK;
 }
 
+int dvm_query_map(const dvm_attention_desc& d, const void* ptr, int tokens, CUtensorMap* map) {
+  const int64_t group = d.q_heads / d.kv_heads;
+  const cuuint64_t dims[4] = {(cuuint64_t)d.head_dim, (cuuint64_t)group, (cuuint64_t)d.kv_heads, (cuuint64_t)d.rows};
+  const cuuint64_t strides[3] = {map_stride(group, d.q_stride[1]), map_stride(d.kv_heads, group * d.q_stride[1]), map_stride(d.rows, d.q_stride[0])};
+  const cuuint32_t box[4] = {64, (cuuint32_t)group, 1, (cuuint32_t)tokens};
+  return encode_map(map, ptr, dims, strides, box);
+}
+
 int dvm_launch_attention(const dvm_attention_desc& d, void* const* t, cudaStream_t stream) {
   using namespace dvm::att;
   DvmDeviceInfo dev;
@@ -98,9 +106,11 @@ int dvm_launch_attention(const dvm_attention_desc& d, void* const* t, cudaStream
   while ((1ll << a.page_log) < d.page_size) ++a.page_log;
   a.window = (int)d.window; a.sinks = (int)d.sinks; a.max_q = (int)d.max_q; a.out_bf16 = d.out_dtype == DVM_BF16; a.scale = d.scale;
   const bool aligned = (((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v) & 15) == 0;
-  if (aligned && dvm_attention_tensor_cores(d) && dvm_attention_single(d)) {
-    st = dvm_launch_attention_single(d, a, stream);
-    if (st == DVM_OK) t_last_kernel = 1;
+  a.out_vec = a.out_bf16 && ((uintptr_t)a.out & 15) == 0 && d.out_stride[0] % 8 == 0 && d.out_stride[1] % 8 == 0;
+  if (aligned && dvm_attention_tensor_cores(d)) {
+    const bool single = dvm_attention_single(d);
+    st = single ? dvm_launch_attention_single(d, a, stream) : dvm_launch_attention_prompt(d, a, stream);
+    if (st == DVM_OK) t_last_kernel = single ? 1 : 2;
     return st;
   }
   const int64_t items = d.rows * d.q_heads, grid = (items + PLAIN_WARPS - 1) / PLAIN_WARPS;

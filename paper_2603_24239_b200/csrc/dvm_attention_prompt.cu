@@ -1,0 +1,508 @@
+// Attention of prompts: many query rows per request, on the tensor cores.
+//
+// A CTA takes two tiles of 128 rows of one kv head: a row is a (token, query head of the group) pair, so heads that share
+// keys share the loads, and 2 x floor(128 / group) tokens move through the cache together.  Per tile of 128 tokens of the
+// cache and row tile x:
+//   S_x = Q_x K^T        tcgen05.mma, both operands in shared memory, S_x in tensor memory (128 fp32 columns)
+//   P_x = 2^(c S_x - m)  128 threads, one row each: running maximum m and sum, no exchange between threads;
+//                        P_x goes back to tensor memory as bf16, over the S_x it came from
+//   O_x += P_x V         tcgen05.mma with P_x as the tensor-memory operand
+// While the threads of one row tile work on its weights, the tensor cores run the products of the other.  The products of
+// a row tile are issued in the order PV(t), QK(t + 1) by one thread and complete in that order, so a finished S_x(t + 1)
+// also says that O_x holds PV(t): the rescaling of O_x by a new maximum needs no barrier of its own.  It is skipped until
+// the maximum has grown by more than 2^8 (weights stay below 2^8, far from any bound of bf16 or fp32; the quotient at the
+// end does not depend on the maximum that was used).  Weights are rounded to bf16 for the second product, their sum is not.
+//
+// Roles: warps 0-3 and 4-7 the rows of the two tiles, warp 8 issues the products, warp 9 fetches (queries once, then
+// keys and values in turn through a ring of 32-KB stages, page by page).  Tensor memory: S_0, S_1, O_0, O_1.
+//
+// Tokens a row does not see get a score of -inf.  That is not enough for the second product, where 0 x NaN is NaN: in
+// tiles with a mask the values that no row of the CTA sees are cleared in shared memory (they may be anything: the end of
+// a page, pages given back), and if a value that some rows see and others do not is not finite, the CTA's rows are done
+// again without tensor cores (attend_row), exactly.
+//
+// Every wait is bounded; when one runs out the CTA raises its abort flag, all roles leave, what is in flight is awaited,
+// tensor memory is released and the status word reports DVM_ERR_DEVICE_TIMEOUT.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "dvm_attention.cuh"
+#include "dvm_attention_launch.h"
+#include "dvm_sm100.cuh"
+
+namespace dvm {
+namespace att {
+
+using namespace sm100;
+
+constexpr int PT = 128;                  // rows of a row tile, tokens of a cache tile
+constexpr int PROMPT_THREADS = 320;
+constexpr uint32_t HALF = PT * 128;      // 64 elements of 128 rows: 16 KB
+constexpr uint32_t SCORE_COLS = 128;
+constexpr float GROWTH = 8.f;            // log2 of how far weights may grow before the sums are rescaled
+
+template <int DP>  // head_dim rounded up to 64 or 128
+struct PromptSmem {
+  static constexpr uint32_t HALVES = DP / 64;
+  static constexpr uint32_t TILE = HALVES * HALF;
+  static constexpr uint32_t STAGES = DP == 128 ? 5 : 8;
+  static constexpr uint32_t RING = 2 * TILE;                     // behind the queries of both row tiles
+  static constexpr uint32_t BARS = RING + STAGES * TILE;         // full[], empty[], q, s[2], p[2], o[2], drain
+  static constexpr uint32_t WORDS = BARS + 16 * STAGES + 64;     // tensor memory address, abort, dirty[2], holes[8]
+  static constexpr uint32_t SCAN = WORDS + 48;                   // 12 sums, found request and block
+  static constexpr uint32_t BYTES = SCAN + 64 + 1024;
+};
+
+// kind::f16, bf16 x bf16 -> fp32, M = 128; A K-major; B K-major (keys) or N-major (values)
+constexpr uint32_t IDESC_QK = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(PT >> 3) << 17) | ((uint32_t)(PT >> 4) << 24);
+template <int DP> constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(DP >> 3) << 17) | ((uint32_t)(PT >> 4) << 24);
+// 128-byte swizzle: 8-row groups 1024 bytes apart; for the values the 64-column halves are HALF bytes apart
+__device__ __forceinline__ uint64_t desc_rows(uint32_t addr) {
+  return (uint64_t)((addr >> 4) & 0x3fff) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+__device__ __forceinline__ uint64_t desc_cols(uint32_t addr) {
+  return (uint64_t)((addr >> 4) & 0x3fff) | ((uint64_t)(HALF >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+// D += A B with A in tensor memory
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+               ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_load32(uint32_t taddr, float* v) {  // (the caller waits: tmem_load_wait)
+  uint32_t* r = (uint32_t*)v;
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_store16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *(const uint32_t*)&h;
+}
+// bits 0 .. n - 1
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+
+template <int DP>
+__global__ void __launch_bounds__(PROMPT_THREADS, 1)
+dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                            const __grid_constant__ Args a) {
+  using S = PromptSmem<DP>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  uint8_t* const sm = smem_raw + (base - raw);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t bar_full = base + S::BARS, bar_empty = bar_full + 8 * S::STAGES, bar_q = bar_empty + 8 * S::STAGES, bar_s = bar_q + 8, bar_p = bar_s + 16,
+                 bar_o = bar_p + 16, bar_drain = bar_o + 16;
+  volatile uint32_t* const words = (volatile uint32_t*)(sm + S::WORDS);
+  volatile uint32_t* const abort_flag = words + 1;
+  volatile uint32_t* const dirty = words + 2;
+  volatile uint32_t* const holes = words + 4;
+  int* const scan = (int*)(sm + S::SCAN);
+
+  // ---- which request and block of rows: the blocks of all requests in a row, a request's last block first ----
+  const int tokens = PT / a.group;  // of a row tile
+  const int block = blockIdx.x / a.hk, kvh = blockIdx.x - block * a.hk;
+  {
+    int before = 0;
+    bool found = false;
+    for (int i0 = 0; i0 < a.n; i0 += PROMPT_THREADS) {
+      const int i = i0 + threadIdx.x;
+      const int mine = i < a.n ? (min(request_at(a, i).q_len, a.max_q) + 2 * tokens - 1) / (2 * tokens) : 0;
+      int upto = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += y;
+      }
+      if (lane == 31) scan[warp] = upto;
+      __syncthreads();
+      int all = 0;
+#pragma unroll
+      for (int w = 0; w < PROMPT_THREADS / 32; ++w) {
+        if (w < warp) upto += scan[w];
+        all += scan[w];
+      }
+      const int at = block - before;
+      if (at >= upto - mine && at < upto) {
+        scan[12] = i;
+        scan[13] = upto - 1 - at;
+      }
+      __syncthreads();
+      found = at < all;
+      if (found) break;
+      before += all;
+    }
+    if (!found) return;  // (the grid is sized for the most blocks that `rows` rows can make)
+  }
+  const int request = scan[12], tok0 = scan[13] * 2 * tokens;
+  const Request rq = request_at(a, request);
+  const int n_tok = min(2 * tokens, min(rq.q_len, a.max_q) - tok0);
+  const long long p_first = rq.pos0 + tok0, p_last = p_first + n_tok - 1, held = (long long)a.max_blocks << a.page_log;
+  // tokens of the cache that some row sees: s < end and (s >= low or s < sinks); tiles: [0, ns), then [first, ...)
+  const int end = (int)max(0ll, min(p_last + 1, held));
+  const long long low_ll = a.window ? max(0ll, p_first - a.window + 1) : 0;
+  const int low = low_ll <= a.sinks ? 0 : (int)min(low_ll, 0x7fffffffll);
+  const int ns = low ? (min(a.sinks, end) + PT - 1) / PT : 0;
+  const int first = max(low / PT, ns);
+  // tiles that row tile x walks: its list ends with its own last position
+  auto tiles_of = [&](int x) -> int {
+    const int n = min(tokens, n_tok - x * tokens);
+    if (n <= 0) return 0;
+    const int last = (int)((max(0ll, min(p_first + x * tokens + n, held)) + PT - 1) / PT);
+    return last <= ns ? last : ns + max(0, last - first);
+  };
+  const int n0 = tiles_of(0), n1 = tiles_of(1), n_tiles = max(n0, n1);
+
+  if (threadIdx.x == 0) {
+    for (uint32_t s = 0; s < 2 * S::STAGES; ++s) mbar_init(bar_full + 8 * s, 1);
+    mbar_init(bar_q, 1);
+    for (uint32_t x = 0; x < 2; ++x) {
+      mbar_init(bar_s + 8 * x, 1);
+      mbar_init(bar_p + 8 * x, 4);  // (one arrival per warp)
+      mbar_init(bar_o + 8 * x, 1);
+      dirty[x] = 0;
+    }
+    mbar_init(bar_drain, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)words)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = words[0], tmem_o = tmem + 2 * SCORE_COLS;
+  auto tile_at = [&](int j) -> int { return j < ns ? j : first + (j - ns); };
+
+  uint32_t issued = 0, f_stage = 0, f_phase = 0;  // the fetching warp's ring, kept for the abort path
+  if (warp == 9) {
+    // ---------------- fetch ----------------
+    const int copy_log = min(a.page_log, 7), copies = PT >> copy_log;
+    const int* table = a.table + (long long)request * a.max_blocks;
+    auto page_of = [&](int j) -> int {  // of this lane's copy of tile j; -1 where it holds no token that some row sees
+      if (lane >= copies || j >= n_tiles) return -1;
+      const long long s = (long long)tile_at(j) * PT + ((long long)lane << copy_log);
+      if (s >= end || (s + (1 << copy_log) <= low && s >= a.sinks)) return -1;
+      const int page = table[s >> a.page_log];
+      return page >= 0 && page < a.pages ? page : -1;
+    };
+    if (lane == 0 && n_tiles > 0) {
+      const uint32_t rows = (uint32_t)(tokens * a.group) * 128 * S::HALVES;
+      mbar_expect_tx(bar_q, (n1 > 0 || n_tok > tokens ? 2 : 1) * rows);
+      for (int x = 0; x < (n1 > 0 || n_tok > tokens ? 2 : 1); ++x)
+        for (uint32_t h = 0; h < S::HALVES; ++h)
+          tma_load_4d(base + x * S::TILE + h * HALF, &tm_q, bar_q, 64 * h, 0, kvh, rq.s0 + tok0 + x * tokens);
+    }
+    __syncwarp();
+    bool ok = true;
+    int page = page_of(0);
+    for (int j = 0; ok && j < n_tiles; ++j) {
+      const int next = page_of(j + 1);  // (its latency hides behind the waits below)
+      const uint32_t missing = __ballot_sync(0xffffffffu, lane < copies && page < 0);
+      const int off = (int)(((long long)tile_at(j) * PT + ((long long)lane << copy_log)) & ((1ll << a.page_log) - 1));
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        ok = mbar_wait(bar_empty + 8 * f_stage, f_phase ^ 1, abort_flag);
+        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        const uint32_t full = bar_full + 8 * f_stage, at = base + S::RING + f_stage * S::TILE;
+        if (lane == 0) {
+          if (kv == 0) holes[j & 7] = missing;  // (read until the weights of tile j are done: the ring is fewer tiles deep)
+          mbar_expect_tx(full, S::TILE);
+        }
+        __syncwarp();
+        if (lane < copies)
+          for (uint32_t h = 0; h < S::HALVES; ++h)
+            tma_load_4d(at + h * HALF + ((uint32_t)lane << (copy_log + 7)), kv ? &tm_v : &tm_k, full, 64 * h, off, kvh, page);
+        ++issued;
+        if (++f_stage == S::STAGES) { f_stage = 0; f_phase ^= 1; }
+      }
+      page = next;
+    }
+    __syncwarp();
+  } else if (warp == 8) {
+    // ---------------- products ----------------
+    if (lane == 0 && n_tiles > 0) {
+      uint32_t stage = 0, phase = 0;
+      bool ok = mbar_wait(bar_q, 0, abort_flag) && mbar_wait(bar_full, 0, abort_flag);
+      auto step = [&]() { if (++stage == S::STAGES) { stage = 0; phase ^= 1; } };
+      auto qk = [&](int x, uint32_t st) {
+        const uint64_t qd = desc_rows(base + x * S::TILE), kd = desc_rows(base + S::RING + st * S::TILE);
+#pragma unroll
+        for (uint32_t k = 0; k < DP / 16; ++k) {
+          const uint32_t to = (k >> 2) * (HALF >> 4) + 2 * (k & 3);
+          umma_bf16(tmem + x * SCORE_COLS, qd + to, kd + to, IDESC_QK, k != 0);
+        }
+        umma_commit(bar_s + 8 * x);
+      };
+      if (ok) {
+        tc_fence_after();
+        if (n0 > 0) qk(0, 0);
+        if (n1 > 0) qk(1, 0);
+        umma_commit(bar_empty);
+        step();
+      }
+      for (int t = 0; ok && t < n_tiles; ++t) {
+        const uint32_t vst = stage;
+        ok = mbar_wait(bar_full + 8 * vst, phase, abort_flag);
+        if (!ok) break;
+        step();
+        bool next = false;
+        for (int x = 0; x < 2; ++x) {
+          const int nx = x ? n1 : n0;
+          if (t >= nx) continue;
+          ok = mbar_wait(bar_p + 8 * x, t & 1, abort_flag);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t vd = desc_cols(base + S::RING + vst * S::TILE);
+#pragma unroll
+          for (uint32_t k = 0; k < PT / 16; ++k)
+            umma_bf16_ts(tmem_o + x * DP, tmem + x * SCORE_COLS + 8 * k, vd + (uint64_t)(2048 >> 4) * k, IDESC_PV<DP>, (t | k) != 0);
+          if (x == (t < n1 ? 1 : 0)) umma_commit(bar_empty + 8 * vst);  // the last product that reads these values
+          if (t + 1 < nx) {
+            if (!next) {
+              ok = mbar_wait(bar_full + 8 * stage, phase, abort_flag);
+              if (!ok) break;
+              tc_fence_after();
+              next = true;
+            }
+            qk(x, stage);
+          } else {
+            umma_commit(bar_o + 8 * x);
+          }
+        }
+        if (ok && next) {
+          umma_commit(bar_empty + 8 * stage);
+          step();
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---------------- weights: one row per thread ----------------
+    const int x = warp >> 2, row = (warp & 3) * 32 + lane;
+    const int tok = row / a.group, head = row - tok * a.group;  // of the row tile; of the group
+    const int n_rows = min(tokens, n_tok - x * tokens);         // tokens of this row tile
+    const bool valid = tok < n_rows;
+    const int nx = x ? n1 : n0;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t t_s = tmem + x * SCORE_COLS + lanes, t_o = tmem_o + x * DP + lanes;
+    const float c = a.scale * 1.4426950408889634f;
+    const long long p0 = p_first + x * tokens, p = p0 + tok;     // position of the row tile's first token, of this row
+    float m = -INFINITY, l = 0.f;
+    bool ok = true;
+    for (int t = 0; t < nx; ++t) {
+      ok = mbar_wait(bar_s + 8 * x, t & 1, abort_flag);
+      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      tc_fence_after();
+      float s[PT];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) tmem_load32(t_s + 32 * q, s + 32 * q);
+      const long long key0 = (long long)tile_at(t) * PT;
+      const uint32_t missing = holes[t & 7];
+      const bool whole = missing == 0 && key0 + PT - 1 <= p0 && key0 + PT <= held &&
+                         (a.window == 0 || key0 > p0 + n_rows - 1 - a.window || key0 + PT <= a.sinks);
+      tmem_load_wait();
+      if (!whole) {
+        // bit i of seen[w]: this row sees token key0 + 32 w + i
+        const int hi = (int)max(-1ll, min(min(p, held - 1) - key0, (long long)PT));                 // columns up to hi
+        const int lo = a.window ? (int)max(0ll, min(p - a.window + 1 - key0, (long long)PT)) : 0;   // from lo on
+        const int sk = (int)max(0ll, min((long long)a.sinks - key0, (long long)PT));                // or below sk
+        const int copy_log = min(a.page_log, 7);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          uint32_t seen = bits_below(hi + 1 - 32 * w) & (~bits_below(lo - 32 * w) | bits_below(sk - 32 * w));
+          if (missing) {
+            uint32_t there = 0;
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+              if (!((missing >> ((32 * w + 8 * b) >> copy_log)) & 1u)) there |= 0xffu << (8 * b);
+            seen &= there;
+          }
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (!((seen >> i) & 1u)) s[32 * w + i] = -INFINITY;
+        }
+        // the values of this tile (thread r: token r): cleared where no row of the CTA sees them, else looked at
+        const uint32_t vi = 2 * t + 1;
+        ok = mbar_wait(bar_full + 8 * (vi % S::STAGES), (vi / S::STAGES) & 1, abort_flag);
+        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        const long long tokn = key0 + row;
+        const bool any = tokn < end && (tokn >= low || tokn < a.sinks) && !((missing >> (row >> copy_log)) & 1u);
+        uint8_t* const v = sm + S::RING + (vi % S::STAGES) * S::TILE + row * 128;
+        __nv_bfloat162 test = __float2bfloat162_rn(0.f);
+#pragma unroll
+        for (uint32_t q = 0; q < 8 * S::HALVES; ++q) {
+          uint4* const at = (uint4*)(v + (q >> 3) * HALF + (((q & 7) ^ (row & 7)) << 4));
+          if (any) {
+            const uint4 w = *at;
+            const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
+            test = __hfma2(*(const __nv_bfloat162*)&w.x, zero, test);
+            test = __hfma2(*(const __nv_bfloat162*)&w.y, zero, test);
+            test = __hfma2(*(const __nv_bfloat162*)&w.z, zero, test);
+            test = __hfma2(*(const __nv_bfloat162*)&w.w, zero, test);
+          } else {
+            *at = make_uint4(0, 0, 0, 0);
+          }
+        }
+        if (__isnan(__low2float(test)) || __isnan(__high2float(test))) dirty[x] = 1;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      }
+      float top = -INFINITY;
+      {
+        float t0 = s[0], t1 = s[1], t2 = s[2], t3 = s[3];
+#pragma unroll
+        for (int i = 4; i < PT; i += 4) { t0 = fmaxf(t0, s[i]); t1 = fmaxf(t1, s[i + 1]); t2 = fmaxf(t2, s[i + 2]); t3 = fmaxf(t3, s[i + 3]); }
+        top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3));
+      }
+      const float m_new = fmaxf(m, top);
+      if (__any_sync(0xffffffffu, (m_new - m) * c > GROWTH)) {  // (from -inf: yes, unless it stays there)
+        const float keep = m_new == m ? 1.f : ex2((m - m_new) * c);
+        l *= keep;
+        m = m_new;
+        if (t > 0) {
+#pragma unroll
+          for (int q = 0; q < DP / 32; ++q) {
+            float o[32];
+            tmem_load32(t_o + 32 * q, o);
+            tmem_load_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] *= keep;
+            tmem_st32(t_o + 32 * q, o);
+          }
+        }
+      }
+      const float off = m == -INFINITY ? 0.f : -m * c;
+      float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint32_t pk[16];
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+          const float w0 = ex2(fmaf(s[32 * q + 2 * i], c, off)), w1 = ex2(fmaf(s[32 * q + 2 * i + 1], c, off));
+          const float w2 = ex2(fmaf(s[32 * q + 2 * i + 2], c, off)), w3 = ex2(fmaf(s[32 * q + 2 * i + 3], c, off));
+          l0 += w0; l1 += w1; l2 += w2; l3 += w3;
+          pk[i] = pack_bf16(w0, w1);
+          pk[i + 1] = pack_bf16(w2, w3);
+        }
+        tmem_store16(t_s + 16 * q, pk);
+      }
+      l += (l0 + l1) + (l2 + l3);
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_p + 8 * x);
+    }
+    // ---- the row's quotient ----
+    if (n_rows > 0) {
+      if (ok && nx > 0) ok = mbar_wait(bar_o + 8 * x, 0, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+      if (ok) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const long long at = (long long)(rq.s0 + tok0 + x * tokens + tok) * a.os[0] + (long long)(kvh * a.group + head) * a.os[1];
+#pragma unroll
+        for (int q = 0; q < DP / 32; ++q) {
+          float o[32];
+          if (nx > 0) {
+            tmem_load32(t_o + 32 * q, o);
+            tmem_load_wait();
+          }
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = nx > 0 && l != 0.f ? o[i] * inv : 0.f;
+          if (valid) {
+            if (a.out_vec && a.out_bf16) {
+              uint4* out = (uint4*)((__nv_bfloat16*)a.out + at + 32 * q);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (32 * q + 8 * i < a.D)
+                  out[i] = make_uint4(pack_bf16(o[8 * i], o[8 * i + 1]), pack_bf16(o[8 * i + 2], o[8 * i + 3]), pack_bf16(o[8 * i + 4], o[8 * i + 5]),
+                                      pack_bf16(o[8 * i + 6], o[8 * i + 7]));
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (32 * q + i < a.D) put(a.out, a.out_bf16, at + 32 * q + i, o[i]);
+            }
+          }
+        }
+      }
+    }
+  }
+
+  // ---------------- teardown ----------------
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {
+    if (warp == 9 && lane == 0) {  // the latest fill of every stage, and the queries
+      for (uint32_t k = min(issued, S::STAGES); k > 0; --k) {
+        if (f_stage == 0) { f_stage = S::STAGES - 1; f_phase ^= 1; } else --f_stage;
+        if (!mbar_try(bar_full + 8 * f_stage, f_phase)) mbar_wait_slow(bar_full + 8 * f_stage, f_phase, abort_flag, DRAIN_NS, false);
+      }
+      if (n_tiles > 0 && !mbar_try(bar_q, 0)) mbar_wait_slow(bar_q, 0, abort_flag, DRAIN_NS, false);
+    }
+    if (warp == 8 && lane == 0) {
+      umma_commit(bar_drain);
+      if (!mbar_try(bar_drain, 0)) mbar_wait_slow(bar_drain, 0, abort_flag, DRAIN_NS, false);
+    }
+    if (threadIdx.x == 0) atomicMax(a.status, (unsigned int)ST_TIMEOUT);
+    __syncthreads();
+  } else if (warp < 8 && dirty[warp >> 2]) {
+    const int x = warp >> 2;
+    for (int r = warp & 3; r < min(tokens, n_tok - x * tokens) * a.group; r += 4) {
+      const int tok = r / a.group;
+      attend_row<__nv_bfloat16>(a, request, p_first + x * tokens + tok, rq.s0 + tok0 + x * tokens + tok, kvh * a.group + (r - tok * a.group));
+    }
+  }
+  if (warp == 8) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  }
+}
+
+template <int DP>
+int launch_prompt(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Args& a, int grid, cudaStream_t stream) {
+  DVM_CUDA(cudaFuncSetAttribute(dvm_attention_prompt_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PromptSmem<DP>::BYTES));
+  dvm_attention_prompt_kernel<DP><<<grid, PROMPT_THREADS, PromptSmem<DP>::BYTES, stream>>>(q, k, v, a);
+  DVM_CUDA(cudaGetLastError());
+  dvm_count_launch();
+  return DVM_OK;
+}
+
+}  // namespace att
+}  // namespace dvm
+
+int dvm_launch_attention_prompt(const dvm_attention_desc& d, const dvm::att::Args& a, cudaStream_t stream) {
+  using namespace dvm::att;
+  const int tokens = PT / a.group;
+  CUtensorMap q, k, v;
+  int st = dvm_query_map(d, a.q, tokens, &q);
+  if (st == DVM_OK) st = dvm_cache_map(d, d.k_stride, a.k, PT, &k);
+  if (st == DVM_OK) st = dvm_cache_map(d, d.v_stride, a.v, PT, &v);
+  if (st != DVM_OK) return st;
+  // the most blocks of 2 x tokens query tokens that the requests can have
+  const int64_t per = 2 * tokens, by_rows = (d.rows + d.requests * (per - 1)) / per, by_max = d.requests * ((d.max_q + per - 1) / per);
+  const int64_t grid = (by_rows < by_max ? by_rows : by_max) * d.kv_heads;
+  if (grid >= (1ll << 31)) return DVM_ERR_TOO_LARGE;
+  return a.D <= 64 ? launch_prompt<64>(q, k, v, a, (int)grid, stream) : launch_prompt<128>(q, k, v, a, (int)grid, stream);
+}
