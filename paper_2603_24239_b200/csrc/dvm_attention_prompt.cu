@@ -83,6 +83,14 @@ __device__ __forceinline__ void tmem_load32(uint32_t taddr, float* v) {  // (the
       : "memory");
 }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// ... and what was loaded is used behind the wait only (the wait itself names no registers)
+__device__ __forceinline__ void tmem_landed(float* v) {
+  tmem_load_wait();
+  asm volatile("" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), 
+                    "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), 
+                    "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]), 
+                    "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31]));
+}
 __device__ __forceinline__ void tmem_store16(uint32_t taddr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
@@ -316,14 +324,11 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       ok = mbar_wait(bar_s + 8 * x, t & 1, abort_flag);
       if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
       tc_fence_after();
-      float s[PT];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) tmem_load32(t_s + 32 * q, s + 32 * q);
       const long long key0 = (long long)tile_at(t) * PT;
       const uint32_t missing = holes[t & 7];
       const bool whole = missing == 0 && key0 + PT - 1 <= p0 && key0 + PT <= held &&
                          (a.window == 0 || key0 > p0 + n_rows - 1 - a.window || key0 + PT <= a.sinks);
-      tmem_load_wait();
+      uint32_t seen[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
       if (!whole) {
         // bit i of seen[w]: this row sees token key0 + 32 w + i
         const int hi = (int)max(-1ll, min(min(p, held - 1) - key0, (long long)PT));                 // columns up to hi
@@ -332,17 +337,14 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         const int copy_log = min(a.page_log, 7);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          uint32_t seen = bits_below(hi + 1 - 32 * w) & (~bits_below(lo - 32 * w) | bits_below(sk - 32 * w));
+          seen[w] = bits_below(hi + 1 - 32 * w) & (~bits_below(lo - 32 * w) | bits_below(sk - 32 * w));
           if (missing) {
             uint32_t there = 0;
 #pragma unroll
             for (int b = 0; b < 4; ++b)
               if (!((missing >> ((32 * w + 8 * b) >> copy_log)) & 1u)) there |= 0xffu << (8 * b);
-            seen &= there;
+            seen[w] &= there;
           }
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (!((seen >> i) & 1u)) s[32 * w + i] = -INFINITY;
         }
         // the values of this tile (thread r: token r): cleared where no row of the CTA sees them, else looked at
         const uint32_t vi = 2 * t + 1;
@@ -369,13 +371,28 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         if (__isnan(__low2float(test)) || __isnan(__high2float(test))) dirty[x] = 1;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       }
+      // The scores are read from tensor memory twice, 32 columns at a time with the next 32 on their way: once for the
+      // maximum, once for the weights.  (Holding all 128 takes more registers than a thread has.)
+      float buf[2][32];
+      auto hide = [&](float* s, uint32_t bits) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (!((bits >> i) & 1u)) s[i] = -INFINITY;
+      };
       float top = -INFINITY;
-      {
+      tmem_load32(t_s, buf[0]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float* const s = buf[q & 1];
+        tmem_landed(s);
+        if (q < 3) tmem_load32(t_s + 32 * (q + 1), buf[(q + 1) & 1]);
+        if (!whole) hide(s, seen[q]);
         float t0 = s[0], t1 = s[1], t2 = s[2], t3 = s[3];
 #pragma unroll
-        for (int i = 4; i < PT; i += 4) { t0 = fmaxf(t0, s[i]); t1 = fmaxf(t1, s[i + 1]); t2 = fmaxf(t2, s[i + 2]); t3 = fmaxf(t3, s[i + 3]); }
-        top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3));
+        for (int i = 4; i < 32; i += 4) { t0 = fmaxf(t0, s[i]); t1 = fmaxf(t1, s[i + 1]); t2 = fmaxf(t2, s[i + 2]); t3 = fmaxf(t3, s[i + 3]); }
+        top = fmaxf(top, fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)));
       }
+      tmem_load32(t_s, buf[0]);
       const float m_new = fmaxf(m, top);
       if (__any_sync(0xffffffffu, (m_new - m) * c > GROWTH)) {  // (from -inf: yes, unless it stays there)
         const float keep = m_new == m ? 1.f : ex2((m - m_new) * c);
@@ -386,7 +403,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
           for (int q = 0; q < DP / 32; ++q) {
             float o[32];
             tmem_load32(t_o + 32 * q, o);
-            tmem_load_wait();
+            tmem_landed(o);
 #pragma unroll
             for (int i = 0; i < 32; ++i) o[i] *= keep;
             tmem_st32(t_o + 32 * q, o);
@@ -397,16 +414,20 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
+        float* const s = buf[q & 1];
+        tmem_landed(s);
+        if (q < 3) tmem_load32(t_s + 32 * (q + 1), buf[(q + 1) & 1]);
+        if (!whole) hide(s, seen[q]);
         uint32_t pk[16];
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
-          const float w0 = ex2(fmaf(s[32 * q + 2 * i], c, off)), w1 = ex2(fmaf(s[32 * q + 2 * i + 1], c, off));
-          const float w2 = ex2(fmaf(s[32 * q + 2 * i + 2], c, off)), w3 = ex2(fmaf(s[32 * q + 2 * i + 3], c, off));
+          const float w0 = ex2(fmaf(s[2 * i], c, off)), w1 = ex2(fmaf(s[2 * i + 1], c, off));
+          const float w2 = ex2(fmaf(s[2 * i + 2], c, off)), w3 = ex2(fmaf(s[2 * i + 3], c, off));
           l0 += w0; l1 += w1; l2 += w2; l3 += w3;
           pk[i] = pack_bf16(w0, w1);
           pk[i + 1] = pack_bf16(w2, w3);
         }
-        tmem_store16(t_s + 16 * q, pk);
+        tmem_store16(t_s + 16 * q, pk);  // (over scores that have been read)
       }
       l += (l0 + l1) + (l2 + l3);
       tmem_st_wait();
@@ -427,7 +448,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
           float o[32];
           if (nx > 0) {
             tmem_load32(t_o + 32 * q, o);
-            tmem_load_wait();
+            tmem_landed(o);
           }
 #pragma unroll
           for (int i = 0; i < 32; ++i) o[i] = nx > 0 && l != 0.f ? o[i] * inv : 0.f;
@@ -448,6 +469,11 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         }
       }
     }
+    // a value that some of these rows see and others do not was not finite: the rows again, one warp each
+    asm volatile("bar.sync 1, 256;" ::: "memory");  // (every warp of the two row tiles comes here)
+    if (dirty[x] && !*abort_flag)
+      for (int r = warp & 3; r < n_rows * a.group; r += 4)
+        attend_row<__nv_bfloat16>(a, request, p0 + r / a.group, rq.s0 + tok0 + x * tokens + r / a.group, kvh * a.group + r % a.group);
   }
 
   // ---------------- teardown ----------------
@@ -467,12 +493,6 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     }
     if (threadIdx.x == 0) atomicMax(a.status, (unsigned int)ST_TIMEOUT);
     __syncthreads();
-  } else if (warp < 8 && dirty[warp >> 2]) {
-    const int x = warp >> 2;
-    for (int r = warp & 3; r < min(tokens, n_tok - x * tokens) * a.group; r += 4) {
-      const int tok = r / a.group;
-      attend_row<__nv_bfloat16>(a, request, p_first + x * tokens + tok, rq.s0 + tok0 + x * tokens + tok, kvh * a.group + (r - tok * a.group));
-    }
   }
   if (warp == 8) {
     tc_fence_after();
