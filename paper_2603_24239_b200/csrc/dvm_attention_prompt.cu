@@ -39,6 +39,7 @@ constexpr int PT = 128;                  // rows of a row tile, tokens of a cach
 constexpr int PROMPT_THREADS = 320;
 constexpr uint32_t HALF = PT * 128;      // 64 elements of 128 rows: 16 KB
 constexpr uint32_t SCORE_COLS = 128;
+constexpr uint32_t WEIGHT_AT = 64;        // the weights' columns within the scores': the upper half
 constexpr float GROWTH = 8.f;            // log2 of how far weights may grow before the sums are rescaled
 
 template <int DP>  // head_dim rounded up to 64 or 128
@@ -97,6 +98,21 @@ __device__ __forceinline__ void tmem_store16(uint32_t taddr, const uint32_t* r) 
       ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
         "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
       : "memory");
+}
+// two fp32 operations in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
 }
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -286,7 +302,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
           const uint64_t vd = desc_cols(base + S::RING + vst * S::TILE);
 #pragma unroll
           for (uint32_t k = 0; k < PT / 16; ++k)
-            umma_bf16_ts(tmem_o + x * DP, tmem + x * SCORE_COLS + 8 * k, vd + (uint64_t)(2048 >> 4) * k, IDESC_PV<DP>, (t | k) != 0);
+            umma_bf16_ts(tmem_o + x * DP, tmem + x * SCORE_COLS + WEIGHT_AT + 8 * k, vd + (uint64_t)(2048 >> 4) * k, IDESC_PV<DP>, (t | k) != 0);
           if (x == (t < n1 ? 1 : 0)) umma_commit(bar_empty + 8 * vst);  // the last product that reads these values
           if (t + 1 < nx) {
             if (!next) {
@@ -324,6 +340,11 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       ok = mbar_wait(bar_s + 8 * x, t & 1, abort_flag);
       if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
       tc_fence_after();
+      // Registers hold 96 of the 128 scores of a row at most: the lower half is read for the maximum, then the upper half,
+      // whose weights come first while the lower half is read again.
+      float lo_s[2][32], hi_s[2][32];
+      tmem_load32(t_s, lo_s[0]);
+      tmem_load32(t_s + 32, lo_s[1]);
       const long long key0 = (long long)tile_at(t) * PT;
       const uint32_t missing = holes[t & 7];
       const bool whole = missing == 0 && key0 + PT - 1 <= p0 && key0 + PT <= held &&
@@ -371,28 +392,27 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         if (__isnan(__low2float(test)) || __isnan(__high2float(test))) dirty[x] = 1;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       }
-      // The scores are read from tensor memory twice, 32 columns at a time with the next 32 on their way: once for the
-      // maximum, once for the weights.  (Holding all 128 takes more registers than a thread has.)
-      float buf[2][32];
       auto hide = [&](float* s, uint32_t bits) {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
           if (!((bits >> i) & 1u)) s[i] = -INFINITY;
       };
-      float top = -INFINITY;
-      tmem_load32(t_s, buf[0]);
+      auto highest = [](const float* s, float top) -> float {
+        float t0 = top, t1 = s[0], t2 = s[1], t3 = s[2];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float* const s = buf[q & 1];
-        tmem_landed(s);
-        if (q < 3) tmem_load32(t_s + 32 * (q + 1), buf[(q + 1) & 1]);
-        if (!whole) hide(s, seen[q]);
-        float t0 = s[0], t1 = s[1], t2 = s[2], t3 = s[3];
-#pragma unroll
-        for (int i = 4; i < 32; i += 4) { t0 = fmaxf(t0, s[i]); t1 = fmaxf(t1, s[i + 1]); t2 = fmaxf(t2, s[i + 2]); t3 = fmaxf(t3, s[i + 3]); }
-        top = fmaxf(top, fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)));
-      }
-      tmem_load32(t_s, buf[0]);
+        for (int i = 3; i < 31; i += 4) { t0 = fmaxf(t0, s[i]); t1 = fmaxf(t1, s[i + 1]); t2 = fmaxf(t2, s[i + 2]); t3 = fmaxf(t3, s[i + 3]); }
+        return fmaxf(fmaxf(fmaxf(t0, s[31]), t1), fmaxf(t2, t3));
+      };
+      tmem_landed(lo_s[0]);
+      tmem_landed(lo_s[1]);
+      tmem_load32(t_s + 64, hi_s[0]);
+      tmem_load32(t_s + 96, hi_s[1]);
+      if (!whole) { hide(lo_s[0], seen[0]); hide(lo_s[1], seen[1]); }
+      float top = highest(lo_s[1], highest(lo_s[0], -INFINITY));
+      tmem_landed(hi_s[0]);
+      tmem_landed(hi_s[1]);
+      if (!whole) { hide(hi_s[0], seen[2]); hide(hi_s[1], seen[3]); }
+      top = highest(hi_s[1], highest(hi_s[0], top));
       const float m_new = fmaxf(m, top);
       if (__any_sync(0xffffffffu, (m_new - m) * c > GROWTH)) {  // (from -inf: yes, unless it stays there)
         const float keep = m_new == m ? 1.f : ex2((m - m_new) * c);
@@ -411,25 +431,32 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         }
       }
       const float off = m == -INFINITY ? 0.f : -m * c;
-      float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float* const s = buf[q & 1];
-        tmem_landed(s);
-        if (q < 3) tmem_load32(t_s + 32 * (q + 1), buf[(q + 1) & 1]);
-        if (!whole) hide(s, seen[q]);
+      float2 l01 = make_float2(0.f, 0.f), l23 = l01;
+      const float2 cc = make_float2(c, c), oo = make_float2(off, off);
+      auto weigh = [&](const float* s, int q) {  // 32 columns: weights, their sum, the bf16 ones to tensor memory
         uint32_t pk[16];
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
-          const float w0 = ex2(fmaf(s[2 * i], c, off)), w1 = ex2(fmaf(s[2 * i + 1], c, off));
-          const float w2 = ex2(fmaf(s[2 * i + 2], c, off)), w3 = ex2(fmaf(s[2 * i + 3], c, off));
-          l0 += w0; l1 += w1; l2 += w2; l3 += w3;
-          pk[i] = pack_bf16(w0, w1);
-          pk[i + 1] = pack_bf16(w2, w3);
+          const float2 x0 = fma2(make_float2(s[2 * i], s[2 * i + 1]), cc, oo), x1 = fma2(make_float2(s[2 * i + 2], s[2 * i + 3]), cc, oo);
+          const float2 w0 = make_float2(ex2(x0.x), ex2(x0.y)), w1 = make_float2(ex2(x1.x), ex2(x1.y));
+          l01 = add2(l01, w0);
+          l23 = add2(l23, w1);
+          pk[i] = pack_bf16(w0.x, w0.y);
+          pk[i + 1] = pack_bf16(w1.x, w1.y);
         }
-        tmem_store16(t_s + 16 * q, pk);  // (over scores that have been read)
-      }
-      l += (l0 + l1) + (l2 + l3);
+        tmem_store16(t_s + WEIGHT_AT + 16 * q, pk);  // (over scores that have been read)
+      };
+      tmem_load32(t_s, lo_s[0]);
+      weigh(hi_s[0], 2);
+      tmem_landed(lo_s[0]);
+      tmem_load32(t_s + 32, lo_s[1]);
+      weigh(hi_s[1], 3);
+      if (!whole) hide(lo_s[0], seen[0]);
+      weigh(lo_s[0], 0);
+      tmem_landed(lo_s[1]);
+      if (!whole) hide(lo_s[1], seen[1]);
+      weigh(lo_s[1], 1);
+      l += (l01.x + l01.y) + (l23.x + l23.y);
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
