@@ -1,20 +1,22 @@
 // Attention of prompts: many query rows per request, on the tensor cores.
 //
 // A CTA takes two tiles of 128 rows of one kv head: a row is a (token, query head of the group) pair, so heads that share
-// keys share the loads, and 2 x floor(128 / group) tokens move through the cache together.  Per tile of 128 tokens of the
+// keys share the loads, and 2 x floor(128 / group) tokens move through the cache together.  Per tile t of 64 tokens of the
 // cache and row tile x:
-//   S_x = Q_x K^T        tcgen05.mma, both operands in shared memory, S_x in tensor memory (128 fp32 columns)
+//   S_x = Q_x K^T        tcgen05.mma, both operands in shared memory, S_x in tensor memory (64 fp32 columns)
 //   P_x = 2^(c S_x - m)  128 threads, one row each: running maximum m and sum, no exchange between threads;
 //                        P_x goes back to tensor memory as bf16, over the S_x it came from
 //   O_x += P_x V         tcgen05.mma with P_x as the tensor-memory operand
-// While the threads of one row tile work on its weights, the tensor cores run the products of the other.  The products of
-// a row tile are issued in the order PV(t), QK(t + 1) by one thread and complete in that order, so a finished S_x(t + 1)
-// also says that O_x holds PV(t): the rescaling of O_x by a new maximum needs no barrier of its own.  It is skipped until
-// the maximum has grown by more than 2^8 (weights stay below 2^8, far from any bound of bf16 or fp32; the quotient at the
-// end does not depend on the maximum that was used).  Weights are rounded to bf16 for the second product, their sum is not.
+// S_x has two places, t and t + 1 in turn: S_x(t + 1) is there before P_x(t) is done, so neither the tensor cores nor the
+// threads wait for the other's whole latency.  (Tiles of 128 tokens leave room for one place only -- tensor memory is
+// S_0, S_1, O_0, O_1 and full -- and then the threads waited 1850 of 4300 cycles per 128 tokens.)  One thread issues
+// all products, PV_x(t) then QK_x(t + 2), and they complete in that order: QK_x(t + 2) overwrites P_x(t) after its use.
+// O_x is rescaled by a new maximum only when that has grown by more than 2^8 (weights stay below 2^8, far from any bound
+// of bf16 or fp32; the quotient at the end does not depend on the maximum that was used); then the row's thread waits for
+// PV_x(t - 1).  Weights are rounded to bf16 for the second product, their sum is not.
 //
 // Roles: warps 0-3 and 4-7 the rows of the two tiles, warp 8 issues the products, warp 9 fetches (queries once, then
-// keys and values in turn through a ring of 32-KB stages, page by page).  Tensor memory: S_0, S_1, O_0, O_1.
+// keys and values in turn through a ring, page by page).
 //
 // Tokens a row does not see get a score of -inf.  That is not enough for the second product, where 0 x NaN is NaN: in
 // tiles with a mask the values that no row of the CTA sees are cleared in shared memory (they may be anything: the end of
@@ -35,34 +37,40 @@ namespace att {
 
 using namespace sm100;
 
-constexpr int PT = 128;                  // rows of a row tile, tokens of a cache tile
+constexpr int PT = 128;                  // rows of a row tile
+constexpr int KT = 64;                   // tokens of a cache tile
 constexpr int PROMPT_THREADS = 320;
-constexpr uint32_t HALF = PT * 128;      // 64 elements of 128 rows: 16 KB
-constexpr uint32_t SCORE_COLS = 128;
-constexpr uint32_t WEIGHT_AT = 64;        // the weights' columns within the scores': the upper half
+constexpr uint32_t Q_HALF = PT * 128;    // 64 elements of the rows: 16 KB
+constexpr uint32_t KV_HALF = KT * 128;   // 64 elements of the tokens: 8 KB
+constexpr int HOLES = 16;                // tiles whose missing pages are remembered: more than the ring is deep
 constexpr float GROWTH = 8.f;            // log2 of how far weights may grow before the sums are rescaled
 
 template <int DP>  // head_dim rounded up to 64 or 128
 struct PromptSmem {
   static constexpr uint32_t HALVES = DP / 64;
-  static constexpr uint32_t TILE = HALVES * HALF;
-  static constexpr uint32_t STAGES = DP == 128 ? 5 : 8;
-  static constexpr uint32_t RING = 2 * TILE;                     // behind the queries of both row tiles
-  static constexpr uint32_t BARS = RING + STAGES * TILE;         // full[], empty[], q, s[2], p[2], o[2], drain
-  static constexpr uint32_t WORDS = BARS + 16 * STAGES + 64;     // tensor memory address, abort, dirty[2], holes[8]
-  static constexpr uint32_t SCAN = WORDS + 48;                   // 12 sums, found request and block
+  static constexpr uint32_t Q_TILE = HALVES * Q_HALF;
+  static constexpr uint32_t STAGE = HALVES * KV_HALF;            // keys or values of a tile
+  static constexpr uint32_t STAGES = DP == 128 ? 10 : 16;
+  static constexpr uint32_t RING = 2 * Q_TILE;                   // behind the queries of both row tiles
+  static constexpr uint32_t BARS = RING + STAGES * STAGE;        // full[], empty[], q, s[2][2], p[2][2], o[2][2], drain
+  static constexpr uint32_t WORDS = BARS + 16 * STAGES + 112;     // tensor memory address, abort, dirty[2], holes[]
+  static constexpr uint32_t SCAN = WORDS + 16 + 4 * HOLES;       // 12 sums, found request and block
   static constexpr uint32_t BYTES = SCAN + 64 + 1024;
+  static_assert(STAGES / 2 + 3 <= HOLES, "a tile's holes are kept until its weights are done");
 };
 
 // kind::f16, bf16 x bf16 -> fp32, M = 128; A K-major; B K-major (keys) or N-major (values)
-constexpr uint32_t IDESC_QK = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(PT >> 3) << 17) | ((uint32_t)(PT >> 4) << 24);
+constexpr uint32_t IDESC_QK = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(KT >> 3) << 17) | ((uint32_t)(PT >> 4) << 24);
 template <int DP> constexpr uint32_t IDESC_PV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(DP >> 3) << 17) | ((uint32_t)(PT >> 4) << 24);
-// 128-byte swizzle: 8-row groups 1024 bytes apart; for the values the 64-column halves are HALF bytes apart
-__device__ __forceinline__ uint64_t desc_rows(uint32_t addr) {
-  return (uint64_t)((addr >> 4) & 0x3fff) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+// 128-byte swizzle: 8-row groups 1024 bytes apart; for the values the 64-column halves are KV_HALF bytes apart
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t leading) { return ((addr >> 4) & 0x3fff) | (leading << 16); }
+__device__ __forceinline__ uint64_t desc_of(uint32_t lo) {
+  return lo | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
-__device__ __forceinline__ uint64_t desc_cols(uint32_t addr) {
-  return (uint64_t)((addr >> 4) & 0x3fff) | ((uint64_t)(HALF >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
 }
 // D += A B with A in tensor memory
 __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
@@ -134,9 +142,9 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* const sm = smem_raw + (base - raw);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t bar_full = base + S::BARS, bar_empty = bar_full + 8 * S::STAGES, bar_q = bar_empty + 8 * S::STAGES, bar_s = bar_q + 8, bar_p = bar_s + 16,
-                 bar_o = bar_p + 16, bar_drain = bar_o + 16;
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;  // (the warp's number: known to be uniform)
+  const uint32_t bar_full = base + S::BARS, bar_empty = bar_full + 8 * S::STAGES, bar_q = bar_empty + 8 * S::STAGES, bar_s = bar_q + 8, bar_p = bar_s + 32,
+                 bar_o = bar_p + 32, bar_drain = bar_o + 32;  // s, p, o: of row tile x and place b = t & 1 at 16 x + 8 b
   volatile uint32_t* const words = (volatile uint32_t*)(sm + S::WORDS);
   volatile uint32_t* const abort_flag = words + 1;
   volatile uint32_t* const dirty = words + 2;
@@ -186,13 +194,13 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
   const int end = (int)max(0ll, min(p_last + 1, held));
   const long long low_ll = a.window ? max(0ll, p_first - a.window + 1) : 0;
   const int low = low_ll <= a.sinks ? 0 : (int)min(low_ll, 0x7fffffffll);
-  const int ns = low ? (min(a.sinks, end) + PT - 1) / PT : 0;
-  const int first = max(low / PT, ns);
+  const int ns = low ? (min(a.sinks, end) + KT - 1) / KT : 0;
+  const int first = max(low / KT, ns);
   // tiles that row tile x walks: its list ends with its own last position
   auto tiles_of = [&](int x) -> int {
     const int n = min(tokens, n_tok - x * tokens);
     if (n <= 0) return 0;
-    const int last = (int)((max(0ll, min(p_first + x * tokens + n, held)) + PT - 1) / PT);
+    const int last = (int)((max(0ll, min(p_first + x * tokens + n, held)) + KT - 1) / KT);
     return last <= ns ? last : ns + max(0, last - first);
   };
   const int n0 = tiles_of(0), n1 = tiles_of(1), n_tiles = max(n0, n1);
@@ -201,9 +209,11 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     for (uint32_t s = 0; s < 2 * S::STAGES; ++s) mbar_init(bar_full + 8 * s, 1);
     mbar_init(bar_q, 1);
     for (uint32_t x = 0; x < 2; ++x) {
-      mbar_init(bar_s + 8 * x, 1);
-      mbar_init(bar_p + 8 * x, 4);  // (one arrival per warp)
-      mbar_init(bar_o + 8 * x, 1);
+      for (uint32_t b = 0; b < 2; ++b) {
+        mbar_init(bar_s + 16 * x + 8 * b, 1);
+        mbar_init(bar_p + 16 * x + 8 * b, 4);  // (one arrival per warp)
+        mbar_init(bar_o + 16 * x + 8 * b, 1);
+      }
       dirty[x] = 0;
     }
     mbar_init(bar_drain, 1);
@@ -217,17 +227,17 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = words[0], tmem_o = tmem + 2 * SCORE_COLS;
+  const uint32_t tmem = words[0], tmem_o = tmem + 4 * KT;  // S_x at place b: 64 (2 x + b)
   auto tile_at = [&](int j) -> int { return j < ns ? j : first + (j - ns); };
 
   uint32_t issued = 0, f_stage = 0, f_phase = 0;  // the fetching warp's ring, kept for the abort path
   if (warp == 9) {
     // ---------------- fetch ----------------
-    const int copy_log = min(a.page_log, 7), copies = PT >> copy_log;
+    const int copy_log = min(a.page_log, 6), copies = KT >> copy_log;
     const int* table = a.table + (long long)request * a.max_blocks;
     auto page_of = [&](int j) -> int {  // of this lane's copy of tile j; -1 where it holds no token that some row sees
       if (lane >= copies || j >= n_tiles) return -1;
-      const long long s = (long long)tile_at(j) * PT + ((long long)lane << copy_log);
+      const long long s = (long long)tile_at(j) * KT + ((long long)lane << copy_log);
       if (s >= end || (s + (1 << copy_log) <= low && s >= a.sinks)) return -1;
       const int page = table[s >> a.page_log];
       return page >= 0 && page < a.pages ? page : -1;
@@ -237,7 +247,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       mbar_expect_tx(bar_q, (n1 > 0 || n_tok > tokens ? 2 : 1) * rows);
       for (int x = 0; x < (n1 > 0 || n_tok > tokens ? 2 : 1); ++x)
         for (uint32_t h = 0; h < S::HALVES; ++h)
-          tma_load_4d(base + x * S::TILE + h * HALF, &tm_q, bar_q, 64 * h, 0, kvh, rq.s0 + tok0 + x * tokens);
+          tma_load_4d(base + x * S::Q_TILE + h * Q_HALF, &tm_q, bar_q, 64 * h, 0, kvh, rq.s0 + tok0 + x * tokens);
     }
     __syncwarp();
     bool ok = true;
@@ -245,20 +255,20 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     for (int j = 0; ok && j < n_tiles; ++j) {
       const int next = page_of(j + 1);  // (its latency hides behind the waits below)
       const uint32_t missing = __ballot_sync(0xffffffffu, lane < copies && page < 0);
-      const int off = (int)(((long long)tile_at(j) * PT + ((long long)lane << copy_log)) & ((1ll << a.page_log) - 1));
+      const int off = (int)(((long long)tile_at(j) * KT + ((long long)lane << copy_log)) & ((1ll << a.page_log) - 1));
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
         ok = mbar_wait(bar_empty + 8 * f_stage, f_phase ^ 1, abort_flag);
         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-        const uint32_t full = bar_full + 8 * f_stage, at = base + S::RING + f_stage * S::TILE;
+        const uint32_t full = bar_full + 8 * f_stage, at = base + S::RING + f_stage * S::STAGE;
         if (lane == 0) {
-          if (kv == 0) holes[j & 7] = missing;  // (read until the weights of tile j are done: the ring is fewer tiles deep)
-          mbar_expect_tx(full, S::TILE);
+          if (kv == 0) holes[j % HOLES] = missing;
+          mbar_expect_tx(full, S::STAGE);
         }
         __syncwarp();
         if (lane < copies)
           for (uint32_t h = 0; h < S::HALVES; ++h)
-            tma_load_4d(at + h * HALF + ((uint32_t)lane << (copy_log + 7)), kv ? &tm_v : &tm_k, full, 64 * h, off, kvh, page);
+            tma_load_4d(at + h * KV_HALF + ((uint32_t)lane << (copy_log + 7)), kv ? &tm_v : &tm_k, full, 64 * h, off, kvh, page);
         ++issued;
         if (++f_stage == S::STAGES) { f_stage = 0; f_phase ^= 1; }
       }
@@ -267,59 +277,68 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     __syncwarp();
   } else if (warp == 8) {
     // ---------------- products ----------------
-    if (lane == 0 && n_tiles > 0) {
-      uint32_t stage = 0, phase = 0;
-      bool ok = mbar_wait(bar_q, 0, abort_flag) && mbar_wait(bar_full, 0, abort_flag);
-      auto step = [&]() { if (++stage == S::STAGES) { stage = 0; phase ^= 1; } };
-      auto qk = [&](int x, uint32_t st) {
-        const uint64_t qd = desc_rows(base + x * S::TILE), kd = desc_rows(base + S::RING + st * S::TILE);
+    // The whole warp walks, so that descriptors and barriers stay in uniform registers; one elected lane issues.  (Issued
+    // from a branch of lane 0 alone, with the descriptors formed anew, a product took 70 to 100 cycles to issue, more than
+    // it takes to run.)
+    const bool leader = elect_one();
+    bool ok = n_tiles == 0 || mbar_wait(bar_q, 0, abort_flag);
+    // the low words of the descriptors: a stage or a step of the inner dimension is an addition to them
+    const uint32_t q_lo = desc_lo(base, 1), k_lo = desc_lo(base + S::RING, 1), v_lo = desc_lo(base + S::RING, KV_HALF >> 4);
+    uint32_t k_stage = 0, k_phase = 0, v_stage = 1, v_phase = 0;  // two walks over the ring, that of the keys two tiles ahead
+    auto step = [](uint32_t& stage, uint32_t& phase) {
+      stage += 2;
+      if (stage >= S::STAGES) { stage -= S::STAGES; phase ^= 1; }
+    };
+    auto qk = [&](int x, int b) {
+      const uint32_t ql = q_lo + x * (S::Q_TILE >> 4), kl = k_lo + k_stage * (S::STAGE >> 4), d = tmem + KT * (2 * x + b);
+      if (leader) {
 #pragma unroll
-        for (uint32_t k = 0; k < DP / 16; ++k) {
-          const uint32_t to = (k >> 2) * (HALF >> 4) + 2 * (k & 3);
-          umma_bf16(tmem + x * SCORE_COLS, qd + to, kd + to, IDESC_QK, k != 0);
-        }
-        umma_commit(bar_s + 8 * x);
-      };
-      if (ok) {
-        tc_fence_after();
-        if (n0 > 0) qk(0, 0);
-        if (n1 > 0) qk(1, 0);
-        umma_commit(bar_empty);
-        step();
+        for (uint32_t k = 0; k < DP / 16; ++k)
+          umma_bf16(d, desc_of(ql + (k >> 2) * (Q_HALF >> 4) + 2 * (k & 3)), desc_of(kl + (k >> 2) * (KV_HALF >> 4) + 2 * (k & 3)), IDESC_QK, k != 0);
+        umma_commit(bar_s + 16 * x + 8 * b);
       }
-      for (int t = 0; ok && t < n_tiles; ++t) {
-        const uint32_t vst = stage;
-        ok = mbar_wait(bar_full + 8 * vst, phase, abort_flag);
-        if (!ok) break;
-        step();
-        bool next = false;
-        for (int x = 0; x < 2; ++x) {
-          const int nx = x ? n1 : n0;
-          if (t >= nx) continue;
-          ok = mbar_wait(bar_p + 8 * x, t & 1, abort_flag);
-          if (!ok) break;
-          tc_fence_after();
-          const uint64_t vd = desc_cols(base + S::RING + vst * S::TILE);
+    };
+    auto pv = [&](int x, int b, uint32_t accumulate, bool last) {
+      const uint32_t vl = v_lo + v_stage * (S::STAGE >> 4), pa = tmem + KT * (2 * x + b), d = tmem_o + x * DP;
+      if (leader) {
 #pragma unroll
-          for (uint32_t k = 0; k < PT / 16; ++k)
-            umma_bf16_ts(tmem_o + x * DP, tmem + x * SCORE_COLS + WEIGHT_AT + 8 * k, vd + (uint64_t)(2048 >> 4) * k, IDESC_PV<DP>, (t | k) != 0);
-          if (x == (t < n1 ? 1 : 0)) umma_commit(bar_empty + 8 * vst);  // the last product that reads these values
-          if (t + 1 < nx) {
-            if (!next) {
-              ok = mbar_wait(bar_full + 8 * stage, phase, abort_flag);
-              if (!ok) break;
-              tc_fence_after();
-              next = true;
-            }
-            qk(x, stage);
-          } else {
-            umma_commit(bar_o + 8 * x);
-          }
-        }
-        if (ok && next) {
-          umma_commit(bar_empty + 8 * stage);
-          step();
-        }
+        for (uint32_t k = 0; k < KT / 16; ++k) umma_bf16_ts(d, pa + 8 * k, desc_of(vl + (2048 >> 4) * k), IDESC_PV<DP>, k != 0 ? 1u : accumulate);
+        umma_commit(bar_o + 16 * x + 8 * b);
+        if (last) umma_commit(bar_empty + 8 * v_stage);  // the last product that reads these values
+      }
+    };
+    for (int t = 0; ok && t < min(2, n_tiles); ++t) {
+      ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * k_stage, k_phase, abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+      if (t < n0) qk(0, t);
+      if (t < n1) qk(1, t);
+      if (leader) umma_commit(bar_empty + 8 * k_stage);
+      step(k_stage, k_phase);
+    }
+    for (int t = 0; ok && t < n_tiles; ++t) {
+      const int b = t & 1;
+      const uint32_t turn = (t >> 1) & 1;
+      ok = mbar_wait(bar_full + 8 * v_stage, v_phase, abort_flag);
+      if (t + 2 < n_tiles) ok = ok && mbar_wait(bar_full + 8 * k_stage, k_phase, abort_flag);
+      if (t < n0) {
+        ok = ok && mbar_wait(bar_p + 8 * b, turn, abort_flag);
+        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        tc_fence_after();
+        pv(0, b, t != 0, t >= n1);
+        if (t + 2 < n0) qk(0, b);
+      }
+      if (t < n1) {
+        ok = ok && mbar_wait(bar_p + 16 + 8 * b, turn, abort_flag);
+        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        tc_fence_after();
+        pv(1, b, t != 0, true);
+        if (t + 2 < n1) qk(1, b);
+      }
+      step(v_stage, v_phase);
+      if (t + 2 < n_tiles) {
+        if (leader) umma_commit(bar_empty + 8 * k_stage);
+        step(k_stage, k_phase);
       }
     }
     __syncwarp();
@@ -331,33 +350,32 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     const bool valid = tok < n_rows;
     const int nx = x ? n1 : n0;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t t_s = tmem + x * SCORE_COLS + lanes, t_o = tmem_o + x * DP + lanes;
+    const uint32_t t_o = tmem_o + x * DP + lanes;
     const float c = a.scale * 1.4426950408889634f;
     const long long p0 = p_first + x * tokens, p = p0 + tok;     // position of the row tile's first token, of this row
     float m = -INFINITY, l = 0.f;
     bool ok = true;
     for (int t = 0; t < nx; ++t) {
-      ok = mbar_wait(bar_s + 8 * x, t & 1, abort_flag);
+      ok = mbar_wait(bar_s + 16 * x + 8 * (t & 1), (t >> 1) & 1, abort_flag);
       if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
       tc_fence_after();
-      // Registers hold 96 of the 128 scores of a row at most: the lower half is read for the maximum, then the upper half,
-      // whose weights come first while the lower half is read again.
-      float lo_s[2][32], hi_s[2][32];
-      tmem_load32(t_s, lo_s[0]);
-      tmem_load32(t_s + 32, lo_s[1]);
-      const long long key0 = (long long)tile_at(t) * PT;
-      const uint32_t missing = holes[t & 7];
-      const bool whole = missing == 0 && key0 + PT - 1 <= p0 && key0 + PT <= held &&
-                         (a.window == 0 || key0 > p0 + n_rows - 1 - a.window || key0 + PT <= a.sinks);
-      uint32_t seen[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
+      const uint32_t t_s = tmem + KT * (2 * x + (t & 1)) + lanes;
+      float s[KT];
+      tmem_load32(t_s, s);
+      tmem_load32(t_s + 32, s + 32);
+      const long long key0 = (long long)tile_at(t) * KT;
+      const uint32_t missing = holes[t % HOLES];
+      const bool whole = missing == 0 && key0 + KT - 1 <= p0 && key0 + KT <= held &&
+                         (a.window == 0 || key0 > p0 + n_rows - 1 - a.window || key0 + KT <= a.sinks);
+      uint32_t seen[2] = {0xffffffffu, 0xffffffffu};
       if (!whole) {
         // bit i of seen[w]: this row sees token key0 + 32 w + i
-        const int hi = (int)max(-1ll, min(min(p, held - 1) - key0, (long long)PT));                 // columns up to hi
-        const int lo = a.window ? (int)max(0ll, min(p - a.window + 1 - key0, (long long)PT)) : 0;   // from lo on
-        const int sk = (int)max(0ll, min((long long)a.sinks - key0, (long long)PT));                // or below sk
-        const int copy_log = min(a.page_log, 7);
+        const int hi = (int)max(-1ll, min(min(p, held - 1) - key0, (long long)KT));                 // columns up to hi
+        const int lo = a.window ? (int)max(0ll, min(p - a.window + 1 - key0, (long long)KT)) : 0;   // from lo on
+        const int sk = (int)max(0ll, min((long long)a.sinks - key0, (long long)KT));                // or below sk
+        const int copy_log = min(a.page_log, 6);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < 2; ++w) {
           seen[w] = bits_below(hi + 1 - 32 * w) & (~bits_below(lo - 32 * w) | bits_below(sk - 32 * w));
           if (missing) {
             uint32_t there = 0;
@@ -367,20 +385,22 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
             seen[w] &= there;
           }
         }
-        // the values of this tile (thread r: token r): cleared where no row of the CTA sees them, else looked at
+        // the values of this tile (two threads per token): cleared where no row of the CTA sees them, else looked at
         const uint32_t vi = 2 * t + 1;
         ok = mbar_wait(bar_full + 8 * (vi % S::STAGES), (vi / S::STAGES) & 1, abort_flag);
         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-        const long long tokn = key0 + row;
-        const bool any = tokn < end && (tokn >= low || tokn < a.sinks) && !((missing >> (row >> copy_log)) & 1u);
-        uint8_t* const v = sm + S::RING + (vi % S::STAGES) * S::TILE + row * 128;
-        __nv_bfloat162 test = __float2bfloat162_rn(0.f);
+        const int vrow = row & (KT - 1);
+        const long long tokn = key0 + vrow;
+        const bool any = tokn < end && (tokn >= low || tokn < a.sinks) && !((missing >> (vrow >> copy_log)) & 1u);
+        uint8_t* const v = sm + S::RING + (vi % S::STAGES) * S::STAGE + vrow * 128;
+        const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
+        __nv_bfloat162 test = zero;
 #pragma unroll
-        for (uint32_t q = 0; q < 8 * S::HALVES; ++q) {
-          uint4* const at = (uint4*)(v + (q >> 3) * HALF + (((q & 7) ^ (row & 7)) << 4));
+        for (uint32_t k = 0; k < 4 * S::HALVES; ++k) {
+          const uint32_t q = k + (row >> 6) * 4 * S::HALVES;
+          uint4* const at = (uint4*)(v + (q >> 3) * KV_HALF + (((q & 7) ^ (row & 7)) << 4));
           if (any) {
             const uint4 w = *at;
-            const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
             test = __hfma2(*(const __nv_bfloat162*)&w.x, zero, test);
             test = __hfma2(*(const __nv_bfloat162*)&w.y, zero, test);
             test = __hfma2(*(const __nv_bfloat162*)&w.z, zero, test);
@@ -403,22 +423,19 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         for (int i = 3; i < 31; i += 4) { t0 = fmaxf(t0, s[i]); t1 = fmaxf(t1, s[i + 1]); t2 = fmaxf(t2, s[i + 2]); t3 = fmaxf(t3, s[i + 3]); }
         return fmaxf(fmaxf(fmaxf(t0, s[31]), t1), fmaxf(t2, t3));
       };
-      tmem_landed(lo_s[0]);
-      tmem_landed(lo_s[1]);
-      tmem_load32(t_s + 64, hi_s[0]);
-      tmem_load32(t_s + 96, hi_s[1]);
-      if (!whole) { hide(lo_s[0], seen[0]); hide(lo_s[1], seen[1]); }
-      float top = highest(lo_s[1], highest(lo_s[0], -INFINITY));
-      tmem_landed(hi_s[0]);
-      tmem_landed(hi_s[1]);
-      if (!whole) { hide(hi_s[0], seen[2]); hide(hi_s[1], seen[3]); }
-      top = highest(hi_s[1], highest(hi_s[0], top));
+      tmem_landed(s);
+      tmem_landed(s + 32);
+      if (!whole) { hide(s, seen[0]); hide(s + 32, seen[1]); }
+      const float top = highest(s + 32, highest(s, -INFINITY));
       const float m_new = fmaxf(m, top);
       if (__any_sync(0xffffffffu, (m_new - m) * c > GROWTH)) {  // (from -inf: yes, unless it stays there)
         const float keep = m_new == m ? 1.f : ex2((m - m_new) * c);
         l *= keep;
         m = m_new;
         if (t > 0) {
+          ok = mbar_wait(bar_o + 16 * x + 8 * ((t - 1) & 1), ((t - 1) >> 1) & 1, abort_flag);  // PV(t - 1); PV(t) waits for this tile's weights
+          if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+          tc_fence_after();
 #pragma unroll
           for (int q = 0; q < DP / 32; ++q) {
             float o[32];
@@ -444,27 +461,19 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
           pk[i] = pack_bf16(w0.x, w0.y);
           pk[i + 1] = pack_bf16(w1.x, w1.y);
         }
-        tmem_store16(t_s + WEIGHT_AT + 16 * q, pk);  // (over scores that have been read)
+        tmem_store16(t_s + 16 * q, pk);  // (over scores that have been read)
       };
-      tmem_load32(t_s, lo_s[0]);
-      weigh(hi_s[0], 2);
-      tmem_landed(lo_s[0]);
-      tmem_load32(t_s + 32, lo_s[1]);
-      weigh(hi_s[1], 3);
-      if (!whole) hide(lo_s[0], seen[0]);
-      weigh(lo_s[0], 0);
-      tmem_landed(lo_s[1]);
-      if (!whole) hide(lo_s[1], seen[1]);
-      weigh(lo_s[1], 1);
+      weigh(s, 0);
+      weigh(s + 32, 1);
       l += (l01.x + l01.y) + (l23.x + l23.y);
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar_p + 8 * x);
+      if (lane == 0) mbar_arrive(bar_p + 16 * x + 8 * (t & 1));
     }
     // ---- the row's quotient ----
     if (n_rows > 0) {
-      if (ok && nx > 0) ok = mbar_wait(bar_o + 8 * x, 0, abort_flag);
+      if (ok && nx > 0) ok = mbar_wait(bar_o + 16 * x + 8 * ((nx - 1) & 1), ((nx - 1) >> 1) & 1, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
       if (ok) {
@@ -514,7 +523,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       }
       if (n_tiles > 0 && !mbar_try(bar_q, 0)) mbar_wait_slow(bar_q, 0, abort_flag, DRAIN_NS, false);
     }
-    if (warp == 8 && lane == 0) {
+    if (warp == 8 && elect_one()) {  // (the lane that issued)
       umma_commit(bar_drain);
       if (!mbar_try(bar_drain, 0)) mbar_wait_slow(bar_drain, 0, abort_flag, DRAIN_NS, false);
     }
@@ -544,8 +553,8 @@ int dvm_launch_attention_prompt(const dvm_attention_desc& d, const dvm::att::Arg
   const int tokens = PT / a.group;
   CUtensorMap q, k, v;
   int st = dvm_query_map(d, a.q, tokens, &q);
-  if (st == DVM_OK) st = dvm_cache_map(d, d.k_stride, a.k, PT, &k);
-  if (st == DVM_OK) st = dvm_cache_map(d, d.v_stride, a.v, PT, &v);
+  if (st == DVM_OK) st = dvm_cache_map(d, d.k_stride, a.k, KT, &k);
+  if (st == DVM_OK) st = dvm_cache_map(d, d.v_stride, a.v, KT, &v);
   if (st != DVM_OK) return st;
   // the most blocks of 2 x tokens query tokens that the requests can have
   const int64_t per = 2 * tokens, by_rows = (d.rows + d.requests * (per - 1)) / per, by_max = d.requests * ((d.max_q + per - 1) / per);
