@@ -10,13 +10,14 @@
 // S_x has two places, t and t + 1 in turn: S_x(t + 1) is there before P_x(t) is done, so neither the tensor cores nor the
 // threads wait for the other's whole latency.  (Tiles of 128 tokens leave room for one place only -- tensor memory is
 // S_0, S_1, O_0, O_1 and full -- and then the threads waited 1850 of 4300 cycles per 128 tokens.)  One thread issues
-// all products, PV_x(t) then QK_x(t + 2), and they complete in that order: QK_x(t + 2) overwrites P_x(t) after its use.
+// a row tile's products, PV_x(t) then QK_x(t + 2), and they complete in that order: QK_x(t + 2) overwrites P_x(t) after its
+// use.  (One thread for both row tiles spent 830 of 2030 cycles per 64 tokens in waits that were over when they began.)
 // O_x is rescaled by a new maximum only when that has grown by more than 2^8 (weights stay below 2^8, far from any bound
 // of bf16 or fp32; the quotient at the end does not depend on the maximum that was used); then the row's thread waits for
 // PV_x(t - 1).  Weights are rounded to bf16 for the second product, their sum is not.
 //
-// Roles: warps 0-3 and 4-7 the rows of the two tiles, warp 8 issues the products, warp 9 fetches (queries once, then
-// keys and values in turn through a ring, page by page).
+// Roles: warps 0-3 and 4-7 the rows of the two tiles, warps 8 and 9 issue their products, warp 10 fetches (queries once,
+// then keys and values in turn through a ring, page by page).
 //
 // Tokens a row does not see get a score of -inf.  That is not enough for the second product, where 0 x NaN is NaN: in
 // tiles with a mask the values that no row of the CTA sees are cleared in shared memory (they may be anything: the end of
@@ -39,10 +40,11 @@ using namespace sm100;
 
 constexpr int PT = 128;                  // rows of a row tile
 constexpr int KT = 64;                   // tokens of a cache tile
-constexpr int PROMPT_THREADS = 320;
+constexpr int PROMPT_THREADS = 352;
 constexpr uint32_t Q_HALF = PT * 128;    // 64 elements of the rows: 16 KB
 constexpr uint32_t KV_HALF = KT * 128;   // 64 elements of the tokens: 8 KB
 constexpr int HOLES = 16;                // tiles whose missing pages are remembered: more than the ring is deep
+constexpr int POLYNOMIAL_EVERY = 4;      // one pair of weights in so many is formed by ex2_by_polynomial
 constexpr float GROWTH = 8.f;            // log2 of how far weights may grow before the sums are rescaled
 
 template <int DP>  // head_dim rounded up to 64 or 128
@@ -52,8 +54,8 @@ struct PromptSmem {
   static constexpr uint32_t STAGE = HALVES * KV_HALF;            // keys or values of a tile
   static constexpr uint32_t STAGES = DP == 128 ? 10 : 16;
   static constexpr uint32_t RING = 2 * Q_TILE;                   // behind the queries of both row tiles
-  static constexpr uint32_t BARS = RING + STAGES * STAGE;        // full[], empty[], q, s[2][2], p[2][2], o[2][2], drain
-  static constexpr uint32_t WORDS = BARS + 16 * STAGES + 112;     // tensor memory address, abort, dirty[2], holes[]
+  static constexpr uint32_t BARS = RING + STAGES * STAGE;        // full[], empty[], q, s[2][2], p[2][2], o[2][2], drain[2]
+  static constexpr uint32_t WORDS = BARS + 16 * STAGES + 120;     // tensor memory address, abort, dirty[2], holes[]
   static constexpr uint32_t SCAN = WORDS + 16 + 4 * HOLES;       // 12 sums, found request and block
   static constexpr uint32_t BYTES = SCAN + 64 + 1024;
   static_assert(STAGES / 2 + 3 <= HOLES, "a tile's holes are kept until its weights are done");
@@ -126,6 +128,29 @@ __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either is
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+// 2^x without the special function unit, for part of the weights: the unit's 16 results a cycle are what the weights take
+// longest for, while multiply-adds are to spare.  x = f + r with f the nearest integer (1.5 2^23 added and taken away) and
+// |r| <= 1/2; 2^r by a polynomial of degree 5 fitted for least relative error (1.7e-7 in fp32) with constant term 1, so
+// that x <= -127 gives exactly 0; f is added to the exponent field.  For x below 128; not for NaN (see `top` below).
+__device__ __forceinline__ float2 ex2_by_polynomial(float2 x) {
+  const float2 big = make_float2(12582912.f, 12582912.f);
+  x.x = fmaxf(x.x, -127.f);
+  x.y = fmaxf(x.y, -127.f);
+  const float2 t = add2(x, big);
+  const float2 r = fma2(add2(t, make_float2(-12582912.f, -12582912.f)), make_float2(-1.f, -1.f), x);
+  float2 p = make_float2(0.001326472731307149f, 0.001326472731307149f);
+  p = fma2(p, r, make_float2(0.009671512991189957f, 0.009671512991189957f));
+  p = fma2(p, r, make_float2(0.05550733581185341f, 0.05550733581185341f));
+  p = fma2(p, r, make_float2(0.24022242426872253f, 0.24022242426872253f));
+  p = fma2(p, r, make_float2(0.6931470036506653f, 0.6931470036506653f));
+  p = fma2(p, r, make_float2(1.f, 1.f));
+  return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
@@ -206,7 +231,10 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
   const int n0 = tiles_of(0), n1 = tiles_of(1), n_tiles = max(n0, n1);
 
   if (threadIdx.x == 0) {
-    for (uint32_t s = 0; s < 2 * S::STAGES; ++s) mbar_init(bar_full + 8 * s, 1);
+    for (uint32_t s = 0; s < S::STAGES; ++s) {
+      mbar_init(bar_full + 8 * s, 1);
+      mbar_init(bar_empty + 8 * s, 2);  // (both row tiles are done with it)
+    }
     mbar_init(bar_q, 1);
     for (uint32_t x = 0; x < 2; ++x) {
       for (uint32_t b = 0; b < 2; ++b) {
@@ -217,6 +245,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       dirty[x] = 0;
     }
     mbar_init(bar_drain, 1);
+    mbar_init(bar_drain + 8, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -231,7 +260,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
   auto tile_at = [&](int j) -> int { return j < ns ? j : first + (j - ns); };
 
   uint32_t issued = 0, f_stage = 0, f_phase = 0;  // the fetching warp's ring, kept for the abort path
-  if (warp == 9) {
+  if (warp == 10) {
     // ---------------- fetch ----------------
     const int copy_log = min(a.page_log, 6), copies = KT >> copy_log;
     const int* table = a.table + (long long)request * a.max_blocks;
@@ -275,69 +304,65 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       page = next;
     }
     __syncwarp();
-  } else if (warp == 8) {
-    // ---------------- products ----------------
+  } else if (warp >= 8) {
+    // ---------------- products of one row tile ----------------
     // The whole warp walks, so that descriptors and barriers stay in uniform registers; one elected lane issues.  (Issued
     // from a branch of lane 0 alone, with the descriptors formed anew, a product took 70 to 100 cycles to issue, more than
     // it takes to run.)
+    const int x = warp - 8, nx = x ? n1 : n0;
     const bool leader = elect_one();
     bool ok = n_tiles == 0 || mbar_wait(bar_q, 0, abort_flag);
     // the low words of the descriptors: a stage or a step of the inner dimension is an addition to them
-    const uint32_t q_lo = desc_lo(base, 1), k_lo = desc_lo(base + S::RING, 1), v_lo = desc_lo(base + S::RING, KV_HALF >> 4);
+    const uint32_t q_lo = desc_lo(base + x * S::Q_TILE, 1), k_lo = desc_lo(base + S::RING, 1), v_lo = desc_lo(base + S::RING, KV_HALF >> 4);
+    const uint32_t d_s = tmem + 2 * KT * x, d_o = tmem_o + x * DP;
     uint32_t k_stage = 0, k_phase = 0, v_stage = 1, v_phase = 0;  // two walks over the ring, that of the keys two tiles ahead
     auto step = [](uint32_t& stage, uint32_t& phase) {
       stage += 2;
       if (stage >= S::STAGES) { stage -= S::STAGES; phase ^= 1; }
     };
-    auto qk = [&](int x, int b) {
-      const uint32_t ql = q_lo + x * (S::Q_TILE >> 4), kl = k_lo + k_stage * (S::STAGE >> 4), d = tmem + KT * (2 * x + b);
+    auto qk = [&](int b) {
+      const uint32_t kl = k_lo + k_stage * (S::STAGE >> 4);
       if (leader) {
 #pragma unroll
         for (uint32_t k = 0; k < DP / 16; ++k)
-          umma_bf16(d, desc_of(ql + (k >> 2) * (Q_HALF >> 4) + 2 * (k & 3)), desc_of(kl + (k >> 2) * (KV_HALF >> 4) + 2 * (k & 3)), IDESC_QK, k != 0);
+          umma_bf16(d_s + KT * b, desc_of(q_lo + (k >> 2) * (Q_HALF >> 4) + 2 * (k & 3)), desc_of(kl + (k >> 2) * (KV_HALF >> 4) + 2 * (k & 3)), IDESC_QK, k != 0);
         umma_commit(bar_s + 16 * x + 8 * b);
+        umma_commit(bar_empty + 8 * k_stage);
       }
     };
-    auto pv = [&](int x, int b, uint32_t accumulate, bool last) {
-      const uint32_t vl = v_lo + v_stage * (S::STAGE >> 4), pa = tmem + KT * (2 * x + b), d = tmem_o + x * DP;
+    auto pv = [&](int b, uint32_t accumulate) {
+      const uint32_t vl = v_lo + v_stage * (S::STAGE >> 4);
       if (leader) {
 #pragma unroll
-        for (uint32_t k = 0; k < KT / 16; ++k) umma_bf16_ts(d, pa + 8 * k, desc_of(vl + (2048 >> 4) * k), IDESC_PV<DP>, k != 0 ? 1u : accumulate);
+        for (uint32_t k = 0; k < KT / 16; ++k) umma_bf16_ts(d_o, d_s + KT * b + 8 * k, desc_of(vl + (2048 >> 4) * k), IDESC_PV<DP>, k != 0 ? 1u : accumulate);
         umma_commit(bar_o + 16 * x + 8 * b);
-        if (last) umma_commit(bar_empty + 8 * v_stage);  // the last product that reads these values
+        umma_commit(bar_empty + 8 * v_stage);
       }
     };
     for (int t = 0; ok && t < min(2, n_tiles); ++t) {
       ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * k_stage, k_phase, abort_flag));
       if (!ok) break;
       tc_fence_after();
-      if (t < n0) qk(0, t);
-      if (t < n1) qk(1, t);
-      if (leader) umma_commit(bar_empty + 8 * k_stage);
+      if (t < nx) qk(t);
+      else if (leader) mbar_arrive(bar_empty + 8 * k_stage);
       step(k_stage, k_phase);
     }
     for (int t = 0; ok && t < n_tiles; ++t) {
       const int b = t & 1;
-      const uint32_t turn = (t >> 1) & 1;
       ok = mbar_wait(bar_full + 8 * v_stage, v_phase, abort_flag);
-      if (t + 2 < n_tiles) ok = ok && mbar_wait(bar_full + 8 * k_stage, k_phase, abort_flag);
-      if (t < n0) {
-        ok = ok && mbar_wait(bar_p + 8 * b, turn, abort_flag);
-        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-        tc_fence_after();
-        pv(0, b, t != 0, t >= n1);
-        if (t + 2 < n0) qk(0, b);
-      }
-      if (t < n1) {
-        ok = ok && mbar_wait(bar_p + 16 + 8 * b, turn, abort_flag);
-        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-        tc_fence_after();
-        pv(1, b, t != 0, true);
-        if (t + 2 < n1) qk(1, b);
-      }
+      if (t < nx) ok = ok && mbar_wait(bar_p + 16 * x + 8 * b, (t >> 1) & 1, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      if (t < nx) pv(b, t != 0);
+      else if (leader) mbar_arrive(bar_empty + 8 * v_stage);
       step(v_stage, v_phase);
       if (t + 2 < n_tiles) {
-        if (leader) umma_commit(bar_empty + 8 * k_stage);
+        ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * k_stage, k_phase, abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        if (t + 2 < nx) qk(b);
+        else if (leader) mbar_arrive(bar_empty + 8 * k_stage);
         step(k_stage, k_phase);
       }
     }
@@ -352,27 +377,31 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_o = tmem_o + x * DP + lanes;
     const float c = a.scale * 1.4426950408889634f;
-    const long long p0 = p_first + x * tokens, p = p0 + tok;     // position of the row tile's first token, of this row
+    const long long p0 = p_first + x * tokens;                  // position of the row tile's first token
+    // this row sees the tokens up to hi_at that are from lo_at on or below the sinks; every row of the tile sees those up
+    // to all_hi that are from all_lo on
+    auto cut = [](long long v) -> int { return (int)max(-1ll, min(v, 0x7fffffffll)); };
+    const int hi_at = cut(min(p0 + tok, held - 1)), lo_at = a.window ? max(0, cut(p0 + tok - a.window + 1)) : 0;
+    const int all_hi = cut(min(p0, held - 1)), all_lo = a.window ? max(0, cut(p0 + n_rows - a.window)) : 0;
     float m = -INFINITY, l = 0.f;
     bool ok = true;
-    for (int t = 0; t < nx; ++t) {
-      ok = mbar_wait(bar_s + 16 * x + 8 * (t & 1), (t >> 1) & 1, abort_flag);
-      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+    // The scores of tile t + 1 are on their way while the second half of tile t's weights is formed: the lower half goes to
+    // the registers that tile t's lower half has left, the upper half to those of the tile before.
+    float s_lo[32], s_hi[2][32];
+    auto scores = [&](int t) -> bool {  // tile t's scores are in tensor memory
+      const bool got = mbar_wait(bar_s + 16 * x + 8 * (t & 1), (t >> 1) & 1, abort_flag);
       tc_fence_after();
-      const uint32_t t_s = tmem + KT * (2 * x + (t & 1)) + lanes;
-      float s[KT];
-      tmem_load32(t_s, s);
-      tmem_load32(t_s + 32, s + 32);
-      const long long key0 = (long long)tile_at(t) * KT;
+      return __all_sync(0xffffffffu, got);
+    };
+    auto tile = [&](int t, float* hi_now, float* hi_next) -> bool {
+      const uint32_t t_s = tmem + KT * (2 * x + (t & 1)) + lanes, t_next = tmem + KT * (2 * x + ((t + 1) & 1)) + lanes;
+      const int key0 = tile_at(t) * KT;
       const uint32_t missing = holes[t % HOLES];
-      const bool whole = missing == 0 && key0 + KT - 1 <= p0 && key0 + KT <= held &&
-                         (a.window == 0 || key0 > p0 + n_rows - 1 - a.window || key0 + KT <= a.sinks);
+      const bool whole = missing == 0 && key0 + KT - 1 <= all_hi && (key0 >= all_lo || key0 <= a.sinks - KT);
       uint32_t seen[2] = {0xffffffffu, 0xffffffffu};
       if (!whole) {
         // bit i of seen[w]: this row sees token key0 + 32 w + i
-        const int hi = (int)max(-1ll, min(min(p, held - 1) - key0, (long long)KT));                 // columns up to hi
-        const int lo = a.window ? (int)max(0ll, min(p - a.window + 1 - key0, (long long)KT)) : 0;   // from lo on
-        const int sk = (int)max(0ll, min((long long)a.sinks - key0, (long long)KT));                // or below sk
+        const int hi = hi_at - key0, lo = lo_at - key0, sk = a.sinks - key0;
         const int copy_log = min(a.page_log, 6);
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
@@ -387,11 +416,9 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         }
         // the values of this tile (two threads per token): cleared where no row of the CTA sees them, else looked at
         const uint32_t vi = 2 * t + 1;
-        ok = mbar_wait(bar_full + 8 * (vi % S::STAGES), (vi / S::STAGES) & 1, abort_flag);
-        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+        if (!__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * (vi % S::STAGES), (vi / S::STAGES) & 1, abort_flag))) return false;
         const int vrow = row & (KT - 1);
-        const long long tokn = key0 + vrow;
-        const bool any = tokn < end && (tokn >= low || tokn < a.sinks) && !((missing >> (vrow >> copy_log)) & 1u);
+        const bool any = key0 + vrow < end && (key0 + vrow >= low || key0 + vrow < a.sinks) && !((missing >> (vrow >> copy_log)) & 1u);
         uint8_t* const v = sm + S::RING + (vi % S::STAGES) * S::STAGE + vrow * 128;
         const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
         __nv_bfloat162 test = zero;
@@ -420,21 +447,22 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       auto highest = [](const float* s, float top) -> float {
         float t0 = top, t1 = s[0], t2 = s[1], t3 = s[2];
 #pragma unroll
-        for (int i = 3; i < 31; i += 4) { t0 = fmaxf(t0, s[i]); t1 = fmaxf(t1, s[i + 1]); t2 = fmaxf(t2, s[i + 2]); t3 = fmaxf(t3, s[i + 3]); }
-        return fmaxf(fmaxf(fmaxf(t0, s[31]), t1), fmaxf(t2, t3));
+        for (int i = 3; i < 31; i += 4) { t0 = max_nan(t0, s[i]); t1 = max_nan(t1, s[i + 1]); t2 = max_nan(t2, s[i + 2]); t3 = max_nan(t3, s[i + 3]); }
+        return max_nan(max_nan(max_nan(t0, s[31]), t1), max_nan(t2, t3));
       };
-      tmem_landed(s);
-      tmem_landed(s + 32);
-      if (!whole) { hide(s, seen[0]); hide(s + 32, seen[1]); }
-      const float top = highest(s + 32, highest(s, -INFINITY));
-      const float m_new = fmaxf(m, top);
-      if (__any_sync(0xffffffffu, (m_new - m) * c > GROWTH)) {  // (from -inf: yes, unless it stays there)
+      tmem_landed(s_lo);
+      tmem_landed(hi_now);
+      if (!whole) { hide(s_lo, seen[0]); hide(hi_now, seen[1]); }
+      // a NaN score makes the maximum NaN and with it every weight of the row, as the quotient has it
+      const float top = highest(hi_now, highest(s_lo, -INFINITY));
+      const float m_new = max_nan(m, top);
+      if (__any_sync(0xffffffffu, (m_new - m) * c > GROWTH || m_new != m_new)) {  // (from -inf: yes, unless it stays there)
         const float keep = m_new == m ? 1.f : ex2((m - m_new) * c);
         l *= keep;
         m = m_new;
         if (t > 0) {
-          ok = mbar_wait(bar_o + 16 * x + 8 * ((t - 1) & 1), ((t - 1) >> 1) & 1, abort_flag);  // PV(t - 1); PV(t) waits for this tile's weights
-          if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+          // PV(t - 1) is done; PV(t) waits for this tile's weights
+          if (!__all_sync(0xffffffffu, mbar_wait(bar_o + 16 * x + 8 * ((t - 1) & 1), ((t - 1) >> 1) & 1, abort_flag))) return false;
           tc_fence_after();
 #pragma unroll
           for (int q = 0; q < DP / 32; ++q) {
@@ -455,7 +483,8 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
           const float2 x0 = fma2(make_float2(s[2 * i], s[2 * i + 1]), cc, oo), x1 = fma2(make_float2(s[2 * i + 2], s[2 * i + 3]), cc, oo);
-          const float2 w0 = make_float2(ex2(x0.x), ex2(x0.y)), w1 = make_float2(ex2(x1.x), ex2(x1.y));
+          const float2 w0 = make_float2(ex2(x0.x), ex2(x0.y));
+          const float2 w1 = i % POLYNOMIAL_EVERY == 0 ? ex2_by_polynomial(x1) : make_float2(ex2(x1.x), ex2(x1.y));
           l01 = add2(l01, w0);
           l23 = add2(l23, w1);
           pk[i] = pack_bf16(w0.x, w0.y);
@@ -463,14 +492,40 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         }
         tmem_store16(t_s + 16 * q, pk);  // (over scores that have been read)
       };
-      weigh(s, 0);
-      weigh(s + 32, 1);
+      weigh(s_lo, 0);
+      // the next scores, if they are there already; nothing waits for them before this tile's weights are handed over
+      const bool more = t + 1 < nx;
+      const bool early = more && __all_sync(0xffffffffu, mbar_test(bar_s + 16 * x + 8 * ((t + 1) & 1), ((t + 1) >> 1) & 1));
+      if (early) {
+        tc_fence_after();
+        tmem_load32(t_next, s_lo);
+        tmem_load32(t_next + 32, hi_next);
+      }
+      weigh(hi_now, 1);
       l += (l01.x + l01.y) + (l23.x + l23.y);
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_p + 16 * x + 8 * (t & 1));
+      if (more && !early) {
+        if (!scores(t + 1)) return false;
+        tmem_load32(t_next, s_lo);
+        tmem_load32(t_next + 32, hi_next);
+      }
+      return true;
+    };
+    if (nx > 0) {
+      ok = scores(0);
+      if (ok) {
+        tmem_load32(tmem + 2 * KT * x + lanes, s_lo);
+        tmem_load32(tmem + 2 * KT * x + lanes + 32, s_hi[0]);
+      }
+      for (int t = 0; ok && t < nx; t += 2) {
+        ok = tile(t, s_hi[0], s_hi[1]);
+        if (ok && t + 1 < nx) ok = tile(t + 1, s_hi[1], s_hi[0]);
+      }
     }
+    tmem_load_wait();  // (a walk that gave up may have loads on their way)
     // ---- the row's quotient ----
     if (n_rows > 0) {
       if (ok && nx > 0) ok = mbar_wait(bar_o + 16 * x + 8 * ((nx - 1) & 1), ((nx - 1) >> 1) & 1, abort_flag);
@@ -516,16 +571,16 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
   tc_fence_before();
   __syncthreads();
   if (*abort_flag) {
-    if (warp == 9 && lane == 0) {  // the latest fill of every stage, and the queries
+    if (warp == 10 && lane == 0) {  // the latest fill of every stage, and the queries
       for (uint32_t k = min(issued, S::STAGES); k > 0; --k) {
         if (f_stage == 0) { f_stage = S::STAGES - 1; f_phase ^= 1; } else --f_stage;
         if (!mbar_try(bar_full + 8 * f_stage, f_phase)) mbar_wait_slow(bar_full + 8 * f_stage, f_phase, abort_flag, DRAIN_NS, false);
       }
       if (n_tiles > 0 && !mbar_try(bar_q, 0)) mbar_wait_slow(bar_q, 0, abort_flag, DRAIN_NS, false);
     }
-    if (warp == 8 && elect_one()) {  // (the lane that issued)
-      umma_commit(bar_drain);
-      if (!mbar_try(bar_drain, 0)) mbar_wait_slow(bar_drain, 0, abort_flag, DRAIN_NS, false);
+    if ((warp == 8 || warp == 9) && elect_one()) {  // (the lanes that issued)
+      umma_commit(bar_drain + 8 * (warp - 8));
+      if (!mbar_try(bar_drain + 8 * (warp - 8), 0)) mbar_wait_slow(bar_drain + 8 * (warp - 8), 0, abort_flag, DRAIN_NS, false);
     }
     if (threadIdx.x == 0) atomicMax(a.status, (unsigned int)ST_TIMEOUT);
     __syncthreads();
