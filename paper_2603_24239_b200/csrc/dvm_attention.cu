@@ -106,10 +106,11 @@ int dvm_launch_attention(const dvm_attention_desc& d, void* const* t, cudaStream
   while ((1ll << a.page_log) < d.page_size) ++a.page_log;
   a.window = (int)d.window; a.sinks = (int)d.sinks; a.max_q = (int)d.max_q; a.out_bf16 = d.out_dtype == DVM_BF16; a.scale = d.scale;
   const bool aligned = (((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v) & 15) == 0;
-  a.out_vec = a.out_bf16 && ((uintptr_t)a.out & 15) == 0 && d.out_stride[0] % 8 == 0 && d.out_stride[1] % 8 == 0;
+  auto stores = [&](int n) { return a.out_bf16 && (uintptr_t)a.out % (2 * n) == 0 && d.out_stride[0] % n == 0 && d.out_stride[1] % n == 0; };
+  a.out_vec = stores(16) && a.D % 16 == 0 ? 2 : stores(8) ? 1 : 0;
   if (aligned && dvm_attention_tensor_cores(d)) {
     const bool single = dvm_attention_single(d);
-    st = single ? dvm_launch_attention_single(d, a, stream) : dvm_launch_attention_prompt(d, a, stream);
+    st = single ? dvm_launch_attention_single(d, a, stream) : dvm_launch_attention_prompt(d, a, dev.sm_count, stream);
     if (st == DVM_OK) t_last_kernel = single ? 1 : 2;
     return st;
   }

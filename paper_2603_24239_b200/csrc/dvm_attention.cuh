@@ -19,7 +19,7 @@ struct Args {
   int n, rows, hq, hk, group, D;    // group: query heads per kv head
   int pages, page_log, max_blocks;
   int window, sinks, max_q, out_bf16;
-  int out_vec;                      // 8 elements of bf16 output in one store
+  int out_vec;                      // bf16 output: 1: 8 elements in one store, 2: 16
   float scale;
 };
 

@@ -16,8 +16,11 @@
 // of bf16 or fp32; the quotient at the end does not depend on the maximum that was used); then the row's thread waits for
 // PV_x(t - 1).  Weights are rounded to bf16 for the second product, their sum is not.
 //
-// Roles: warps 0-3 and 4-7 the rows of the two tiles, warps 8 and 9 issue their products, warp 10 fetches (queries once,
-// then keys and values in turn through a ring, page by page).
+// CTAs stay (one per SM) and take blocks of rows in turn, so that a block's start -- tensor memory, barriers, lengths,
+// tables, queries, the first keys -- and its end hide behind its neighbours: started anew for each block they were 10,000
+// cycles beside 2,000 for a tile.  Roles: warps 0-3 and 4-7 the rows of the two tiles, warps 8 and 9 issue their products,
+// warp 10 fetches (a block's queries once the last score product of the block before has read its own, then keys and
+// values in turn through a ring, page by page), warp 11 finds the blocks and hands them on.
 //
 // Tokens a row does not see get a score of -inf.  That is not enough for the second product, where 0 x NaN is NaN: in
 // tiles with a mask the values that no row of the CTA sees are cleared in shared memory (they may be anything: the end of
@@ -40,7 +43,11 @@ using namespace sm100;
 
 constexpr int PT = 128;                  // rows of a row tile
 constexpr int KT = 64;                   // tokens of a cache tile
-constexpr int PROMPT_THREADS = 352;
+// Registers are dealt out by role: 384 threads are launched with 168 each, 64,512 in all; the two warpgroups that hold rows of
+// scores go up to ROW_REGS, the third down to OTHER_REGS: 256 x 216 + 128 x 72 = 64,512.
+constexpr int PROMPT_THREADS = 384;
+constexpr int ROW_REGS = 216, OTHER_REGS = 72;
+static_assert(256 * ROW_REGS + 128 * OTHER_REGS <= PROMPT_THREADS * 168, "an increase draws on the registers of the launch");
 constexpr uint32_t Q_HALF = PT * 128;    // 64 elements of the rows: 16 KB
 constexpr uint32_t KV_HALF = KT * 128;   // 64 elements of the tokens: 8 KB
 constexpr int HOLES = 16;                // tiles whose missing pages are remembered: more than the ring is deep
@@ -54,10 +61,11 @@ struct PromptSmem {
   static constexpr uint32_t STAGE = HALVES * KV_HALF;            // keys or values of a tile
   static constexpr uint32_t STAGES = DP == 128 ? 10 : 16;
   static constexpr uint32_t RING = 2 * Q_TILE;                   // behind the queries of both row tiles
-  static constexpr uint32_t BARS = RING + STAGES * STAGE;        // full[], empty[], q, s[2][2], p[2][2], o[2][2], drain[2]
-  static constexpr uint32_t WORDS = BARS + 16 * STAGES + 120;     // tensor memory address, abort, dirty[2], holes[]
-  static constexpr uint32_t SCAN = WORDS + 16 + 4 * HOLES;       // 12 sums, found request and block
-  static constexpr uint32_t BYTES = SCAN + 64 + 1024;
+  static constexpr uint32_t BARS = RING + STAGES * STAGE;        // see the kernel
+  static constexpr uint32_t WORDS = BARS + 16 * STAGES + 208;    // tensor memory address, abort, dirty[2][3], holes[]
+  static constexpr uint32_t WORK = WORDS + 32 + 4 * HOLES;       // two descriptions of blocks, the answer of a cancelled launch
+  static constexpr uint32_t BYTES = WORK + 2 * 64 + 16 + 1024;
+  static_assert(WORK % 16 == 0, "an answer is 16 bytes, aligned");
   static_assert(STAGES / 2 + 3 <= HOLES, "a tile's holes are kept until its weights are done");
 };
 
@@ -168,67 +176,17 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   uint8_t* const sm = smem_raw + (base - raw);
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;  // (the warp's number: known to be uniform)
-  const uint32_t bar_full = base + S::BARS, bar_empty = bar_full + 8 * S::STAGES, bar_q = bar_empty + 8 * S::STAGES, bar_s = bar_q + 8, bar_p = bar_s + 32,
-                 bar_o = bar_p + 32, bar_drain = bar_o + 32;  // s, p, o: of row tile x and place b = t & 1 at 16 x + 8 b
+  // full[], empty[]: the ring; q, qe: queries there, queries read; s, p, o of row tile x and place b at 16 x + 8 b: scores,
+  // weights, sums done; w, we: block descriptions; g: the threads of a row tile meet; drain; c: an answer
+  const uint32_t bar_full = base + S::BARS, bar_empty = bar_full + 8 * S::STAGES, bar_q = bar_empty + 8 * S::STAGES, bar_qe = bar_q + 8, bar_s = bar_q + 16,
+                 bar_p = bar_s + 32, bar_o = bar_p + 32, bar_w = bar_o + 32, bar_we = bar_w + 16, bar_g = bar_we + 16, bar_drain = bar_g + 16, bar_c = bar_drain + 16;
   volatile uint32_t* const words = (volatile uint32_t*)(sm + S::WORDS);
   volatile uint32_t* const abort_flag = words + 1;
-  volatile uint32_t* const dirty = words + 2;
-  volatile uint32_t* const holes = words + 4;
-  int* const scan = (int*)(sm + S::SCAN);
-
-  // ---- which request and block of rows: the blocks of all requests in a row, a request's last block first ----
+  volatile uint32_t* const dirty = words + 2;  // [x][block mod 3]
+  volatile uint32_t* const holes = words + 8;
+  volatile int* const work = (volatile int*)(sm + S::WORK);
   const int tokens = PT / a.group;  // of a row tile
-  const int block = blockIdx.x / a.hk, kvh = blockIdx.x - block * a.hk;
-  {
-    int before = 0;
-    bool found = false;
-    for (int i0 = 0; i0 < a.n; i0 += PROMPT_THREADS) {
-      const int i = i0 + threadIdx.x;
-      const int mine = i < a.n ? (min(request_at(a, i).q_len, a.max_q) + 2 * tokens - 1) / (2 * tokens) : 0;
-      int upto = mine;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, upto, d);
-        if (lane >= d) upto += y;
-      }
-      if (lane == 31) scan[warp] = upto;
-      __syncthreads();
-      int all = 0;
-#pragma unroll
-      for (int w = 0; w < PROMPT_THREADS / 32; ++w) {
-        if (w < warp) upto += scan[w];
-        all += scan[w];
-      }
-      const int at = block - before;
-      if (at >= upto - mine && at < upto) {
-        scan[12] = i;
-        scan[13] = upto - 1 - at;
-      }
-      __syncthreads();
-      found = at < all;
-      if (found) break;
-      before += all;
-    }
-    if (!found) return;  // (the grid is sized for the most blocks that `rows` rows can make)
-  }
-  const int request = scan[12], tok0 = scan[13] * 2 * tokens;
-  const Request rq = request_at(a, request);
-  const int n_tok = min(2 * tokens, min(rq.q_len, a.max_q) - tok0);
-  const long long p_first = rq.pos0 + tok0, p_last = p_first + n_tok - 1, held = (long long)a.max_blocks << a.page_log;
-  // tokens of the cache that some row sees: s < end and (s >= low or s < sinks); tiles: [0, ns), then [first, ...)
-  const int end = (int)max(0ll, min(p_last + 1, held));
-  const long long low_ll = a.window ? max(0ll, p_first - a.window + 1) : 0;
-  const int low = low_ll <= a.sinks ? 0 : (int)min(low_ll, 0x7fffffffll);
-  const int ns = low ? (min(a.sinks, end) + KT - 1) / KT : 0;
-  const int first = max(low / KT, ns);
-  // tiles that row tile x walks: its list ends with its own last position
-  auto tiles_of = [&](int x) -> int {
-    const int n = min(tokens, n_tok - x * tokens);
-    if (n <= 0) return 0;
-    const int last = (int)((max(0ll, min(p_first + x * tokens + n, held)) + KT - 1) / KT);
-    return last <= ns ? last : ns + max(0, last - first);
-  };
-  const int n0 = tiles_of(0), n1 = tiles_of(1), n_tiles = max(n0, n1);
+  const long long held = (long long)a.max_blocks << a.page_log;
 
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < S::STAGES; ++s) {
@@ -236,16 +194,20 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       mbar_init(bar_empty + 8 * s, 2);  // (both row tiles are done with it)
     }
     mbar_init(bar_q, 1);
+    mbar_init(bar_qe, 2);
     for (uint32_t x = 0; x < 2; ++x) {
       for (uint32_t b = 0; b < 2; ++b) {
         mbar_init(bar_s + 16 * x + 8 * b, 1);
         mbar_init(bar_p + 16 * x + 8 * b, 4);  // (one arrival per warp)
         mbar_init(bar_o + 16 * x + 8 * b, 1);
       }
-      dirty[x] = 0;
+      mbar_init(bar_w + 8 * x, 1);
+      mbar_init(bar_we + 8 * x, 11);           // (every warp but the one that finds blocks)
+      mbar_init(bar_g + 8 * x, 4);
+      mbar_init(bar_drain + 8 * x, 1);
     }
-    mbar_init(bar_drain, 1);
-    mbar_init(bar_drain + 8, 1);
+    mbar_init(bar_c, 1);
+    for (int i = 0; i < 6; ++i) dirty[i] = 0;
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -257,65 +219,176 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = words[0], tmem_o = tmem + 4 * KT;  // S_x at place b: 64 (2 x + b)
-  auto tile_at = [&](int j) -> int { return j < ns ? j : first + (j - ns); };
 
-  uint32_t issued = 0, f_stage = 0, f_phase = 0;  // the fetching warp's ring, kept for the abort path
-  if (warp == 10) {
+  // A block: up to 2 x tokens rows of query tokens of one request, for one kv head, described by 16 words of shared memory
+  // that stay until every warp has let them go.  Tiles of the cache: [0, ns), then [first, ...); tokens that some row sees:
+  // s < end and (s >= low or s < sinks); n0, n1: tiles that the row tiles walk; p_first: position of the first row's token.
+  enum { B_REQUEST, B_KVH, B_ROW0, B_TOKENS, B_N0, B_N1, B_NS, B_FIRST, B_END, B_LOW, B_P_LO, B_P_HI };
+  // the k-th block of this CTA, or none (also when a wait ran out)
+  auto take = [&](int k) -> volatile const int* {
+    const bool got = mbar_wait_flat(bar_w + 8 * (k & 1), (k >> 1) & 1, abort_flag);
+    volatile const int* const w = work + 16 * (k & 1);
+    return __all_sync(0xffffffffu, got) && w[B_TOKENS] > 0 ? w : nullptr;
+  };
+  auto let_go = [&](int k) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar_we + 8 * (k & 1));
+  };
+
+  uint32_t issued = 0, f_stage = 0, f_phase = 0;  // the fetching warp's ring and queries, kept for the abort path
+  int q_loads = 0;
+  if (warp == 11) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
+    // ---------------- blocks: those of all requests in a row, a request's last block first ----------------
+    int chunk = -32, before = 0, all = 0, mine = 0, upto = 0;  // 32 requests, the blocks before them, theirs
+    // The grid has a CTA for every block.  One that runs takes its own, then those of CTAs that have not started, in their
+    // order, by cancelling their launch: whoever is free takes the next, longest first, without a counter in memory.
+    const uint32_t answer = base + S::WORK + 128;
+    bool ok = true;
+    long long id = blockIdx.x;
+    for (int k = 0, asked = 0; ok;) {
+      const long long block = id < 0 ? -1 : id / a.hk;
+      bool any = id >= 0;
+      if (any && block < before) chunk = -32, before = all = 0;  // (an order that the hardware does not promise)
+      while (any && block >= (long long)before + all) {
+        before += all;
+        chunk += 32;
+        any = chunk < a.n;
+        const int i = chunk + lane;
+        mine = i < a.n ? (min(request_at(a, i).q_len, a.max_q) + 2 * tokens - 1) / (2 * tokens) : 0;
+        upto = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, upto, d);
+          if (lane >= d) upto += y;
+        }
+        all = __shfl_sync(0xffffffffu, upto, 31);
+      }
+      const int at = (int)(block - before);
+      const uint32_t owner = __ballot_sync(0xffffffffu, any && at >= upto - mine && at < upto);
+      const int src = owner ? __ffs(owner) - 1 : 0;
+      const int tok0 = __shfl_sync(0xffffffffu, upto - 1 - at, src) * 2 * tokens, request = chunk + src;
+      const bool beyond = !owner && id >= 0;  // (the grid is sized for the most blocks that `rows` rows can make)
+      if (!beyond) {
+      ok = k < 2 || mbar_wait_flat(bar_we + 8 * (k & 1), ((k >> 1) & 1) ^ 1, abort_flag);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      if (lane == 0) {
+        volatile int* const w = work + 16 * (k & 1);
+        w[B_TOKENS] = 0;
+        if (owner) {
+          const Request rq = request_at(a, request);
+          const int n_tok = min(2 * tokens, min(rq.q_len, a.max_q) - tok0);
+          const long long p_first = rq.pos0 + tok0;
+          const int end = (int)max(0ll, min(p_first + n_tok, held));
+          const long long from = a.window ? max(0ll, p_first - a.window + 1) : 0;
+          const int low = from <= a.sinks ? 0 : (int)min(from, 0x7fffffffll);
+          const int ns = low ? (min(a.sinks, end) + KT - 1) / KT : 0, first = max(low / KT, ns);
+          // tiles that row tile x walks: its list ends with its own last position
+          auto tiles_of = [&](int x) -> int {
+            const int n = min(tokens, n_tok - x * tokens);
+            if (n <= 0) return 0;
+            const int last = (int)((max(0ll, min(p_first + x * tokens + n, held)) + KT - 1) / KT);
+            return last <= ns ? last : ns + max(0, last - first);
+          };
+          w[B_REQUEST] = request; w[B_KVH] = (int)(id - block * a.hk); w[B_ROW0] = rq.s0 + tok0; w[B_TOKENS] = n_tok;
+          w[B_N0] = tiles_of(0); w[B_N1] = tiles_of(1); w[B_NS] = ns; w[B_FIRST] = first; w[B_END] = end; w[B_LOW] = low;
+          w[B_P_LO] = (int)(uint32_t)p_first; w[B_P_HI] = (int)(p_first >> 32);
+        }
+        mbar_arrive(bar_w + 8 * (k & 1));
+      }
+      __syncwarp();
+      if (!owner) break;
+      ++k;
+      }
+      if (lane == 0) {
+        mbar_expect_tx(bar_c, 16);
+        asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer), "r"(bar_c) : "memory");
+      }
+      __syncwarp();
+      ok = __all_sync(0xffffffffu, mbar_wait_flat(bar_c, asked++ & 1, abort_flag));
+      uint32_t got = 0, cta = 0;
+      asm volatile(
+          "{\n\t.reg .pred p;\n\t.reg .b128 r;\n\tld.shared.b128 r, [%2];\n\tclusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+          "selp.u32 %0, 1, 0, p;\n\tmov.u32 %1, 0;\n\t@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n\t}"
+          : "=r"(got), "=r"(cta)
+          : "r"(answer)
+          : "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // (read before the next answer is written)
+      __syncwarp();
+      id = ok && got ? (long long)cta : -1;  // none left: the end is handed on like a block
+    }
+  } else if (warp == 10) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
     // ---------------- fetch ----------------
     const int copy_log = min(a.page_log, 6), copies = KT >> copy_log;
-    const int* table = a.table + (long long)request * a.max_blocks;
-    auto page_of = [&](int j) -> int {  // of this lane's copy of tile j; -1 where it holds no token that some row sees
-      if (lane >= copies || j >= n_tiles) return -1;
-      const long long s = (long long)tile_at(j) * KT + ((long long)lane << copy_log);
-      if (s >= end || (s + (1 << copy_log) <= low && s >= a.sinks)) return -1;
-      const int page = table[s >> a.page_log];
-      return page >= 0 && page < a.pages ? page : -1;
-    };
-    if (lane == 0 && n_tiles > 0) {
-      const uint32_t rows = (uint32_t)(tokens * a.group) * 128 * S::HALVES;
-      mbar_expect_tx(bar_q, (n1 > 0 || n_tok > tokens ? 2 : 1) * rows);
-      for (int x = 0; x < (n1 > 0 || n_tok > tokens ? 2 : 1); ++x)
-        for (uint32_t h = 0; h < S::HALVES; ++h)
-          tma_load_4d(base + x * S::Q_TILE + h * Q_HALF, &tm_q, bar_q, 64 * h, 0, kvh, rq.s0 + tok0 + x * tokens);
-    }
-    __syncwarp();
     bool ok = true;
-    int page = page_of(0);
-    for (int j = 0; ok && j < n_tiles; ++j) {
-      const int next = page_of(j + 1);  // (its latency hides behind the waits below)
-      const uint32_t missing = __ballot_sync(0xffffffffu, lane < copies && page < 0);
-      const int off = (int)(((long long)tile_at(j) * KT + ((long long)lane << copy_log)) & ((1ll << a.page_log) - 1));
-#pragma unroll
-      for (int kv = 0; kv < 2; ++kv) {
-        ok = mbar_wait(bar_empty + 8 * f_stage, f_phase ^ 1, abort_flag);
-        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-        const uint32_t full = bar_full + 8 * f_stage, at = base + S::RING + f_stage * S::STAGE;
-        if (lane == 0) {
-          if (kv == 0) holes[j % HOLES] = missing;
-          mbar_expect_tx(full, S::STAGE);
-        }
-        __syncwarp();
-        if (lane < copies)
+    int seen = 0;  // tiles of the blocks before
+    for (int k = 0; ok; ++k) {
+      volatile const int* const w = take(k);
+      if (!w) break;
+      const int n_tok = w[B_TOKENS], n_tiles = max(w[B_N0], w[B_N1]), ns = w[B_NS], first = w[B_FIRST], end = w[B_END], low = w[B_LOW], kvh = w[B_KVH], row0 = w[B_ROW0];
+      const int* table = a.table + (long long)w[B_REQUEST] * a.max_blocks;
+      let_go(k);
+      if (n_tiles == 0) continue;
+      auto tile_at = [&](int j) -> int { return j < ns ? j : first + (j - ns); };
+      auto page_of = [&](int j) -> int {  // of this lane's copy of tile j; -1 where it holds no token that some row sees
+        if (lane >= copies || j >= n_tiles) return -1;
+        const long long s = (long long)tile_at(j) * KT + ((long long)lane << copy_log);
+        if (s >= end || (s + (1 << copy_log) <= low && s >= a.sinks)) return -1;
+        const int page = table[s >> a.page_log];
+        return page >= 0 && page < a.pages ? page : -1;
+      };
+      int page = page_of(0);
+      ok = __all_sync(0xffffffffu, q_loads == 0 || mbar_wait_flat(bar_qe, (q_loads - 1) & 1, abort_flag));
+      if (!ok) break;
+      if (lane == 0) {
+        const int active = n_tok > tokens ? 2 : 1;
+        mbar_expect_tx(bar_q, active * (uint32_t)(tokens * a.group) * 128 * S::HALVES);
+        for (int x = 0; x < active; ++x)
           for (uint32_t h = 0; h < S::HALVES; ++h)
-            tma_load_4d(at + h * KV_HALF + ((uint32_t)lane << (copy_log + 7)), kv ? &tm_v : &tm_k, full, 64 * h, off, kvh, page);
-        ++issued;
-        if (++f_stage == S::STAGES) { f_stage = 0; f_phase ^= 1; }
+            tma_load_4d(base + x * S::Q_TILE + h * Q_HALF, &tm_q, bar_q, 64 * h, 0, kvh, row0 + x * tokens);
       }
-      page = next;
+      ++q_loads;
+      __syncwarp();
+      for (int j = 0; ok && j < n_tiles; ++j) {
+        const int next = page_of(j + 1);  // (its latency hides behind the waits below)
+        const uint32_t missing = __ballot_sync(0xffffffffu, lane < copies && page < 0);
+        const int off = (int)(((long long)tile_at(j) * KT + ((long long)lane << copy_log)) & ((1ll << a.page_log) - 1));
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          ok = __all_sync(0xffffffffu, ok && mbar_wait_flat(bar_empty + 8 * f_stage, f_phase ^ 1, abort_flag));
+          if (!ok) break;
+          const uint32_t full = bar_full + 8 * f_stage, at = base + S::RING + f_stage * S::STAGE;
+          if (lane == 0) {
+            if (kv == 0) holes[(seen + j) % HOLES] = missing;
+            mbar_expect_tx(full, S::STAGE);
+          }
+          __syncwarp();
+          if (lane < copies)
+            for (uint32_t h = 0; h < S::HALVES; ++h)
+              tma_load_4d(at + h * KV_HALF + ((uint32_t)lane << (copy_log + 7)), kv ? &tm_v : &tm_k, full, 64 * h, off, kvh, page);
+          ++issued;
+          if (++f_stage == S::STAGES) { f_stage = 0; f_phase ^= 1; }
+        }
+        page = next;
+      }
+      seen += n_tiles;
     }
     __syncwarp();
   } else if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
     // ---------------- products of one row tile ----------------
     // The whole warp walks, so that descriptors and barriers stay in uniform registers; one elected lane issues.  (Issued
     // from a branch of lane 0 alone, with the descriptors formed anew, a product took 70 to 100 cycles to issue, more than
     // it takes to run.)
-    const int x = warp - 8, nx = x ? n1 : n0;
+    const int x = warp - 8;
     const bool leader = elect_one();
-    bool ok = n_tiles == 0 || mbar_wait(bar_q, 0, abort_flag);
+    bool ok = true;
     // the low words of the descriptors: a stage or a step of the inner dimension is an addition to them
     const uint32_t q_lo = desc_lo(base + x * S::Q_TILE, 1), k_lo = desc_lo(base + S::RING, 1), v_lo = desc_lo(base + S::RING, KV_HALF >> 4);
     const uint32_t d_s = tmem + 2 * KT * x, d_o = tmem_o + x * DP;
     uint32_t k_stage = 0, k_phase = 0, v_stage = 1, v_phase = 0;  // two walks over the ring, that of the keys two tiles ahead
+    int g = 0, queries = 0;                                       // tiles of this row tile and blocks with tiles so far
     auto step = [](uint32_t& stage, uint32_t& phase) {
       stage += 2;
       if (stage >= S::STAGES) { stage -= S::STAGES; phase ^= 1; }
@@ -339,64 +412,80 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         umma_commit(bar_empty + 8 * v_stage);
       }
     };
-    for (int t = 0; ok && t < min(2, n_tiles); ++t) {
-      ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * k_stage, k_phase, abort_flag));
-      if (!ok) break;
-      tc_fence_after();
-      if (t < nx) qk(t);
-      else if (leader) mbar_arrive(bar_empty + 8 * k_stage);
-      step(k_stage, k_phase);
-    }
-    for (int t = 0; ok && t < n_tiles; ++t) {
-      const int b = t & 1;
-      ok = mbar_wait(bar_full + 8 * v_stage, v_phase, abort_flag);
-      if (t < nx) ok = ok && mbar_wait(bar_p + 16 * x + 8 * b, (t >> 1) & 1, abort_flag);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      tc_fence_after();
-      if (t < nx) pv(b, t != 0);
-      else if (leader) mbar_arrive(bar_empty + 8 * v_stage);
-      step(v_stage, v_phase);
-      if (t + 2 < n_tiles) {
-        ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * k_stage, k_phase, abort_flag));
+    for (int k = 0; ok; ++k) {
+      volatile const int* const w = take(k);
+      if (!w) break;
+      const int n_tiles = max(w[B_N0], w[B_N1]), nx = w[x ? B_N1 : B_N0];
+      let_go(k);
+      if (n_tiles == 0) continue;
+      ok = __all_sync(0xffffffffu, mbar_wait_flat(bar_q, queries++ & 1, abort_flag));
+      auto scores = [&](int t) -> bool {  // QK(t), if this row tile walks that far; else the keys are let go unread
+        if (!__all_sync(0xffffffffu, mbar_wait_flat(bar_full + 8 * k_stage, k_phase, abort_flag))) return false;
+        tc_fence_after();
+        if (t < nx) qk((g + t) & 1);
+        else if (leader) mbar_arrive(bar_empty + 8 * k_stage);
+        if (leader && t + 1 == max(nx, 1)) {  // the queries have been read (or are not wanted)
+          if (nx > 0) umma_commit(bar_qe);
+          else mbar_arrive(bar_qe);
+        }
+        step(k_stage, k_phase);
+        return true;
+      };
+      for (int t = 0; ok && t < min(2, n_tiles); ++t) ok = scores(t);
+      for (int t = 0; ok && t < n_tiles; ++t) {
+        const int b = (g + t) & 1;
+        ok = mbar_wait_flat(bar_full + 8 * v_stage, v_phase, abort_flag);
+        if (t < nx) ok = ok && mbar_wait_flat(bar_p + 16 * x + 8 * b, ((g + t) >> 1) & 1, abort_flag);
+        ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tc_fence_after();
-        if (t + 2 < nx) qk(b);
-        else if (leader) mbar_arrive(bar_empty + 8 * k_stage);
-        step(k_stage, k_phase);
+        if (t < nx) pv(b, t != 0);
+        else if (leader) mbar_arrive(bar_empty + 8 * v_stage);
+        step(v_stage, v_phase);
+        if (t + 2 < n_tiles) ok = scores(t + 2);
       }
+      g += nx;
     }
     __syncwarp();
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(ROW_REGS));
     // ---------------- weights: one row per thread ----------------
     const int x = warp >> 2, row = (warp & 3) * 32 + lane;
     const int tok = row / a.group, head = row - tok * a.group;  // of the row tile; of the group
-    const int n_rows = min(tokens, n_tok - x * tokens);         // tokens of this row tile
-    const bool valid = tok < n_rows;
-    const int nx = x ? n1 : n0;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_o = tmem_o + x * DP + lanes;
     const float c = a.scale * 1.4426950408889634f;
-    const long long p0 = p_first + x * tokens;                  // position of the row tile's first token
+    int g = 0, seen_tiles = 0;  // tiles of this row tile, of the CTA so far
+    bool ok = true;
+    for (int k = 0; ok; ++k) {
+    volatile const int* const w = take(k);
+    if (!w) break;
+    const int n_rows = min(tokens, w[B_TOKENS] - x * tokens);   // tokens of this row tile
+    const int nx = w[x ? B_N1 : B_N0], ns = w[B_NS], first = w[B_FIRST];
+    auto position = [&]() -> long long {                        // of the row tile's first token
+      return (long long)(((unsigned long long)(uint32_t)w[B_P_HI] << 32) | (uint32_t)w[B_P_LO]) + x * tokens;
+    };
+    const long long p0 = position();
     // this row sees the tokens up to hi_at that are from lo_at on or below the sinks; every row of the tile sees those up
     // to all_hi that are from all_lo on
     auto cut = [](long long v) -> int { return (int)max(-1ll, min(v, 0x7fffffffll)); };
     const int hi_at = cut(min(p0 + tok, held - 1)), lo_at = a.window ? max(0, cut(p0 + tok - a.window + 1)) : 0;
     const int all_hi = cut(min(p0, held - 1)), all_lo = a.window ? max(0, cut(p0 + n_rows - a.window)) : 0;
     float m = -INFINITY, l = 0.f;
-    bool ok = true;
+    if (row == 0) dirty[3 * x + (k + 1) % 3] = 0;  // (last read before the threads met for block k - 2, next set for k + 1)
     // The scores of tile t + 1 are on their way while the second half of tile t's weights is formed: the lower half goes to
     // the registers that tile t's lower half has left, the upper half to those of the tile before.
-    float s_lo[32], s_hi[2][32];
+    float s_lo[32], s_next[32];
     auto scores = [&](int t) -> bool {  // tile t's scores are in tensor memory
-      const bool got = mbar_wait(bar_s + 16 * x + 8 * (t & 1), (t >> 1) & 1, abort_flag);
+      const bool got = mbar_wait_flat(bar_s + 16 * x + 8 * ((g + t) & 1), ((g + t) >> 1) & 1, abort_flag);
       tc_fence_after();
       return __all_sync(0xffffffffu, got);
     };
-    auto tile = [&](int t, float* hi_now, float* hi_next) -> bool {
-      const uint32_t t_s = tmem + KT * (2 * x + (t & 1)) + lanes, t_next = tmem + KT * (2 * x + ((t + 1) & 1)) + lanes;
-      const int key0 = tile_at(t) * KT;
-      const uint32_t missing = holes[t % HOLES];
+    auto tile = [&](int t) -> bool {
+      const int b = (g + t) & 1;
+      const uint32_t t_s = tmem + KT * (2 * x + b) + lanes, t_next = tmem + KT * (2 * x + (b ^ 1)) + lanes;
+      const int key0 = (t < ns ? t : first + (t - ns)) * KT;
+      const uint32_t missing = holes[(seen_tiles + t) % HOLES];
       const bool whole = missing == 0 && key0 + KT - 1 <= all_hi && (key0 >= all_lo || key0 <= a.sinks - KT);
       uint32_t seen[2] = {0xffffffffu, 0xffffffffu};
       if (!whole) {
@@ -404,39 +493,39 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         const int hi = hi_at - key0, lo = lo_at - key0, sk = a.sinks - key0;
         const int copy_log = min(a.page_log, 6);
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          seen[w] = bits_below(hi + 1 - 32 * w) & (~bits_below(lo - 32 * w) | bits_below(sk - 32 * w));
+        for (int h = 0; h < 2; ++h) {
+          seen[h] = bits_below(hi + 1 - 32 * h) & (~bits_below(lo - 32 * h) | bits_below(sk - 32 * h));
           if (missing) {
             uint32_t there = 0;
 #pragma unroll
             for (int b = 0; b < 4; ++b)
-              if (!((missing >> ((32 * w + 8 * b) >> copy_log)) & 1u)) there |= 0xffu << (8 * b);
-            seen[w] &= there;
+              if (!((missing >> ((32 * h + 8 * b) >> copy_log)) & 1u)) there |= 0xffu << (8 * b);
+            seen[h] &= there;
           }
         }
         // the values of this tile (two threads per token): cleared where no row of the CTA sees them, else looked at
-        const uint32_t vi = 2 * t + 1;
-        if (!__all_sync(0xffffffffu, mbar_wait(bar_full + 8 * (vi % S::STAGES), (vi / S::STAGES) & 1, abort_flag))) return false;
+        const uint32_t vi = 2 * (seen_tiles + t) + 1;
+        if (!__all_sync(0xffffffffu, mbar_wait_flat(bar_full + 8 * (vi % S::STAGES), (vi / S::STAGES) & 1, abort_flag))) return false;
         const int vrow = row & (KT - 1);
-        const bool any = key0 + vrow < end && (key0 + vrow >= low || key0 + vrow < a.sinks) && !((missing >> (vrow >> copy_log)) & 1u);
+        const bool any = key0 + vrow < w[B_END] && (key0 + vrow >= w[B_LOW] || key0 + vrow < a.sinks) && !((missing >> (vrow >> copy_log)) & 1u);
         uint8_t* const v = sm + S::RING + (vi % S::STAGES) * S::STAGE + vrow * 128;
         const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
         __nv_bfloat162 test = zero;
 #pragma unroll
-        for (uint32_t k = 0; k < 4 * S::HALVES; ++k) {
-          const uint32_t q = k + (row >> 6) * 4 * S::HALVES;
+        for (uint32_t i = 0; i < 4 * S::HALVES; ++i) {
+          const uint32_t q = i + (row >> 6) * 4 * S::HALVES;
           uint4* const at = (uint4*)(v + (q >> 3) * KV_HALF + (((q & 7) ^ (row & 7)) << 4));
           if (any) {
-            const uint4 w = *at;
-            test = __hfma2(*(const __nv_bfloat162*)&w.x, zero, test);
-            test = __hfma2(*(const __nv_bfloat162*)&w.y, zero, test);
-            test = __hfma2(*(const __nv_bfloat162*)&w.z, zero, test);
-            test = __hfma2(*(const __nv_bfloat162*)&w.w, zero, test);
+            const uint4 u = *at;
+            test = __hfma2(*(const __nv_bfloat162*)&u.x, zero, test);
+            test = __hfma2(*(const __nv_bfloat162*)&u.y, zero, test);
+            test = __hfma2(*(const __nv_bfloat162*)&u.z, zero, test);
+            test = __hfma2(*(const __nv_bfloat162*)&u.w, zero, test);
           } else {
             *at = make_uint4(0, 0, 0, 0);
           }
         }
-        if (__isnan(__low2float(test)) || __isnan(__high2float(test))) dirty[x] = 1;
+        if (__isnan(__low2float(test)) || __isnan(__high2float(test))) dirty[3 * x + k % 3] = 1;
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       }
       auto hide = [&](float* s, uint32_t bits) {
@@ -451,10 +540,13 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         return max_nan(max_nan(max_nan(t0, s[31]), t1), max_nan(t2, t3));
       };
       tmem_landed(s_lo);
-      tmem_landed(hi_now);
-      if (!whole) { hide(s_lo, seen[0]); hide(hi_now, seen[1]); }
+      tmem_landed(s_next);
+      float s_hi[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) s_hi[i] = s_next[i];
+      if (!whole) { hide(s_lo, seen[0]); hide(s_hi, seen[1]); }
       // a NaN score makes the maximum NaN and with it every weight of the row, as the quotient has it
-      const float top = highest(hi_now, highest(s_lo, -INFINITY));
+      const float top = highest(s_hi, highest(s_lo, -INFINITY));
       const float m_new = max_nan(m, top);
       if (__any_sync(0xffffffffu, (m_new - m) * c > GROWTH || m_new != m_new)) {  // (from -inf: yes, unless it stays there)
         const float keep = m_new == m ? 1.f : ex2((m - m_new) * c);
@@ -462,7 +554,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         m = m_new;
         if (t > 0) {
           // PV(t - 1) is done; PV(t) waits for this tile's weights
-          if (!__all_sync(0xffffffffu, mbar_wait(bar_o + 16 * x + 8 * ((t - 1) & 1), ((t - 1) >> 1) & 1, abort_flag))) return false;
+          if (!__all_sync(0xffffffffu, mbar_wait_flat(bar_o + 16 * x + 8 * (b ^ 1), ((g + t - 1) >> 1) & 1, abort_flag))) return false;
           tc_fence_after();
 #pragma unroll
           for (int q = 0; q < DP / 32; ++q) {
@@ -495,76 +587,90 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       weigh(s_lo, 0);
       // the next scores, if they are there already; nothing waits for them before this tile's weights are handed over
       const bool more = t + 1 < nx;
-      const bool early = more && __all_sync(0xffffffffu, mbar_test(bar_s + 16 * x + 8 * ((t + 1) & 1), ((t + 1) >> 1) & 1));
+      const bool early = more && __all_sync(0xffffffffu, mbar_test(bar_s + 16 * x + 8 * (b ^ 1), ((g + t + 1) >> 1) & 1));
       if (early) {
         tc_fence_after();
         tmem_load32(t_next, s_lo);
-        tmem_load32(t_next + 32, hi_next);
+        tmem_load32(t_next + 32, s_next);
       }
-      weigh(hi_now, 1);
+      weigh(s_hi, 1);
       l += (l01.x + l01.y) + (l23.x + l23.y);
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar_p + 16 * x + 8 * (t & 1));
+      if (lane == 0) mbar_arrive(bar_p + 16 * x + 8 * b);
       if (more && !early) {
         if (!scores(t + 1)) return false;
         tmem_load32(t_next, s_lo);
-        tmem_load32(t_next + 32, hi_next);
+        tmem_load32(t_next + 32, s_next);
       }
       return true;
     };
     if (nx > 0) {
       ok = scores(0);
       if (ok) {
-        tmem_load32(tmem + 2 * KT * x + lanes, s_lo);
-        tmem_load32(tmem + 2 * KT * x + lanes + 32, s_hi[0]);
+        tmem_load32(tmem + KT * (2 * x + (g & 1)) + lanes, s_lo);
+        tmem_load32(tmem + KT * (2 * x + (g & 1)) + lanes + 32, s_next);
       }
-      for (int t = 0; ok && t < nx; t += 2) {
-        ok = tile(t, s_hi[0], s_hi[1]);
-        if (ok && t + 1 < nx) ok = tile(t + 1, s_hi[1], s_hi[0]);
-      }
+      for (int t = 0; ok && t < nx; ++t) ok = tile(t);
     }
-    tmem_load_wait();  // (a walk that gave up may have loads on their way)
-    // ---- the row's quotient ----
-    if (n_rows > 0) {
-      if (ok && nx > 0) ok = mbar_wait(bar_o + 16 * x + 8 * ((nx - 1) & 1), ((nx - 1) >> 1) & 1, abort_flag);
-      ok = __all_sync(0xffffffffu, ok);
+    const int last = g + nx - 1;
+    if (ok && nx > 0) {
+      ok = __all_sync(0xffffffffu, mbar_wait_flat(bar_o + 16 * x + 8 * (last & 1), (last >> 1) & 1, abort_flag));
       tc_fence_after();
-      if (ok) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        const long long at = (long long)(rq.s0 + tok0 + x * tokens + tok) * a.os[0] + (long long)(kvh * a.group + head) * a.os[1];
+    }
+    if (ok && n_rows > 0) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const long long at = (long long)(w[B_ROW0] + x * tokens + tok) * a.os[0] + (long long)(w[B_KVH] * a.group + head) * a.os[1];
 #pragma unroll
-        for (int q = 0; q < DP / 32; ++q) {
-          float o[32];
-          if (nx > 0) {
-            tmem_load32(t_o + 32 * q, o);
-            tmem_landed(o);
-          }
+      for (int q = 0; q < DP / 32; ++q) {
+        float o[32];
+        if (nx > 0) {
+          tmem_load32(t_o + 32 * q, o);
+          tmem_landed(o);
+        }
 #pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] = nx > 0 && l != 0.f ? o[i] * inv : 0.f;
-          if (valid) {
-            if (a.out_vec && a.out_bf16) {
-              uint4* out = (uint4*)((__nv_bfloat16*)a.out + at + 32 * q);
+        for (int i = 0; i < 32; ++i) o[i] = nx > 0 && l != 0.f ? o[i] * inv : 0.f;
+        if (tok >= n_rows) continue;
+        if (a.out_vec) {
+          __nv_bfloat16* const out = (__nv_bfloat16*)a.out + at + 32 * q;
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (32 * q + 8 * i < a.D)
-                  out[i] = make_uint4(pack_bf16(o[8 * i], o[8 * i + 1]), pack_bf16(o[8 * i + 2], o[8 * i + 3]), pack_bf16(o[8 * i + 4], o[8 * i + 5]),
-                                      pack_bf16(o[8 * i + 6], o[8 * i + 7]));
+          for (int i = 0; i < 4; i += 2) {
+            uint32_t u[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] = pack_bf16(o[8 * i + 2 * e], o[8 * i + 2 * e + 1]);
+            if (a.out_vec == 2) {  // a whole 32-byte sector at a time
+              if (32 * q + 8 * i < a.D)
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + 8 * i), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]),
+                             "r"(u[5]), "r"(u[6]), "r"(u[7])
+                             : "memory");
             } else {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (32 * q + i < a.D) put(a.out, a.out_bf16, at + 32 * q + i, o[i]);
+              if (32 * q + 8 * i < a.D) *(uint4*)(out + 8 * i) = make_uint4(u[0], u[1], u[2], u[3]);
+              if (32 * q + 8 * i + 8 < a.D) *(uint4*)(out + 8 * i + 8) = make_uint4(u[4], u[5], u[6], u[7]);
             }
           }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (32 * q + i < a.D) put(a.out, a.out_bf16, at + 32 * q + i, o[i]);
         }
       }
+      tc_fence_before();  // (the next block's first product into O_x comes after this row's next arrival)
     }
-    // a value that some of these rows see and others do not was not finite: the rows again, one warp each
-    asm volatile("bar.sync 1, 256;" ::: "memory");  // (every warp of the two row tiles comes here)
-    if (dirty[x] && !*abort_flag)
+    // a value that some of these rows see and others do not was not finite: the rows again, one warp each.  The threads of
+    // the row tile meet first, so that all have seen all tiles and stored their rows.
+    __syncwarp();
+    if (ok) {
+      if (lane == 0) mbar_arrive(bar_g + 8 * x);
+      ok = __all_sync(0xffffffffu, mbar_wait_flat(bar_g + 8 * x, k & 1, abort_flag));
+    }
+    if (ok && dirty[3 * x + k % 3])
       for (int r = warp & 3; r < n_rows * a.group; r += 4)
-        attend_row<__nv_bfloat16>(a, request, p0 + r / a.group, rq.s0 + tok0 + x * tokens + r / a.group, kvh * a.group + r % a.group);
+        attend_row<__nv_bfloat16>(a, w[B_REQUEST], position() + r / a.group, w[B_ROW0] + x * tokens + r / a.group, w[B_KVH] * a.group + r % a.group);
+    g += nx;
+    seen_tiles += max(w[B_N0], w[B_N1]);
+    let_go(k);
+    }
   }
 
   // ---------------- teardown ----------------
@@ -574,13 +680,13 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     if (warp == 10 && lane == 0) {  // the latest fill of every stage, and the queries
       for (uint32_t k = min(issued, S::STAGES); k > 0; --k) {
         if (f_stage == 0) { f_stage = S::STAGES - 1; f_phase ^= 1; } else --f_stage;
-        if (!mbar_try(bar_full + 8 * f_stage, f_phase)) mbar_wait_slow(bar_full + 8 * f_stage, f_phase, abort_flag, DRAIN_NS, false);
+        if (!mbar_try(bar_full + 8 * f_stage, f_phase)) mbar_spin(bar_full + 8 * f_stage, f_phase, abort_flag, DRAIN_NS, false);
       }
-      if (n_tiles > 0 && !mbar_try(bar_q, 0)) mbar_wait_slow(bar_q, 0, abort_flag, DRAIN_NS, false);
+      if (q_loads > 0 && !mbar_try(bar_q, (q_loads - 1) & 1)) mbar_spin(bar_q, (q_loads - 1) & 1, abort_flag, DRAIN_NS, false);
     }
     if ((warp == 8 || warp == 9) && elect_one()) {  // (the lanes that issued)
       umma_commit(bar_drain + 8 * (warp - 8));
-      if (!mbar_try(bar_drain + 8 * (warp - 8), 0)) mbar_wait_slow(bar_drain + 8 * (warp - 8), 0, abort_flag, DRAIN_NS, false);
+      if (!mbar_try(bar_drain + 8 * (warp - 8), 0)) mbar_spin(bar_drain + 8 * (warp - 8), 0, abort_flag, DRAIN_NS, false);
     }
     if (threadIdx.x == 0) atomicMax(a.status, (unsigned int)ST_TIMEOUT);
     __syncthreads();
@@ -603,7 +709,7 @@ int launch_prompt(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap&
 }  // namespace att
 }  // namespace dvm
 
-int dvm_launch_attention_prompt(const dvm_attention_desc& d, const dvm::att::Args& a, cudaStream_t stream) {
+int dvm_launch_attention_prompt(const dvm_attention_desc& d, const dvm::att::Args& a, int sms, cudaStream_t stream) {
   using namespace dvm::att;
   const int tokens = PT / a.group;
   CUtensorMap q, k, v;

@@ -46,8 +46,8 @@ __device__ __forceinline__ unsigned long long gtimer() {
 }
 // Bounded wait: gives up after limit_ns (or WAIT_SPINS polls), raising the CTA's abort flag; with
 // heed_abort it also gives up as soon as another role has raised the flag.
-static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag,
-                                            unsigned long long limit_ns, bool heed_abort) {
+__device__ __forceinline__ bool mbar_spin(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag,
+                                          unsigned long long limit_ns, bool heed_abort) {
   const unsigned long long t0 = gtimer();
   for (uint32_t spin = 0; spin < WAIT_SPINS; ++spin) {
     if (mbar_try(bar, parity)) return true;
@@ -56,6 +56,14 @@ static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity
   }
   *abort_flag = 1;
   return false;
+}
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag,
+                                                   unsigned long long limit_ns, bool heed_abort) {
+  return mbar_spin(bar, parity, abort_flag, limit_ns, heed_abort);
+}
+// The same without a call: for kernels that deal out registers by role (setmaxnreg), where a callee has no count of its own.
+__device__ __forceinline__ bool mbar_wait_flat(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag) {
+  return mbar_try(bar, parity) || mbar_spin(bar, parity, abort_flag, WAIT_NS, true);
 }
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag) {
   if (mbar_try(bar, parity)) return true;
