@@ -62,8 +62,8 @@ struct PromptSmem {
   static constexpr uint32_t STAGES = DP == 128 ? 10 : 16;
   static constexpr uint32_t RING = 2 * Q_TILE;                   // behind the queries of both row tiles
   static constexpr uint32_t BARS = RING + STAGES * STAGE;        // see the kernel
-  static constexpr uint32_t WORDS = BARS + 16 * STAGES + 208;    // tensor memory address, abort, dirty[2][3], holes[]
-  static constexpr uint32_t WORK = WORDS + 32 + 4 * HOLES;       // two descriptions of blocks, the answer of a cancelled launch
+  static constexpr uint32_t WORDS = BARS + 16 * STAGES + 192;    // tensor memory address, abort, dirty[2][4], holes[]
+  static constexpr uint32_t WORK = WORDS + 48 + 4 * HOLES;       // two descriptions of blocks, the answer of a cancelled launch
   static constexpr uint32_t BYTES = WORK + 2 * 64 + 16 + 1024;
   static_assert(WORK % 16 == 0, "an answer is 16 bytes, aligned");
   static_assert(STAGES / 2 + 3 <= HOLES, "a tile's holes are kept until its weights are done");
@@ -142,6 +142,11 @@ __device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either i
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
   return d;
 }
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 // 2^x without the special function unit, for part of the weights: the unit's 16 results a cycle are what the weights take
 // longest for, while multiply-adds are to spare.  x = f + r with f the nearest integer (1.5 2^23 added and taken away) and
 // |r| <= 1/2; 2^r by a polynomial of degree 5 fitted for least relative error (1.7e-7 in fp32) with constant term 1, so
@@ -177,13 +182,13 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
   uint8_t* const sm = smem_raw + (base - raw);
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;  // (the warp's number: known to be uniform)
   // full[], empty[]: the ring; q, qe: queries there, queries read; s, p, o of row tile x and place b at 16 x + 8 b: scores,
-  // weights, sums done; w, we: block descriptions; g: the threads of a row tile meet; drain; c: an answer
+  // weights, sums done; w, we: block descriptions; drain; c: an answer
   const uint32_t bar_full = base + S::BARS, bar_empty = bar_full + 8 * S::STAGES, bar_q = bar_empty + 8 * S::STAGES, bar_qe = bar_q + 8, bar_s = bar_q + 16,
-                 bar_p = bar_s + 32, bar_o = bar_p + 32, bar_w = bar_o + 32, bar_we = bar_w + 16, bar_g = bar_we + 16, bar_drain = bar_g + 16, bar_c = bar_drain + 16;
+                 bar_p = bar_s + 32, bar_o = bar_p + 32, bar_w = bar_o + 32, bar_we = bar_w + 16, bar_drain = bar_we + 16, bar_c = bar_drain + 16;
   volatile uint32_t* const words = (volatile uint32_t*)(sm + S::WORDS);
   volatile uint32_t* const abort_flag = words + 1;
-  volatile uint32_t* const dirty = words + 2;  // [x][block mod 3]
-  volatile uint32_t* const holes = words + 8;
+  volatile uint32_t* const dirty = words + 2;  // [x][block mod 4]
+  volatile uint32_t* const holes = words + 10;
   volatile int* const work = (volatile int*)(sm + S::WORK);
   const int tokens = PT / a.group;  // of a row tile
   const long long held = (long long)a.max_blocks << a.page_log;
@@ -203,11 +208,10 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       }
       mbar_init(bar_w + 8 * x, 1);
       mbar_init(bar_we + 8 * x, 11);           // (every warp but the one that finds blocks)
-      mbar_init(bar_g + 8 * x, 4);
       mbar_init(bar_drain + 8 * x, 1);
     }
     mbar_init(bar_c, 1);
-    for (int i = 0; i < 6; ++i) dirty[i] = 0;
+    for (int i = 0; i < 8; ++i) dirty[i] = 0;
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -472,7 +476,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     const int hi_at = cut(min(p0 + tok, held - 1)), lo_at = a.window ? max(0, cut(p0 + tok - a.window + 1)) : 0;
     const int all_hi = cut(min(p0, held - 1)), all_lo = a.window ? max(0, cut(p0 + n_rows - a.window)) : 0;
     float m = -INFINITY, l = 0.f;
-    if (row == 0) dirty[3 * x + (k + 1) % 3] = 0;  // (last read before the threads met for block k - 2, next set for k + 1)
+    if (row == 0) dirty[4 * x + ((k + 2) & 3)] = 0;  // (block k - 2 is through in every warp, or k were not here; k + 2 not before all let k go)
     // The scores of tile t + 1 are on their way while the second half of tile t's weights is formed: the lower half goes to
     // the registers that tile t's lower half has left, the upper half to those of the tile before.
     float s_lo[32], s_next[32];
@@ -503,30 +507,40 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
             seen[h] &= there;
           }
         }
-        // the values of this tile (two threads per token): cleared where no row of the CTA sees them, else looked at
+        // The values of this tile, two threads per token.  Hidden tokens meet weights of 0, which does it unless their values
+        // are not finite: then they are cleared if no row of the CTA sees the token, else the block's rows are done again.
         const uint32_t vi = 2 * (seen_tiles + t) + 1;
         if (!__all_sync(0xffffffffu, mbar_wait_flat(bar_full + 8 * (vi % S::STAGES), (vi / S::STAGES) & 1, abort_flag))) return false;
         const int vrow = row & (KT - 1);
-        const bool any = key0 + vrow < w[B_END] && (key0 + vrow >= w[B_LOW] || key0 + vrow < a.sinks) && !((missing >> (vrow >> copy_log)) & 1u);
         uint8_t* const v = sm + S::RING + (vi % S::STAGES) * S::STAGE + vrow * 128;
-        const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
-        __nv_bfloat162 test = zero;
-#pragma unroll
-        for (uint32_t i = 0; i < 4 * S::HALVES; ++i) {
+        auto chunk_of = [&](uint32_t i) -> uint4* {
           const uint32_t q = i + (row >> 6) * 4 * S::HALVES;
-          uint4* const at = (uint4*)(v + (q >> 3) * KV_HALF + (((q & 7) ^ (row & 7)) << 4));
-          if (any) {
-            const uint4 u = *at;
-            test = __hfma2(*(const __nv_bfloat162*)&u.x, zero, test);
-            test = __hfma2(*(const __nv_bfloat162*)&u.y, zero, test);
-            test = __hfma2(*(const __nv_bfloat162*)&u.z, zero, test);
-            test = __hfma2(*(const __nv_bfloat162*)&u.w, zero, test);
-          } else {
-            *at = make_uint4(0, 0, 0, 0);
-          }
+          return (uint4*)(v + (q >> 3) * KV_HALF + (((q & 7) ^ (row & 7)) << 4));
+        };
+        const __nv_bfloat162 zero = __float2bfloat162_rn(0.f);
+        __nv_bfloat162 test = zero, test2 = zero;
+#pragma unroll 2
+        for (uint32_t i = 0; i < 4 * S::HALVES; ++i) {
+          const uint4 u = *chunk_of(i);
+          test = __hfma2(*(const __nv_bfloat162*)&u.x, zero, test);
+          test2 = __hfma2(*(const __nv_bfloat162*)&u.y, zero, test2);
+          test = __hfma2(*(const __nv_bfloat162*)&u.z, zero, test);
+          test2 = __hfma2(*(const __nv_bfloat162*)&u.w, zero, test2);
         }
-        if (__isnan(__low2float(test)) || __isnan(__high2float(test))) dirty[3 * x + k % 3] = 1;
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        test = __hadd2(test, test2);
+        const bool wild = __isnan(__low2float(test)) || __isnan(__high2float(test));
+        if (__any_sync(0xffffffffu, wild)) {
+          const int at = key0 + vrow;
+          if (wild) {
+            if (at < w[B_END] && (at >= w[B_LOW] || at < a.sinks) && !((missing >> (vrow >> copy_log)) & 1u)) {
+              dirty[4 * x + (k & 3)] = 1;
+            } else {
+#pragma unroll 1
+              for (uint32_t i = 0; i < 4 * S::HALVES; ++i) *chunk_of(i) = make_uint4(0, 0, 0, 0);
+            }
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
       }
       auto hide = [&](float* s, uint32_t bits) {
 #pragma unroll
@@ -625,10 +639,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
 #pragma unroll
       for (int q = 0; q < DP / 32; ++q) {
         float o[32];
-        if (nx > 0) {
-          tmem_load32(t_o + 32 * q, o);
-          tmem_landed(o);
-        }
+        if (nx > 0) { tmem_load32(t_o + 32 * q, o); tmem_landed(o); }
 #pragma unroll
         for (int i = 0; i < 32; ++i) o[i] = nx > 0 && l != 0.f ? o[i] * inv : 0.f;
         if (tok >= n_rows) continue;
@@ -657,15 +668,11 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       }
       tc_fence_before();  // (the next block's first product into O_x comes after this row's next arrival)
     }
-    // a value that some of these rows see and others do not was not finite: the rows again, one warp each.  The threads of
-    // the row tile meet first, so that all have seen all tiles and stored their rows.
+    // A value that some of these rows see and others do not was not finite: this warp's rows again.  (Whoever found one
+    // said so before its weights of that tile were handed over, without which the sums would not be done.)
     __syncwarp();
-    if (ok) {
-      if (lane == 0) mbar_arrive(bar_g + 8 * x);
-      ok = __all_sync(0xffffffffu, mbar_wait_flat(bar_g + 8 * x, k & 1, abort_flag));
-    }
-    if (ok && dirty[3 * x + k % 3])
-      for (int r = warp & 3; r < n_rows * a.group; r += 4)
+    if (ok && dirty[4 * x + (k & 3)])
+      for (int r = (warp & 3) * 32; r < min((warp & 3) * 32 + 32, n_rows * a.group); ++r)
         attend_row<__nv_bfloat16>(a, w[B_REQUEST], position() + r / a.group, w[B_ROW0] + x * tokens + r / a.group, w[B_KVH] * a.group + r % a.group);
     g += nx;
     seen_tiles += max(w[B_N0], w[B_N1]);

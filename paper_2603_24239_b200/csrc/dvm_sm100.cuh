@@ -61,9 +61,19 @@ static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity
                                                    unsigned long long limit_ns, bool heed_abort) {
   return mbar_spin(bar, parity, abort_flag, limit_ns, heed_abort);
 }
-// The same without a call: for kernels that deal out registers by role (setmaxnreg), where a callee has no count of its own.
+// The same without a call, for kernels that deal out registers by role (setmaxnreg), where a callee has no count of its own;
+// and with the clock and the flag looked at every 16th time only: a read of the clock takes longer than most of these waits.
 __device__ __forceinline__ bool mbar_wait_flat(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag) {
-  return mbar_try(bar, parity) || mbar_spin(bar, parity, abort_flag, WAIT_NS, true);
+  unsigned long long t0 = 0;
+  for (uint32_t spin = 0; spin < WAIT_SPINS; ++spin) {
+    if (mbar_try(bar, parity)) return true;
+    if ((spin & 15) != 15) continue;
+    if (*abort_flag) return false;
+    if (t0 == 0) t0 = gtimer();
+    else if (gtimer() - t0 > WAIT_NS) break;
+  }
+  *abort_flag = 1;
+  return false;
 }
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag) {
   if (mbar_try(bar, parity)) return true;
