@@ -44,14 +44,14 @@ using namespace sm100;
 constexpr int PT = 128;                  // rows of a row tile
 constexpr int KT = 64;                   // tokens of a cache tile
 // Registers are dealt out by role: 384 threads are launched with 168 each, 64,512 in all; the two warpgroups that hold rows of
-// scores go up to ROW_REGS, the third down to OTHER_REGS: 256 x 216 + 128 x 72 = 64,512.
+// scores go up to ROW_REGS, the third down to OTHER_REGS: 256 x 224 + 128 x 56 = 64,512.
 constexpr int PROMPT_THREADS = 384;
-constexpr int ROW_REGS = 216, OTHER_REGS = 72;
+constexpr int ROW_REGS = 224, OTHER_REGS = 56;
 static_assert(256 * ROW_REGS + 128 * OTHER_REGS <= PROMPT_THREADS * 168, "an increase draws on the registers of the launch");
 constexpr uint32_t Q_HALF = PT * 128;    // 64 elements of the rows: 16 KB
 constexpr uint32_t KV_HALF = KT * 128;   // 64 elements of the tokens: 8 KB
 constexpr int HOLES = 16;                // tiles whose missing pages are remembered: more than the ring is deep
-constexpr int POLYNOMIAL_EVERY = 4;      // one pair of weights in so many is formed by ex2_by_polynomial
+constexpr int POLYNOMIAL_EVERY = 8;      // one pair of weights in so many is formed by ex2_by_polynomial
 constexpr float GROWTH = 8.f;            // log2 of how far weights may grow before the sums are rescaled
 
 template <int DP>  // head_dim rounded up to 64 or 128
@@ -116,21 +116,6 @@ __device__ __forceinline__ void tmem_store16(uint32_t taddr, const uint32_t* r) 
       ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
         "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
       : "memory");
-}
-// two fp32 operations in one instruction
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
 }
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -479,13 +464,13 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     if (row == 0) dirty[4 * x + ((k + 2) & 3)] = 0;  // (block k - 2 is through in every warp, or k were not here; k + 2 not before all let k go)
     // The scores of tile t + 1 are on their way while the second half of tile t's weights is formed: the lower half goes to
     // the registers that tile t's lower half has left, the upper half to those of the tile before.
-    float s_lo[32], s_next[32];
+    float s_lo[32], s_hi[2][32];
     auto scores = [&](int t) -> bool {  // tile t's scores are in tensor memory
-      const bool got = mbar_wait_flat(bar_s + 16 * x + 8 * ((g + t) & 1), ((g + t) >> 1) & 1, abort_flag);
+      const bool got = mbar_poll(bar_s + 16 * x + 8 * ((g + t) & 1), ((g + t) >> 1) & 1, abort_flag);
       tc_fence_after();
       return __all_sync(0xffffffffu, got);
     };
-    auto tile = [&](int t) -> bool {
+    auto tile = [&](int t, float* hi_now, float* hi_next) -> bool {
       const int b = (g + t) & 1;
       const uint32_t t_s = tmem + KT * (2 * x + b) + lanes, t_next = tmem + KT * (2 * x + (b ^ 1)) + lanes;
       const int key0 = (t < ns ? t : first + (t - ns)) * KT;
@@ -554,13 +539,10 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         return max_nan(max_nan(max_nan(t0, s[31]), t1), max_nan(t2, t3));
       };
       tmem_landed(s_lo);
-      tmem_landed(s_next);
-      float s_hi[32];
-#pragma unroll
-      for (int i = 0; i < 32; ++i) s_hi[i] = s_next[i];
-      if (!whole) { hide(s_lo, seen[0]); hide(s_hi, seen[1]); }
+      tmem_landed(hi_now);
+      if (!whole) { hide(s_lo, seen[0]); hide(hi_now, seen[1]); }
       // a NaN score makes the maximum NaN and with it every weight of the row, as the quotient has it
-      const float top = highest(s_hi, highest(s_lo, -INFINITY));
+      const float top = highest(hi_now, highest(s_lo, -INFINITY));
       const float m_new = max_nan(m, top);
       if (__any_sync(0xffffffffu, (m_new - m) * c > GROWTH || m_new != m_new)) {  // (from -inf: yes, unless it stays there)
         const float keep = m_new == m ? 1.f : ex2((m - m_new) * c);
@@ -568,7 +550,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         m = m_new;
         if (t > 0) {
           // PV(t - 1) is done; PV(t) waits for this tile's weights
-          if (!__all_sync(0xffffffffu, mbar_wait_flat(bar_o + 16 * x + 8 * (b ^ 1), ((g + t - 1) >> 1) & 1, abort_flag))) return false;
+          if (!__all_sync(0xffffffffu, mbar_poll(bar_o + 16 * x + 8 * (b ^ 1), ((g + t - 1) >> 1) & 1, abort_flag))) return false;
           tc_fence_after();
 #pragma unroll
           for (int q = 0; q < DP / 32; ++q) {
@@ -605,9 +587,9 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       if (early) {
         tc_fence_after();
         tmem_load32(t_next, s_lo);
-        tmem_load32(t_next + 32, s_next);
+        tmem_load32(t_next + 32, hi_next);
       }
-      weigh(s_hi, 1);
+      weigh(hi_now, 1);
       l += (l01.x + l01.y) + (l23.x + l23.y);
       tmem_st_wait();
       tc_fence_before();
@@ -616,7 +598,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       if (more && !early) {
         if (!scores(t + 1)) return false;
         tmem_load32(t_next, s_lo);
-        tmem_load32(t_next + 32, s_next);
+        tmem_load32(t_next + 32, hi_next);
       }
       return true;
     };
@@ -624,13 +606,16 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       ok = scores(0);
       if (ok) {
         tmem_load32(tmem + KT * (2 * x + (g & 1)) + lanes, s_lo);
-        tmem_load32(tmem + KT * (2 * x + (g & 1)) + lanes + 32, s_next);
+        tmem_load32(tmem + KT * (2 * x + (g & 1)) + lanes + 32, s_hi[0]);
       }
-      for (int t = 0; ok && t < nx; ++t) ok = tile(t);
+      for (int t = 0; ok && t < nx; t += 2) {
+        ok = tile(t, s_hi[0], s_hi[1]);
+        if (ok && t + 1 < nx) ok = tile(t + 1, s_hi[1], s_hi[0]);
+      }
     }
     const int last = g + nx - 1;
     if (ok && nx > 0) {
-      ok = __all_sync(0xffffffffu, mbar_wait_flat(bar_o + 16 * x + 8 * (last & 1), (last >> 1) & 1, abort_flag));
+      ok = __all_sync(0xffffffffu, mbar_poll(bar_o + 16 * x + 8 * (last & 1), (last >> 1) & 1, abort_flag));
       tc_fence_after();
     }
     if (ok && n_rows > 0) {

@@ -5,20 +5,27 @@
 // [4 l, 4 l + 4) and [R / 2 + 4 l, R / 2 + 4 l + 4) of a head whose halves are paired, [8 l, 8 l + 8) where neighbours
 // are, and every lane from R / 8 on holds [8 l, 8 l + 8), which stay.  Rotation then takes no exchange between lanes, and
 // either way a lane needs cos and sin of the pairs [4 l, 4 l + 4): 16 bytes each.  Only the mean of squares crosses lanes.
-// A CTA works on the heads of one token, so position, slot and angles are read once per thread and serve all its heads;
-// the heads' loads go out before anything waits for the position.  Everything between load and store is fp32; the store
-// rounds once.
+// A CTA keeps the same heads for all tokens it takes -- all of them, or a part where there are more than its groups can
+// have in flight -- so what a thread reads and writes is found once and moves by a stride; position, slot and angles are
+// read once per thread and token, and while one token is computed the heads and angles of the next are on their way, and
+// the position and slot of the one after it.  Everything between load and store is fp32 (two elements to an
+// instruction); the store rounds once.  With the head's place worked out anew for every token, the same kernel took 744
+// instructions per warp and token and was bound by them: 80 us for 8192 tokens of 32 + 8 + 8 heads of 128.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include "dvm_launch.h"
 #include "dvm_serving.h"
+#include "dvm_sm100.cuh"
 
 namespace dvm {
 namespace rotary {
 
+using namespace sm100;
+
 constexpr int THREADS = 256;
-constexpr int UNROLL = 3;  // heads a group loads before it works on the first
+// heads that a group has in flight: 16 bytes of registers each in bf16, 32 in fp32
+template <class T> constexpr int UNROLL = sizeof(T) == 2 ? 3 : 2;
 
 struct Args {
   const void *q, *k, *v, *wq, *wk;
@@ -26,11 +33,11 @@ struct Args {
   const int *positions, *slots;
   void *q_out, *k_out, *v_out;
   long long qs[2], ks[2], vs[2], qo[2], ko[3], vo[3];
-  int tokens, hq, hk, D, rot, angle_rows, n_slots, page, chunks;
+  int tokens, hq, hk, D, rot, angle_rows, n_slots, page, page_log, chunks;  // page_log: -1 where page is no power of two
   int lanes;       // lanes of a group
-  int vec_in, vec_out, vec_a;  // runs of 4 elements are aligned
+  int vec;         // runs of 4 elements are aligned in every tensor
   int norm, interleaved, paged, w_bf16;
-  float eps;
+  float eps, inv_D;
 };
 
 // Four elements as they lie in memory, and as fp32.
@@ -45,146 +52,201 @@ template <> struct Run<__nv_bfloat16> {
       w = make_uint2(h[0] | ((uint32_t)h[1] << 16), h[2] | ((uint32_t)h[3] << 16));
     }
   }
-  __device__ __forceinline__ void get(float* x) const {
-    x[0] = __uint_as_float(w.x << 16);
-    x[1] = __uint_as_float(w.x & 0xffff0000u);
-    x[2] = __uint_as_float(w.y << 16);
-    x[3] = __uint_as_float(w.y & 0xffff0000u);
+  __device__ __forceinline__ void get(float2* x) const {
+    x[0] = make_float2(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u));
+    x[1] = make_float2(__uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
   }
 };
 template <> struct Run<float> {
   float4 w;
   __device__ __forceinline__ void load(const float* p, bool vec) { w = vec ? *(const float4*)p : make_float4(p[0], p[1], p[2], p[3]); }
-  __device__ __forceinline__ void get(float* x) const { x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w; }
+  __device__ __forceinline__ void get(float2* x) const { x[0] = make_float2(w.x, w.y); x[1] = make_float2(w.z, w.w); }
 };
-__device__ __forceinline__ void store4(__nv_bfloat16* p, bool vec, const float* x) {
-  const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+__device__ __forceinline__ void store4(__nv_bfloat16* p, bool vec, const float2* x) {
+  const __nv_bfloat162 a = __float22bfloat162_rn(x[0]), b = __float22bfloat162_rn(x[1]);
   if (vec) {
     *(uint2*)p = make_uint2(*(const uint32_t*)&a, *(const uint32_t*)&b);
   } else {
     p[0] = a.x; p[1] = a.y; p[2] = b.x; p[3] = b.y;
   }
 }
-__device__ __forceinline__ void store4(float* p, bool vec, const float* x) {
+__device__ __forceinline__ void store4(float* p, bool vec, const float2* x) {
   if (vec) {
-    *(float4*)p = make_float4(x[0], x[1], x[2], x[3]);
+    *(float4*)p = make_float4(x[0].x, x[0].y, x[1].x, x[1].y);
   } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) p[i] = x[i];
+    p[0] = x[0].x; p[1] = x[0].y; p[2] = x[1].x; p[3] = x[1].y;
   }
 }
 
-template <class TI, class TO>
-__global__ void __launch_bounds__(THREADS, sizeof(TI) == 2 ? 4 : 3) dvm_rotary_kernel(const __grid_constant__ Args a) {
-  const int L = a.lanes, group = threadIdx.x / L, lane = threadIdx.x & (L - 1), groups = THREADS / L;
+// LANES: lanes of a group, VEC: runs of 4 elements are aligned everywhere; 0, false: the kernel for the other layouts.
+template <class TI, class TO, int LANES, bool VEC>
+__global__ void __launch_bounds__(THREADS, 2) dvm_rotary_kernel(const __grid_constant__ Args a) {
+  constexpr int U = UNROLL<TI>;
+  const int L = LANES ? LANES : a.lanes, group = threadIdx.x / L, lane = threadIdx.x & (L - 1), groups = THREADS / L;
   const bool live = 8 * lane < a.D, turned = 8 * lane < a.rot;
   const bool halves = turned && !a.interleaved;
   const int at0 = halves ? 4 * lane : 8 * lane, at1 = halves ? (a.rot >> 1) + 4 * lane : 8 * lane + 4;  // this lane's two runs
   const int heads = a.hq + a.hk * (a.paged ? 2 : 1);
 
-  float wq[8], wk[8];
-  if (a.norm && live) {
-    if (a.w_bf16) {
-      Run<__nv_bfloat16> r;
-      r.load((const __nv_bfloat16*)a.wq + at0, false); r.get(wq);
-      r.load((const __nv_bfloat16*)a.wq + at1, false); r.get(wq + 4);
-      r.load((const __nv_bfloat16*)a.wk + at0, false); r.get(wk);
-      r.load((const __nv_bfloat16*)a.wk + at1, false); r.get(wk + 4);
-    } else {
-      Run<float> r;
-      r.load((const float*)a.wq + at0, false); r.get(wq);
-      r.load((const float*)a.wq + at1, false); r.get(wq + 4);
-      r.load((const float*)a.wk + at0, false); r.get(wk);
-      r.load((const float*)a.wk + at1, false); r.get(wk + 4);
-    }
-  }
-  const int per = (heads + a.chunks - 1) / a.chunks;
-  const long long items = (long long)a.tokens * a.chunks;
-  for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-    const int t = (int)(item / a.chunks), chunk = (int)(item - (long long)t * a.chunks);
-    const int h_end = min(heads, (chunk + 1) * per);
-    Run<TI> x[UNROLL][2];
-    auto fetch = [&](int hb) {
+  __shared__ float4 weight[2][2][32];  // [query, key][run][lane]
+  if (a.norm && threadIdx.x < 2 * L && live) {
+    const void* w = threadIdx.x < L ? a.wq : a.wk;
+    float v[8];
 #pragma unroll
-      for (int u = 0; u < UNROLL; ++u) {
-        const int h = hb + u * groups + group;
-        if (h < h_end && live) {
-          const TI* p = h < a.hq          ? (const TI*)a.q + t * a.qs[0] + h * a.qs[1]
-                        : h < a.hq + a.hk ? (const TI*)a.k + t * a.ks[0] + (h - a.hq) * a.ks[1]
-                                          : (const TI*)a.v + t * a.vs[0] + (h - a.hq - a.hk) * a.vs[1];
-          x[u][0].load(p + at0, a.vec_in);
-          x[u][1].load(p + at1, a.vec_in);
-        }
+    for (int i = 0; i < 8; ++i) {
+      const int e = (i < 4 ? at0 : at1) + (i & 3);
+      v[i] = a.w_bf16 ? __bfloat162float(((const __nv_bfloat16*)w)[e]) : ((const float*)w)[e];
+    }
+    weight[threadIdx.x >= L][0][lane] = make_float4(v[0], v[1], v[2], v[3]);
+    weight[threadIdx.x >= L][1][lane] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+  __syncthreads();
+
+  // This thread's heads: chunk per + u groups + group, where they read and write for token 0, and what a token adds.
+  enum { QUERY, KEY, VALUE, NONE };
+  const int chunk = blockIdx.x % a.chunks, t_step = gridDim.x / a.chunks, per = (heads + a.chunks - 1) / a.chunks;
+  int t = blockIdx.x / a.chunks;
+  const TI* src[U];
+  long long add[U];
+  TO* dst[U];
+  int kind[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int i = u * groups + group, h = chunk * per + i;
+    kind[u] = i >= per || h >= heads || !live ? NONE : h < a.hq ? QUERY : h < a.hq + a.hk ? KEY : VALUE;
+    const int hh = kind[u] == QUERY ? h : kind[u] == KEY ? h - a.hq : h - a.hq - a.hk;
+    if (kind[u] == QUERY) {
+      src[u] = (const TI*)a.q + hh * a.qs[1];
+      add[u] = a.qs[0];
+      dst[u] = (TO*)a.q_out + hh * a.qo[1];
+    } else if (kind[u] == KEY) {
+      src[u] = (const TI*)a.k + hh * a.ks[1];
+      add[u] = a.ks[0];
+      dst[u] = (TO*)a.k_out + hh * (a.paged ? a.ko[2] : a.ko[1]);
+    } else {
+      src[u] = (const TI*)a.v + hh * a.vs[1];
+      add[u] = a.vs[0];
+      dst[u] = (TO*)a.v_out + hh * a.vo[2];
+    }
+    src[u] += at0 + t * add[u];
+    add[u] *= t_step;
+    dst[u] += at0;
+  }
+  const int run = at1 - at0;
+
+  struct Place { int pos, slot; };
+  auto place_of = [&](int t) -> Place {
+    Place p = {-1, -1};
+    if (t < a.tokens) {
+      p.pos = a.positions[t];
+      if (a.paged) p.slot = a.slots[t];
+    }
+    return p;
+  };
+  auto in_table = [&](Place p) -> bool { return p.pos >= 0 && p.pos < a.angle_rows; };  // (the same for the whole CTA)
+  struct Data { Run<TI> x[U][2]; Run<float> c, s; };
+  auto fetch = [&](Place p, Data& d) {  // of the token that src points to
+    if (!in_table(p)) return;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (kind[u] != NONE) {
+        d.x[u][0].load(src[u], VEC);
+        d.x[u][1].load(src[u] + run, VEC);
       }
-    };
-    fetch(chunk * per);
-    const int pos = a.positions[t];
-    if (pos < 0 || pos >= a.angle_rows) continue;  // (the whole CTA: t is the same for all its threads)
+    if (turned) {  // cos and sin of the pairs [4 lane, 4 lane + 4)
+      const float* row = a.angles + (long long)p.pos * a.rot + 4 * lane;
+      d.c.load(row, VEC);
+      d.s.load(row + (a.rot >> 1), VEC);
+    }
+  };
+  auto compute = [&](int t, Place p, const Data& d) {
+    if (!in_table(p)) return;
     long long k_at = t * a.ko[0], v_at = 0;
     bool stored = true;
     if (a.paged) {
-      const int slot = a.slots[t];
-      stored = slot >= 0 && slot < a.n_slots;
-      const int page = slot / a.page, off = slot - page * a.page;
+      stored = p.slot >= 0 && p.slot < a.n_slots;
+      const int page = a.page_log >= 0 ? p.slot >> a.page_log : p.slot / a.page, off = p.slot - page * a.page;
       k_at = page * a.ko[0] + off * a.ko[1];
       v_at = page * a.vo[0] + off * a.vo[1];
     }
-    float c[4], s[4];  // of the pairs [4 lane, 4 lane + 4)
-    if (turned) {
-      const float* row = a.angles + (long long)pos * a.rot + 4 * lane;
-      Run<float> r;
-      r.load(row, a.vec_a); r.get(c);
-      r.load(row + (a.rot >> 1), a.vec_a); r.get(s);
-    }
-    for (int hb = chunk * per; hb < h_end; hb += groups * UNROLL) {
-      if (hb != chunk * per) fetch(hb);
+    const long long q_at = t * a.qo[0];
+    float2 c[2], s[2], ns[2];
+    d.c.get(c);
+    d.s.get(s);
 #pragma unroll
-      for (int u = 0; u < UNROLL; ++u) {
-        if (hb + u * groups >= h_end) break;  // (the same for the whole CTA: the shuffles below stay converged)
-        const int h = hb + u * groups + group;
-        const bool mine = h < h_end && live, is_q = h < a.hq, is_v = h >= a.hq + a.hk;
-        float y[8] = {};
-        if (mine) {
-          x[u][0].get(y);
-          x[u][1].get(y + 4);
-        }
-        if (a.norm) {
-          float sum = 0.f;
+    for (int i = 0; i < 2; ++i) ns[i] = make_float2(-s[i].x, -s[i].y);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) sum = fmaf(y[i], y[i], sum);
-          for (int d = L >> 1; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-          if (!is_v) {
-            const float r = rsqrtf(sum / (float)a.D + a.eps);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = y[i] * r * (is_q ? wq[i] : wk[i]);
-          }
-        }
-        if (!mine || (!is_q && !stored)) continue;
-        if (turned && !is_v) {
-          if (a.interleaved) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float p = y[2 * i], q = y[2 * i + 1];
-              y[2 * i] = p * c[i] - q * s[i];
-              y[2 * i + 1] = q * c[i] + p * s[i];
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float p = y[i], q = y[4 + i];
-              y[i] = p * c[i] - q * s[i];
-              y[4 + i] = q * c[i] + p * s[i];
-            }
-          }
-        }
-        TO* out = is_q   ? (TO*)a.q_out + t * a.qo[0] + h * a.qo[1]
-                  : is_v ? (TO*)a.v_out + v_at + (h - a.hq - a.hk) * a.vo[2]
-                         : (TO*)a.k_out + k_at + (h - a.hq) * (a.paged ? a.ko[2] : a.ko[1]);
-        store4(out + at0, a.vec_out, y);
-        store4(out + at1, a.vec_out, y + 4);
+    for (int u = 0; u < U; ++u) {
+      if (u * groups >= per) break;  // (the same for the whole CTA: the shuffles below stay converged)
+      float2 y[4] = {};
+      if (kind[u] != NONE) {
+        d.x[u][0].get(y);
+        d.x[u][1].get(y + 2);
       }
+      if (a.norm) {
+        float2 sq = mul2(y[0], y[0]);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) sq = fma2(y[i], y[i], sq);
+        float sum = sq.x + sq.y;
+        if (LANES) {
+#pragma unroll
+          for (int e = LANES >> 1; e > 0; e >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, e);
+        } else {
+          for (int e = L >> 1; e > 0; e >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, e);
+        }
+        if (kind[u] <= KEY) {
+          const float r = rsqrtf(sum * a.inv_D + a.eps);
+          const float4 w0 = weight[kind[u]][0][lane], w1 = weight[kind[u]][1][lane];
+          const float2 w[4] = {make_float2(w0.x, w0.y), make_float2(w0.z, w0.w), make_float2(w1.x, w1.y), make_float2(w1.z, w1.w)};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = mul2(mul2(y[i], make_float2(r, r)), w[i]);
+        }
+      }
+      if (kind[u] == NONE || (kind[u] != QUERY && !stored)) continue;
+      if (turned && kind[u] != VALUE) {
+        if (a.interleaved) {  // y[i] is pair i
+          const float cc[4] = {c[0].x, c[0].y, c[1].x, c[1].y}, ss[4] = {s[0].x, s[0].y, s[1].x, s[1].y};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = fma2(make_float2(-y[i].y, y[i].x), make_float2(ss[i], ss[i]), mul2(y[i], make_float2(cc[i], cc[i])));
+        } else {              // y[i] and y[2 + i] are the halves of two pairs
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float2 p0 = y[i], p1 = y[2 + i];
+            y[i] = fma2(p1, ns[i], mul2(p0, c[i]));
+            y[2 + i] = fma2(p0, s[i], mul2(p1, c[i]));
+          }
+        }
+      }
+      TO* const out = dst[u] + (kind[u] == QUERY ? q_at : kind[u] == KEY ? k_at : v_at);
+      store4(out, VEC, y);
+      store4(out + run, VEC, y + 2);
+    }
+  };
+  Place now = place_of(t), next = place_of(t + t_step);
+  Data d[2];
+  fetch(now, d[0]);
+  while (t < a.tokens) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      if (t >= a.tokens) break;
+      const Place later = place_of(t + 2 * t_step);
+#pragma unroll
+      for (int u = 0; u < U; ++u) src[u] += add[u];
+      fetch(next, d[b ^ 1]);
+      compute(t, now, d[b]);
+      now = next;
+      next = later;
+      t += t_step;
     }
   }
+}
+
+template <class TI, class TO>
+void launch(const Args& a, int grid, cudaStream_t stream) {
+  if (!a.vec) dvm_rotary_kernel<TI, TO, 0, false><<<grid, THREADS, 0, stream>>>(a);
+  else if (a.lanes == 8) dvm_rotary_kernel<TI, TO, 8, true><<<grid, THREADS, 0, stream>>>(a);
+  else if (a.lanes == 16) dvm_rotary_kernel<TI, TO, 16, true><<<grid, THREADS, 0, stream>>>(a);
+  else dvm_rotary_kernel<TI, TO, 32, true><<<grid, THREADS, 0, stream>>>(a);
 }
 
 }  // namespace rotary
@@ -210,25 +272,29 @@ int dvm_launch_rotary(const dvm_rotary_desc& d, void* const* t, cudaStream_t str
   };
   for (int i = 0; i < 2; ++i) { a.qs[i] = d.q_stride[i]; a.ks[i] = d.k_stride[i]; a.vs[i] = d.v_stride[i]; a.qo[i] = d.q_out_stride[i]; a.ko[i] = d.k_out_stride[i]; }
   if (d.paged) for (int i = 0; i < 3; ++i) { a.ko[i] = d.k_cache_stride[i]; a.vo[i] = d.v_cache_stride[i]; }
-  a.vec_in = aligned(a.q, a.qs, 2, ei) && aligned(a.k, a.ks, 2, ei) && (!d.paged || aligned(a.v, a.vs, 2, ei));
-  a.vec_out = aligned(a.q_out, a.qo, 2, eo) && aligned(a.k_out, a.ko, d.paged ? 3 : 2, eo) && (!d.paged || aligned(a.v_out, a.vo, 3, eo));
-  a.vec_a = ((uintptr_t)a.angles & 15) == 0;
+  a.vec = aligned(a.q, a.qs, 2, ei) && aligned(a.k, a.ks, 2, ei) && aligned(a.q_out, a.qo, 2, eo) && aligned(a.k_out, a.ko, d.paged ? 3 : 2, eo) &&
+          ((uintptr_t)a.angles & 15) == 0 && (!d.paged || (aligned(a.v, a.vs, 2, ei) && aligned(a.v_out, a.vo, 3, eo)));
   a.tokens = (int)d.tokens; a.hq = (int)d.q_heads; a.hk = (int)d.kv_heads; a.D = (int)d.head_dim; a.rot = (int)d.rotary_dim;
   a.angle_rows = (int)d.angle_rows; a.n_slots = d.paged ? (int)(d.pages * d.page_size) : 0; a.page = d.paged ? (int)d.page_size : 1;
   a.norm = d.norm; a.interleaved = d.interleaved; a.paged = d.paged; a.w_bf16 = d.weight_dtype == DVM_BF16; a.eps = d.eps;
   a.lanes = d.head_dim <= 64 ? 8 : d.head_dim <= 128 ? 16 : 32;
-  // few tokens: their heads are spread over CTAs until every SM has some
-  const int heads = a.hq + a.hk * (d.paged ? 2 : 1), groups = THREADS / a.lanes, most = (heads + groups - 1) / groups;
-  const int64_t want = 4 * (int64_t)dev.sm_count / d.tokens;
-  a.chunks = (int)(want < 1 ? 1 : want < most ? want : most);
-  const int64_t items = d.tokens * a.chunks, cap = 64 * (int64_t)dev.sm_count;
-  const int grid = (int)(items < cap ? items : cap);
+  a.inv_D = 1.f / (float)d.head_dim;
+  a.page_log = -1;
+  for (int i = 0; i < 31; ++i) if (a.page == 1 << i) a.page_log = i;
+  // a CTA takes as many heads of a token as its groups have in flight; of few tokens, fewer, until every SM has some
+  const int heads = a.hq + a.hk * (d.paged ? 2 : 1), groups = THREADS / a.lanes;
+  const int in_flight = groups * (d.dtype == DVM_BF16 ? UNROLL<__nv_bfloat16> : UNROLL<float>);
+  const int least = (heads + in_flight - 1) / in_flight, most = (heads + groups - 1) / groups;
+  const int64_t want = 2 * (int64_t)dev.sm_count / d.tokens;
+  a.chunks = (int)(want < least ? least : want < most ? want : most);
+  const int64_t cap = 2 * (int64_t)dev.sm_count / a.chunks;  // tokens at a time
+  const int grid = (int)(d.tokens < cap ? d.tokens : cap < 1 ? 1 : cap) * a.chunks;
   if (d.dtype == DVM_BF16) {
-    if (d.out_dtype == DVM_BF16) dvm_rotary_kernel<__nv_bfloat16, __nv_bfloat16><<<grid, THREADS, 0, stream>>>(a);
-    else dvm_rotary_kernel<__nv_bfloat16, float><<<grid, THREADS, 0, stream>>>(a);
+    if (d.out_dtype == DVM_BF16) launch<__nv_bfloat16, __nv_bfloat16>(a, grid, stream);
+    else launch<__nv_bfloat16, float>(a, grid, stream);
   } else {
-    if (d.out_dtype == DVM_BF16) dvm_rotary_kernel<float, __nv_bfloat16><<<grid, THREADS, 0, stream>>>(a);
-    else dvm_rotary_kernel<float, float><<<grid, THREADS, 0, stream>>>(a);
+    if (d.out_dtype == DVM_BF16) launch<float, __nv_bfloat16>(a, grid, stream);
+    else launch<float, float>(a, grid, stream);
   }
   DVM_CUDA(cudaGetLastError());
   dvm_count_launch();

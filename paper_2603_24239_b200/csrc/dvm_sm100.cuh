@@ -11,6 +11,28 @@ constexpr unsigned long long WAIT_NS = 2000000000ull;   // limit of one wait: 2 
 constexpr unsigned long long DRAIN_NS = 200000000ull;   // limit of a wait for work in flight after an abort
 constexpr uint32_t WAIT_SPINS = 1u << 27;
 
+// two fp32 operations in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
@@ -68,6 +90,20 @@ __device__ __forceinline__ bool mbar_wait_flat(uint32_t bar, uint32_t parity, vo
   for (uint32_t spin = 0; spin < WAIT_SPINS; ++spin) {
     if (mbar_try(bar, parity)) return true;
     if ((spin & 15) != 15) continue;
+    if (*abort_flag) return false;
+    if (t0 == 0) t0 = gtimer();
+    else if (gtimer() - t0 > WAIT_NS) break;
+  }
+  *abort_flag = 1;
+  return false;
+}
+// The same for waits that are short and on the critical path: the first polls do not sleep (a warp that sleeps takes
+// hundreds of cycles to be back).
+__device__ __forceinline__ bool mbar_poll(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag) {
+  unsigned long long t0 = 0;
+  for (uint32_t spin = 0; spin < WAIT_SPINS; ++spin) {
+    if (spin < 64 ? mbar_test(bar, parity) : mbar_try(bar, parity)) return true;
+    if ((spin & 63) != 63) continue;
     if (*abort_flag) return false;
     if (t0 == 0) t0 = gtimer();
     else if (gtimer() - t0 > WAIT_NS) break;
