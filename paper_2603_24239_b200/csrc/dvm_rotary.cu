@@ -10,7 +10,9 @@
 // read once per thread and token, and while one token is computed the heads and angles of the next are on their way, and
 // the position and slot of the one after it.  Everything between load and store is fp32 (two elements to an
 // instruction); the store rounds once.  With the head's place worked out anew for every token, the same kernel took 744
-// instructions per warp and token and was bound by them: 80 us for 8192 tokens of 32 + 8 + 8 heads of 128.
+// instructions per warp and token and was bound by them: 80 us for 8192 tokens of 32 + 8 + 8 heads of 128.  With the next
+// token's data in registers (one token ahead, two CTAs per SM) it was bound by what is in flight: 50 us.  Now each
+// thread copies its own runs into shared memory (cp.async, DEPTH tokens ahead) and reads them from there.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -23,9 +25,11 @@ namespace rotary {
 
 using namespace sm100;
 
-constexpr int THREADS = 256;
-// heads that a group has in flight: 16 bytes of registers each in bf16, 32 in fp32
-template <class T> constexpr int UNROLL = sizeof(T) == 2 ? 3 : 2;
+constexpr int THREADS = 256;   // at most
+constexpr int DEPTH = 2;       // tokens on their way
+constexpr int UNROLL = 3;      // heads of a group
+// bytes of a thread: per token on its way two runs of each head, and cos and sin
+template <class T> constexpr int BYTES = DEPTH * (UNROLL * 2 * 4 * (int)sizeof(T) + 32);
 
 struct Args {
   const void *q, *k, *v, *wq, *wk;
@@ -52,6 +56,9 @@ template <> struct Run<__nv_bfloat16> {
       w = make_uint2(h[0] | ((uint32_t)h[1] << 16), h[2] | ((uint32_t)h[3] << 16));
     }
   }
+  static __device__ __forceinline__ void copy(uint32_t dst, const __nv_bfloat16* p) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(p) : "memory");
+  }
   __device__ __forceinline__ void get(float2* x) const {
     x[0] = make_float2(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u));
     x[1] = make_float2(__uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
@@ -60,6 +67,9 @@ template <> struct Run<__nv_bfloat16> {
 template <> struct Run<float> {
   float4 w;
   __device__ __forceinline__ void load(const float* p, bool vec) { w = vec ? *(const float4*)p : make_float4(p[0], p[1], p[2], p[3]); }
+  static __device__ __forceinline__ void copy(uint32_t dst, const float* p) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(p) : "memory");
+  }
   __device__ __forceinline__ void get(float2* x) const { x[0] = make_float2(w.x, w.y); x[1] = make_float2(w.z, w.w); }
 };
 __device__ __forceinline__ void store4(__nv_bfloat16* p, bool vec, const float2* x) {
@@ -80,32 +90,20 @@ __device__ __forceinline__ void store4(float* p, bool vec, const float2* x) {
 
 // LANES: lanes of a group, VEC: runs of 4 elements are aligned everywhere; 0, false: the kernel for the other layouts.
 template <class TI, class TO, int LANES, bool VEC>
-__global__ void __launch_bounds__(THREADS, 2) dvm_rotary_kernel(const __grid_constant__ Args a) {
-  constexpr int U = UNROLL<TI>;
-  const int L = LANES ? LANES : a.lanes, group = threadIdx.x / L, lane = threadIdx.x & (L - 1), groups = THREADS / L;
+__global__ void __launch_bounds__(THREADS, VEC ? 3 : 2) dvm_rotary_kernel(const __grid_constant__ Args a) {
+  constexpr int U = UNROLL;
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int L = LANES ? LANES : a.lanes, group = threadIdx.x / L, lane = threadIdx.x & (L - 1), groups = blockDim.x / L;
   const bool live = 8 * lane < a.D, turned = 8 * lane < a.rot;
   const bool halves = turned && !a.interleaved;
   const int at0 = halves ? 4 * lane : 8 * lane, at1 = halves ? (a.rot >> 1) + 4 * lane : 8 * lane + 4;  // this lane's two runs
   const int heads = a.hq + a.hk * (a.paged ? 2 : 1);
 
   __shared__ float4 weight[2][2][32];  // [query, key][run][lane]
-  if (a.norm && threadIdx.x < 2 * L && live) {
-    const void* w = threadIdx.x < L ? a.wq : a.wk;
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int e = (i < 4 ? at0 : at1) + (i & 3);
-      v[i] = a.w_bf16 ? __bfloat162float(((const __nv_bfloat16*)w)[e]) : ((const float*)w)[e];
-    }
-    weight[threadIdx.x >= L][0][lane] = make_float4(v[0], v[1], v[2], v[3]);
-    weight[threadIdx.x >= L][1][lane] = make_float4(v[4], v[5], v[6], v[7]);
-  }
-  __syncthreads();
-
   // This thread's heads: chunk per + u groups + group, where they read and write for token 0, and what a token adds.
   enum { QUERY, KEY, VALUE, NONE };
-  const int chunk = blockIdx.x % a.chunks, t_step = gridDim.x / a.chunks, per = (heads + a.chunks - 1) / a.chunks;
-  int t = blockIdx.x / a.chunks;
+  const int chunk = blockIdx.x % a.chunks, step = gridDim.x / a.chunks, per = (heads + a.chunks - 1) / a.chunks;
+  long long t = blockIdx.x / a.chunks;
   const TI* src[U];
   long long add[U];
   TO* dst[U];
@@ -129,13 +127,13 @@ __global__ void __launch_bounds__(THREADS, 2) dvm_rotary_kernel(const __grid_con
       dst[u] = (TO*)a.v_out + hh * a.vo[2];
     }
     src[u] += at0 + t * add[u];
-    add[u] *= t_step;
+    add[u] *= step;
     dst[u] += at0;
   }
   const int run = at1 - at0;
 
   struct Place { int pos, slot; };
-  auto place_of = [&](int t) -> Place {
+  auto place_of = [&](long long t) -> Place {
     Place p = {-1, -1};
     if (t < a.tokens) {
       p.pos = a.positions[t];
@@ -144,35 +142,65 @@ __global__ void __launch_bounds__(THREADS, 2) dvm_rotary_kernel(const __grid_con
     return p;
   };
   auto in_table = [&](Place p) -> bool { return p.pos >= 0 && p.pos < a.angle_rows; };  // (the same for the whole CTA)
-  struct Data { Run<TI> x[U][2]; Run<float> c, s; };
-  auto fetch = [&](Place p, Data& d) {  // of the token that src points to
-    if (!in_table(p)) return;
+  // Token i of this CTA goes through place i mod DEPTH of the thread's shared memory: 2 U runs, cos, sin.
+  constexpr uint32_t RUN = 4 * sizeof(TI);
+  const uint32_t place_bytes = blockDim.x * (2 * U * RUN + 32), mine = threadIdx.x * RUN, mine_cs = blockDim.x * 2 * U * RUN + threadIdx.x * 16;
+  const uint32_t base = smem_u32(smem);
+  auto fetch = [&](uint32_t place, long long t, Place p) {  // of the token that src points to
+    if (VEC && t < a.tokens) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (kind[u] != NONE) {
-        d.x[u][0].load(src[u], VEC);
-        d.x[u][1].load(src[u] + run, VEC);
+      for (int u = 0; u < U; ++u)
+        if (kind[u] != NONE) {
+          Run<TI>::copy(base + place + mine + (2 * u) * blockDim.x * RUN, src[u]);
+          Run<TI>::copy(base + place + mine + (2 * u + 1) * blockDim.x * RUN, src[u] + run);
+        }
+      if (turned && in_table(p)) {  // cos and sin of the pairs [4 lane, 4 lane + 4)
+        const float* row = a.angles + (long long)p.pos * a.rot + 4 * lane;
+        Run<float>::copy(base + place + mine_cs, row);
+        Run<float>::copy(base + place + mine_cs + blockDim.x * 16, row + (a.rot >> 1));
       }
-    if (turned) {  // cos and sin of the pairs [4 lane, 4 lane + 4)
-      const float* row = a.angles + (long long)p.pos * a.rot + 4 * lane;
-      d.c.load(row, VEC);
-      d.s.load(row + (a.rot >> 1), VEC);
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  auto compute = [&](int t, Place p, const Data& d) {
+  auto compute = [&](uint32_t place, long long t, Place p) {
     if (!in_table(p)) return;
-    long long k_at = t * a.ko[0], v_at = 0;
+    const uint8_t* const here = smem + place;
+    Run<TI> x[U][2];
+    Run<float> dc, ds;
+    if (VEC) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) x[u][i] = *(const Run<TI>*)(here + mine + (2 * u + i) * blockDim.x * RUN);
+      dc = *(const Run<float>*)(here + mine_cs);
+      ds = *(const Run<float>*)(here + mine_cs + blockDim.x * 16);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (kind[u] != NONE) {
+          x[u][0].load(src[u], false);
+          x[u][1].load(src[u] + run, false);
+        }
+      if (turned) {
+        const float* row = a.angles + (long long)p.pos * a.rot + 4 * lane;
+        dc.load(row, false);
+        ds.load(row + (a.rot >> 1), false);
+      }
+    }
+    const long long q_at = t * a.qo[0];
+    long long k_at = 0, v_at = 0;
     bool stored = true;
     if (a.paged) {
       stored = p.slot >= 0 && p.slot < a.n_slots;
       const int page = a.page_log >= 0 ? p.slot >> a.page_log : p.slot / a.page, off = p.slot - page * a.page;
       k_at = page * a.ko[0] + off * a.ko[1];
       v_at = page * a.vo[0] + off * a.vo[1];
+    } else {
+      k_at = t * a.ko[0];
     }
-    const long long q_at = t * a.qo[0];
     float2 c[2], s[2], ns[2];
-    d.c.get(c);
-    d.s.get(s);
+    dc.get(c);
+    ds.get(s);
 #pragma unroll
     for (int i = 0; i < 2; ++i) ns[i] = make_float2(-s[i].x, -s[i].y);
 #pragma unroll
@@ -180,8 +208,8 @@ __global__ void __launch_bounds__(THREADS, 2) dvm_rotary_kernel(const __grid_con
       if (u * groups >= per) break;  // (the same for the whole CTA: the shuffles below stay converged)
       float2 y[4] = {};
       if (kind[u] != NONE) {
-        d.x[u][0].get(y);
-        d.x[u][1].get(y + 2);
+        x[u][0].get(y);
+        x[u][1].get(y + 2);
       }
       if (a.norm) {
         float2 sq = mul2(y[0], y[0]);
@@ -222,31 +250,59 @@ __global__ void __launch_bounds__(THREADS, 2) dvm_rotary_kernel(const __grid_con
       store4(out + run, VEC, y + 2);
     }
   };
-  Place now = place_of(t), next = place_of(t + t_step);
-  Data d[2];
-  fetch(now, d[0]);
-  while (t < a.tokens) {
+  // (with VEC src runs DEPTH tokens ahead of t)
+  Place p[DEPTH + 1];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      if (t >= a.tokens) break;
-      const Place later = place_of(t + 2 * t_step);
+  for (int i = 0; i <= DEPTH; ++i) p[i] = place_of(t + i * step);
+  auto advance = [&]() {
 #pragma unroll
-      for (int u = 0; u < U; ++u) src[u] += add[u];
-      fetch(next, d[b ^ 1]);
-      compute(t, now, d[b]);
-      now = next;
-      next = later;
-      t += t_step;
+    for (int u = 0; u < U; ++u) src[u] += add[u];
+  };
+  if (VEC) {
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) {
+      fetch(i * place_bytes, t + i * step, p[i]);
+      advance();
     }
   }
+  // (the weights last: nothing but the first token's sums waits for them)
+  for (int i = threadIdx.x; a.norm && i < 2 * L && live; i += blockDim.x) {  // (blockDim is a multiple of L: i has this lane)
+    const void* w = i < L ? a.wq : a.wk;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int e = (j < 4 ? at0 : at1) + (j & 3);
+      v[j] = a.w_bf16 ? __bfloat162float(((const __nv_bfloat16*)w)[e]) : ((const float*)w)[e];
+    }
+    weight[i >= L][0][lane] = make_float4(v[0], v[1], v[2], v[3]);
+    weight[i >= L][1][lane] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+  __syncthreads();
+  for (uint32_t place = 0; t < a.tokens; t += step) {
+    const Place later = place_of(t + (DEPTH + 1) * step);
+    if (VEC) asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
+    compute(place, t, p[0]);
+    if (VEC) fetch(place, t + DEPTH * step, p[DEPTH]);
+    advance();
+    place = place == (DEPTH - 1) * place_bytes ? 0 : place + place_bytes;
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) p[i] = p[i + 1];
+    p[DEPTH] = later;
+  }
+  if (VEC) asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
 template <class TI, class TO>
-void launch(const Args& a, int grid, cudaStream_t stream) {
-  if (!a.vec) dvm_rotary_kernel<TI, TO, 0, false><<<grid, THREADS, 0, stream>>>(a);
-  else if (a.lanes == 8) dvm_rotary_kernel<TI, TO, 8, true><<<grid, THREADS, 0, stream>>>(a);
-  else if (a.lanes == 16) dvm_rotary_kernel<TI, TO, 16, true><<<grid, THREADS, 0, stream>>>(a);
-  else dvm_rotary_kernel<TI, TO, 32, true><<<grid, THREADS, 0, stream>>>(a);
+int launch(const Args& a, int grid, int threads, cudaStream_t stream) {
+  const int bytes = threads * BYTES<TI>;
+  if (!a.vec) {
+    dvm_rotary_kernel<TI, TO, 0, false><<<grid, threads, 0, stream>>>(a);
+    return DVM_OK;
+  }
+  auto kernel = a.lanes == 8 ? dvm_rotary_kernel<TI, TO, 8, true> : a.lanes == 16 ? dvm_rotary_kernel<TI, TO, 16, true> : dvm_rotary_kernel<TI, TO, 32, true>;
+  if (bytes > 46 * 1024) DVM_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  kernel<<<grid, threads, bytes, stream>>>(a);
+  return DVM_OK;
 }
 
 }  // namespace rotary
@@ -281,21 +337,20 @@ int dvm_launch_rotary(const dvm_rotary_desc& d, void* const* t, cudaStream_t str
   a.inv_D = 1.f / (float)d.head_dim;
   a.page_log = -1;
   for (int i = 0; i < 31; ++i) if (a.page == 1 << i) a.page_log = i;
-  // a CTA takes as many heads of a token as its groups have in flight; of few tokens, fewer, until every SM has some
-  const int heads = a.hq + a.hk * (d.paged ? 2 : 1), groups = THREADS / a.lanes;
-  const int in_flight = groups * (d.dtype == DVM_BF16 ? UNROLL<__nv_bfloat16> : UNROLL<float>);
-  const int least = (heads + in_flight - 1) / in_flight, most = (heads + groups - 1) / groups;
-  const int64_t want = 2 * (int64_t)dev.sm_count / d.tokens;
+  // A CTA takes as many heads of a token as its groups have places for, with no more threads than that takes; of few tokens,
+  // fewer heads, until every SM has some.
+  const int heads = a.hq + a.hk * (d.paged ? 2 : 1);
+  int threads = 32;
+  while (threads < THREADS && threads / a.lanes * UNROLL < heads) threads *= 2;
+  const int groups = threads / a.lanes, least = (heads + groups * UNROLL - 1) / (groups * UNROLL), most = (heads + groups - 1) / groups;
+  const int64_t resident = 3 * (THREADS / threads) * (int64_t)dev.sm_count, want = resident / d.tokens;
   a.chunks = (int)(want < least ? least : want < most ? want : most);
-  const int64_t cap = 2 * (int64_t)dev.sm_count / a.chunks;  // tokens at a time
-  const int grid = (int)(d.tokens < cap ? d.tokens : cap < 1 ? 1 : cap) * a.chunks;
-  if (d.dtype == DVM_BF16) {
-    if (d.out_dtype == DVM_BF16) launch<__nv_bfloat16, __nv_bfloat16>(a, grid, stream);
-    else launch<__nv_bfloat16, float>(a, grid, stream);
-  } else {
-    if (d.out_dtype == DVM_BF16) launch<float, __nv_bfloat16>(a, grid, stream);
-    else launch<float, float>(a, grid, stream);
-  }
+  const int64_t cap = resident / a.chunks < 1 ? 1 : resident / a.chunks;  // tokens at a time
+  const int grid = (int)(d.tokens < cap ? d.tokens : cap) * a.chunks;
+  int rc;
+  if (d.dtype == DVM_BF16) rc = d.out_dtype == DVM_BF16 ? launch<__nv_bfloat16, __nv_bfloat16>(a, grid, threads, stream) : launch<__nv_bfloat16, float>(a, grid, threads, stream);
+  else rc = d.out_dtype == DVM_BF16 ? launch<float, __nv_bfloat16>(a, grid, threads, stream) : launch<float, float>(a, grid, threads, stream);
+  if (rc != DVM_OK) return rc;
   DVM_CUDA(cudaGetLastError());
   dvm_count_launch();
   return DVM_OK;
