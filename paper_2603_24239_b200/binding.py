@@ -10,6 +10,7 @@ import ctypes as C
 
 import numpy as np
 import os
+import struct
 from typing import Iterable, List, Optional, Sequence
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -403,10 +404,21 @@ def _stream(stream) -> Optional[int]:
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
+_launch = lib["dvm_launch"]   # a function object of its own: the addresses travel as packed bytes
+_launch.argtypes, _launch.restype = [_vp, _sz, C.c_char_p, _i, _vp], _i
+_PACK = [struct.Struct(f"{n}Q").pack for n in range(17)]
+
+
 def launch(code: Code, tensors: Sequence, stream=None):
     """dvm_launch: tensors are device tensors (or raw device addresses), inputs then outputs."""
-    arr = (_vp * len(tensors))(*[_ptr(t) for t in tensors])
-    _check(lib.dvm_launch(code.buf, code.size, arr, len(tensors), _stream(stream)), "dvm_launch")
+    n = len(tensors)
+    try:
+        addresses = [t.data_ptr() for t in tensors]
+    except AttributeError:
+        addresses = [_ptr(t) for t in tensors]
+    st = _launch(code.buf, code.size, _PACK[n](*addresses) if n <= 16 else struct.pack(f"{n}Q", *addresses), n, _stream(stream))
+    if st != 0:
+        raise DvmError(st, "dvm_launch")
 
 
 def tensor_extents(code: Code) -> List[int]:

@@ -110,7 +110,7 @@ int dvm_launch_attention(const dvm_attention_desc& d, void* const* t, cudaStream
   a.out_vec = stores(16) && a.D % 16 == 0 ? 2 : stores(8) ? 1 : 0;
   if (aligned && dvm_attention_tensor_cores(d)) {
     const bool single = dvm_attention_single(d);
-    st = single ? dvm_launch_attention_single(d, a, stream) : dvm_launch_attention_prompt(d, a, dev.sm_count, stream);
+    st = single ? dvm_launch_attention_single(d, a, dev.device, stream) : dvm_launch_attention_prompt(d, a, dev.device, stream);
     if (st == DVM_OK) t_last_kernel = single ? 1 : 2;
     return st;
   }

@@ -14,6 +14,5 @@ int dvm_cache_map(const dvm_attention_desc& d, const int64_t* stride, const void
 // of one group and `tokens` rows: row r of the box is token r / group, head r % group.
 int dvm_query_map(const dvm_attention_desc& d, const void* ptr, int tokens, CUtensorMap* map);
 
-// sms: CTAs that run at a time, one per SM
-int dvm_launch_attention_prompt(const dvm_attention_desc& d, const dvm::att::Args& a, int sms, cudaStream_t stream);
-int dvm_launch_attention_single(const dvm_attention_desc& d, const dvm::att::Args& a, cudaStream_t stream);
+int dvm_launch_attention_prompt(const dvm_attention_desc& d, const dvm::att::Args& a, int device, cudaStream_t stream);
+int dvm_launch_attention_single(const dvm_attention_desc& d, const dvm::att::Args& a, int device, cudaStream_t stream);

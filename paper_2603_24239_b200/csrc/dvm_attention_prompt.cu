@@ -690,8 +690,10 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
 }
 
 template <int DP>
-int launch_prompt(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Args& a, int grid, cudaStream_t stream) {
-  DVM_CUDA(cudaFuncSetAttribute(dvm_attention_prompt_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PromptSmem<DP>::BYTES));
+int launch_prompt(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const Args& a, int grid, int device, cudaStream_t stream) {
+  static std::atomic<uint64_t> allowed{0};
+  const int st = dvm_allow_smem((const void*)dvm_attention_prompt_kernel<DP>, (int)PromptSmem<DP>::BYTES, device, &allowed);
+  if (st != DVM_OK) return st;
   dvm_attention_prompt_kernel<DP><<<grid, PROMPT_THREADS, PromptSmem<DP>::BYTES, stream>>>(q, k, v, a);
   DVM_CUDA(cudaGetLastError());
   dvm_count_launch();
@@ -701,7 +703,7 @@ int launch_prompt(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap&
 }  // namespace att
 }  // namespace dvm
 
-int dvm_launch_attention_prompt(const dvm_attention_desc& d, const dvm::att::Args& a, int sms, cudaStream_t stream) {
+int dvm_launch_attention_prompt(const dvm_attention_desc& d, const dvm::att::Args& a, int device, cudaStream_t stream) {
   using namespace dvm::att;
   const int tokens = PT / a.group;
   CUtensorMap q, k, v;
@@ -713,5 +715,5 @@ int dvm_launch_attention_prompt(const dvm_attention_desc& d, const dvm::att::Arg
   const int64_t per = 2 * tokens, by_rows = (d.rows + d.requests * (per - 1)) / per, by_max = d.requests * ((d.max_q + per - 1) / per);
   const int64_t grid = (by_rows < by_max ? by_rows : by_max) * d.kv_heads;
   if (grid >= (1ll << 31)) return DVM_ERR_TOO_LARGE;
-  return a.D <= 64 ? launch_prompt<64>(q, k, v, a, (int)grid, stream) : launch_prompt<128>(q, k, v, a, (int)grid, stream);
+  return a.D <= 64 ? launch_prompt<64>(q, k, v, a, (int)grid, device, stream) : launch_prompt<128>(q, k, v, a, (int)grid, device, stream);
 }

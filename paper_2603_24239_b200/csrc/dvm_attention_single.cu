@@ -468,8 +468,10 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) dvm_attention_join_kernel(con
 }
 
 template <int DP>
-int launch_single(const CUtensorMap& k, const CUtensorMap& v, const Args& a, cudaStream_t stream) {
-  DVM_CUDA(cudaFuncSetAttribute(dvm_attention_single_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SingleSmem<DP>::BYTES));
+int launch_single(const CUtensorMap& k, const CUtensorMap& v, const Args& a, int device, cudaStream_t stream) {
+  static std::atomic<uint64_t> allowed{0};
+  const int st = dvm_allow_smem((const void*)dvm_attention_single_kernel<DP>, (int)SingleSmem<DP>::BYTES, device, &allowed);
+  if (st != DVM_OK) return st;
   dvm_attention_single_kernel<DP><<<DVM_ATT_UNITS, THREADS, SingleSmem<DP>::BYTES, stream>>>(k, v, a);
   DVM_CUDA(cudaGetLastError());
   dvm_count_launch();
@@ -479,12 +481,12 @@ int launch_single(const CUtensorMap& k, const CUtensorMap& v, const Args& a, cud
 }  // namespace att
 }  // namespace dvm
 
-int dvm_launch_attention_single(const dvm_attention_desc& d, const dvm::att::Args& a, cudaStream_t stream) {
+int dvm_launch_attention_single(const dvm_attention_desc& d, const dvm::att::Args& a, int device, cudaStream_t stream) {
   using namespace dvm::att;
   CUtensorMap k, v;
   int st = dvm_cache_map(d, d.k_stride, a.k, TILE, &k);
   if (st == DVM_OK) st = dvm_cache_map(d, d.v_stride, a.v, TILE, &v);
-  if (st == DVM_OK) st = a.D <= 64 ? launch_single<64>(k, v, a, stream) : launch_single<128>(k, v, a, stream);
+  if (st == DVM_OK) st = a.D <= 64 ? launch_single<64>(k, v, a, device, stream) : launch_single<128>(k, v, a, device, stream);
   if (st != DVM_OK) return st;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute at[1];

@@ -59,6 +59,7 @@ int dvm_device_state(DvmDeviceInfo* info) {
   }
   info->scratch = d.scratch;
   info->sm_count = d.sm_count;
+  info->device = dev;
   info->queue_slot = d.queue_slot;
   d.queue_slot = (d.queue_slot + 1) % QUEUE_SLOTS;
   return DVM_OK;

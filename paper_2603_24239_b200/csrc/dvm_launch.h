@@ -4,10 +4,16 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <atomic>
+
+#include "../../include/dvm.h"
+
 // Device status word values (read back by dvm_last_device_status).
 namespace dvm {
 enum { ST_OK = 0, ST_BAD_CODE = 1, ST_TIMEOUT = 2 };
 }
+
+void dvm_note_cuda_error(int e);
 
 // Records a failed CUDA runtime call (dvm_last_cuda_error) and returns DVM_ERR_CUDA from the caller.
 #define DVM_CUDA(call)                \
@@ -22,12 +28,20 @@ enum { ST_OK = 0, ST_BAD_CODE = 1, ST_TIMEOUT = 2 };
 struct DvmDeviceInfo {
   unsigned int* scratch;  // library-owned device words: [0] status, then work-queue counter pairs
   int sm_count;
+  int device;
   unsigned queue_slot;    // work-queue slot reserved for this launch
 };
 
 // Per-device lazy set-up (scratch allocation, occupancy) for the current device.
 int dvm_device_state(DvmDeviceInfo* info);
-void dvm_note_cuda_error(int e);
+// Lets `kernel` have `bytes` of dynamic shared memory; `done` (a bit per device) spares the driver call from the second time on.
+inline int dvm_allow_smem(const void* kernel, int bytes, int device, std::atomic<uint64_t>* done) {
+  const uint64_t bit = 1ull << (device & 63);
+  if (done->load(std::memory_order_acquire) & bit) return DVM_OK;
+  DVM_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  done->fetch_or(bit, std::memory_order_release);
+  return DVM_OK;
+}
 void dvm_count_launch();
 
 int dvm_launch_matmul(const uint32_t* code, size_t n_words, void* const* tensors, int n_tensors,
