@@ -5,7 +5,8 @@
 // Bound by memory: every visible key and value is read once, 4 D flops per kv head and token against 4 D bytes times the
 // group of query heads that share them.  So the work is cut by bytes: the tiles of DVM_ATT_TOKEN_TILE tokens of all
 // (request, kv head) pairs form one line, and each of DVM_ATT_UNITS CTAs (two per SM) takes an equal range of it, whatever
-// the lengths are -- they live on the device, so every CTA finds its range itself.  A pair that lies in one range is
+// the lengths are -- they live on the device, so every CTA finds its range itself.  (One request alone: ranges begin where a
+// head's tiles do, so that no CTA ends two pairs: 8000 tokens, 8 kv heads 16.5 -> 15.3 us.)  A pair that lies in one range is
 // finished there; the parts of one that spans several go to the workspace and a second kernel joins them (a dependent
 // launch that starts while the first one drains).  The cut depends on the lengths alone: results do not vary.
 //
@@ -61,17 +62,18 @@ struct Walk {
   Request r;
   Span p;
   long long base;   // place of the pair's first tile on the line
+  int length;       // places of a pair on the line: its tiles, or `whole` (where not 0)
   int j0, j1;
-  __device__ __forceinline__ void load(const Args& a) { r = request_at(a, request); p = span_of(a, r); }
+  __device__ __forceinline__ void load(const Args& a, int whole) { r = request_at(a, request); p = span_of(a, r); length = whole ? whole : p.count; }
   __device__ __forceinline__ void cut(long long begin, long long stop) {
     j0 = (int)max(0ll, begin - base);
     j1 = (int)min((long long)p.count, stop - base);
   }
   __device__ __forceinline__ void next(const Args& a, long long begin, long long stop) {
-    base += p.count;
+    base += length;
     if (++kvh == a.hk) {
       kvh = 0;
-      do { ++request; load(a); } while (p.count == 0);  // (only called while tiles are left: some later request has them)
+      do { ++request; load(a, 0); } while (p.count == 0);  // (only called while tiles are left: some later request has them)
     }
     cut(begin, stop);
   }
@@ -110,9 +112,10 @@ struct SingleSmem {
   static constexpr uint32_t PART = TILE * 128;                 // 64 elements of every token of a tile
   static constexpr uint32_t STAGE = 2 * HALVES * PART;         // keys, then values
   static constexpr int STAGES = DP == 128 ? 3 : 6;
-  static constexpr uint32_t SUM = STAGES * STAGE;              // [16][DP] fp32: the warps' outputs added up
-  static constexpr uint32_t STATS = SUM + 16 * DP * 4;         // [WARPS][16] maxima, [WARPS][16] sums
-  static constexpr uint32_t BARS = STATS + 2 * WARPS * 16 * 4; // full[STAGES], empty[STAGES]
+  static constexpr uint32_t SUM = STAGES * STAGE;              // [16][SUM_ROW] fp32: the warps' outputs added up
+  static constexpr int SUM_ROW = DP + 8;                       // (the rows of a quarter warp lie in different banks)
+  static constexpr uint32_t STATS = SUM + 16 * SUM_ROW * 4;    // [WARPS][16] maxima, [WARPS][16] sums, then [16] of each in all
+  static constexpr uint32_t BARS = STATS + 2 * (WARPS + 1) * 16 * 4; // full[STAGES], empty[STAGES]
   static constexpr uint32_t BAD = BARS + 16 * STAGES;          // per stage: pages that hold nothing (a bit per copy)
   static constexpr uint32_t SCAN = BAD + 8 * STAGES;
   static constexpr uint32_t BYTES = SCAN + 16 * 8 + 16 + 1024; // 1024: alignment of the swizzled stages
@@ -139,12 +142,18 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (the second kernel waits for this grid's end before it reads)
+  if (threadIdx.x == WARPS * 32) {
+    tma_prefetch(&tm_k);
+    tma_prefetch(&tm_v);
+  }
+  grid_ready();  // (the second kernel waits for this grid's end before it reads)
+  grid_wait();
 
   // ---- this CTA's range of the line: thread t counts the tiles of requests [t per, (t + 1) per) ----
   const int per = (a.n + THREADS - 1) / THREADS;
   long long mine = 0;
-  for (int i = threadIdx.x * per; i < min(a.n, (int)(threadIdx.x + 1) * per); ++i) mine += span_of(a, request_at(a, i)).count;
+  int count = 0;  // of the last one (with up to THREADS requests: the only one)
+  for (int i = threadIdx.x * per; i < min(a.n, (int)(threadIdx.x + 1) * per); ++i) mine += count = span_of(a, request_at(a, i)).count;
   long long upto = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -159,25 +168,35 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
     if (w < warp) upto += scan[w];
     total += scan[w];
   }
+  const long long count_all = total;
   total *= a.hk;
-  const long long chunk = max((total + DVM_ATT_UNITS - 1) / DVM_ATT_UNITS, (long long)MIN_TILES);
+  long long chunk = max((total + DVM_ATT_UNITS - 1) / DVM_ATT_UNITS, (long long)MIN_TILES);
+  int whole = 0;
+  if (a.n == 1 && a.hk <= DVM_ATT_UNITS) {
+    const int units = DVM_ATT_UNITS / a.hk;  // per kv head
+    chunk = max((count_all + units - 1) / units, (long long)MIN_TILES);
+    whole = (int)((count_all + chunk - 1) / chunk * chunk);
+    total = (long long)whole * a.hk;
+  }
   const long long begin = min(total, blockIdx.x * chunk), stop = min(total, begin + chunk);
   if (begin == stop) {
     if (threadIdx.x == 0 && !heads_by_pair(a)) *head_of(a, blockIdx.x) = make_int4(0, 0, 0, 0);
     return;
   }
   // the thread whose requests hold tile `begin` walks to it
-  const long long from = (upto - mine) * a.hk, to = upto * a.hk;
+  const long long from = (upto - mine) * a.hk, to = whole ? (threadIdx.x ? 0 : total) : upto * a.hk;
   if (begin >= from && begin < to) {
     long long at = from;
     for (int i = threadIdx.x * per;; ++i) {
-      const int count = span_of(a, request_at(a, i)).count;
-      const long long after = at + (long long)count * a.hk;
+      if (per > 1) count = span_of(a, request_at(a, i)).count;
+      const long long each = whole ? whole : count, after = at + each * a.hk;
       if (begin < after) {
-        const long long kvh = (begin - at) / count;
+        const long long kvh = (begin - at) / each;
         scan[8] = i;
         scan[9] = kvh;
-        scan[10] = at + kvh * count;
+        scan[10] = at + kvh * each;
+        scan[11] = chunk;
+        scan[12] = stop;
         break;
       }
       at = after;
@@ -188,7 +207,7 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
   w.request = (int)scan[8];
   w.kvh = (int)scan[9];
   w.base = scan[10];
-  w.load(a);
+  w.load(a, whole);
   w.cut(begin, stop);
 
   if (warp == WARPS) {
@@ -232,7 +251,7 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
         if (++stage == S::STAGES) { stage = 0; phase ^= 1; }
         page = page_next;
       }
-      if (!ok || w.base + w.p.count >= stop) break;
+      if (!ok || w.base + w.length >= stop) break;
       w.next(a, begin, stop);
     }
     if (!ok && lane == 0) {  // given up: the copies in flight land before the CTA ends (bounded again)
@@ -353,47 +372,61 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
       float f[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float top = -INFINITY;
+        float top = -INFINITY, all = 0.f;
 #pragma unroll
         for (int x = 0; x < WARPS; ++x) top = fmaxf(top, stats[x * 16 + g + 8 * h]);
-        f[h] = top == -INFINITY ? 1.f : exp2f((m[h] - top) * c);
-      }
-      for (int x = 0; x < WARPS; ++x) {  // in this order, always
-        if (warp == x) {
 #pragma unroll
-          for (int n = 0; n < DP / 8; ++n)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              float2* at = (float2*)(sum + (g + 8 * h) * DP + 8 * n + 2 * t4);
-              float2 v = make_float2(o[n][2 * h] * f[h], o[n][2 * h + 1] * f[h]);
-              if (x) { v.x += at->x; v.y += at->y; }
-              *at = v;
-            }
+        for (int x = 0; x < WARPS; ++x) {
+          const float e = top == -INFINITY ? 1.f : exp2f((stats[x * 16 + g + 8 * h] - top) * c);
+          all = fmaf(stats[(WARPS + x) * 16 + g + 8 * h], e, all);
+          if (x == warp) f[h] = e;
         }
+        if (warp == 0 && t4 == 0) {
+          stats[2 * WARPS * 16 + g + 8 * h] = top;
+          stats[(2 * WARPS + 1) * 16 + g + 8 * h] = all;
+        }
+      }
+      // each warp adds another quarter of the columns at a time: always in the same order
+#pragma unroll 1
+      for (int x = 0; x < WARPS; ++x) {
+#pragma unroll
+        for (int n = 0; n < DP / 8; ++n)
+          if (n / (DP / 32) == ((warp + x) & 3)) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              if (g + 8 * h < a.group) {
+                float2* at = (float2*)(sum + (g + 8 * h) * S::SUM_ROW + 8 * n + 2 * t4);
+                float2 v = make_float2(o[n][2 * h] * f[h], o[n][2 * h + 1] * f[h]);
+                if (x) { v.x += at->x; v.y += at->y; }
+                *at = v;
+              }
+          }
         consumers_sync();
       }
+      // (read again: kept in registers, they would cost the loop above its own)
+      const long long chunk = ((volatile long long*)scan)[11], stop = ((volatile long long*)scan)[12], begin = blockIdx.x * chunk;
       const bool alone = w.j0 == 0 && w.j1 == w.p.count;
       const int slot = w.j0 == 0 && w.base > begin ? 1 : 0;
       float* const part = slot_of(a, blockIdx.x, slot);
-      for (int x = threadIdx.x; x < a.group * a.D; x += WARPS * 32) {
-        const int head = x / a.D, d = x - head * a.D;
-        float top = -INFINITY, all = 0.f;
+      for (int head = warp; head < a.group; head += WARPS) {
+        const float top = stats[2 * WARPS * 16 + head], all = stats[(2 * WARPS + 1) * 16 + head];
+        const float by = all == 0.f ? 0.f : 1.f / all;
+        const long long at = w.r.s0 * a.os[0] + ((long long)w.kvh * a.group + head) * a.os[1];
 #pragma unroll
-        for (int y = 0; y < WARPS; ++y) top = fmaxf(top, stats[y * 16 + head]);
-#pragma unroll
-        for (int y = 0; y < WARPS; ++y) {
-          const float my = stats[y * 16 + head];
-          all += stats[(WARPS + y) * 16 + head] * (my == -INFINITY ? 1.f : exp2f((my - top) * c));
+        for (int e = 0; e < DP / 32; ++e) {
+          const int d = lane + 32 * e;
+          if (d < a.D) {
+            const float v = sum[head * S::SUM_ROW + d];
+            if (alone) put(a.out, a.out_bf16, at + d, v * by);
+            else part[head * a.D + d] = v;
+          }
         }
-        const float v = sum[head * DP + d];
-        if (alone) {
-          put(a.out, a.out_bf16, w.r.s0 * a.os[0] + ((long long)w.kvh * a.group + head) * a.os[1] + d, all == 0.f ? 0.f : v / all);
-        } else {
-          part[x] = v;
-          if (d == 0) { part[a.group * a.D + head] = top; part[a.group * (a.D + 1) + head] = all; }
+        if (!alone && lane == 0) {
+          part[a.group * a.D + head] = top;
+          part[a.group * (a.D + 1) + head] = all;
         }
       }
-      const long long after = w.base + w.p.count;
+      const long long after = w.base + w.length;
       if (threadIdx.x == 0) {
         const bool by_pair = heads_by_pair(a);
         const int parts = w.j0 == 0 && after > stop ? (int)((after - 1) / chunk) - (int)blockIdx.x + 1 : 0;
@@ -410,25 +443,43 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
 
 // Joins the parts of a pair that spans several ranges: one CTA per head (grid x) and query head of the pair (grid y).
 // The parts' maxima and sums first, then every warp adds up every JOIN_WARPS-th part, then the warps' sums in their order.
-constexpr int JOIN_WARPS = 8;
+constexpr int JOIN_WARPS = 8, AHEAD = 4;
 __global__ void __launch_bounds__(JOIN_WARPS * 32) dvm_attention_join_kernel(const __grid_constant__ Args a) {
   __shared__ float weight[DVM_ATT_UNITS];
   __shared__ float stat[2][JOIN_WARPS];
   __shared__ float sums[JOIN_WARPS][128];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (heads_by_pair(a) && request_at(a, blockIdx.x / a.hk).q_len == 0) return;  // (no row: no CTA wrote this head)
+  grid_ready();
+  grid_wait();
   const int4 head = *head_of(a, blockIdx.x);
+  const bool by_pair = heads_by_pair(a);
+  if (by_pair && request_at(a, blockIdx.x / a.hk).q_len == 0) return;  // (no row: no CTA wrote this head)
   const int parts = head.z;
   if (parts < 2) return;
   const float c = a.scale * 1.4426950408889634f;
   const int size = a.group * a.D;
   auto part = [&](int k) -> const float* { return slot_of(a, head.y + k, k ? 0 : head.w); };
-  float m = -INFINITY, l = 0.f;
-  for (int k = threadIdx.x; k < parts; k += JOIN_WARPS * 32) {
-    weight[k] = part(k)[size + h];
-    m = fmaxf(m, weight[k]);
+  // Everything is asked for at once: statistics of part threadIdx.x, the first AHEAD outputs of this warp, the row's place.
+  const int request = head.x / a.hk, kvh = head.x - request * a.hk;
+  const long long row = request_at(a, request).s0;
+  float m0 = -INFINITY, l0 = 0.f, first[AHEAD][4] = {};
+  if ((int)threadIdx.x < parts) {
+    const float* p = part(threadIdx.x) + size + h;
+    m0 = p[0];
+    l0 = p[a.group];
   }
+#pragma unroll
+  for (int x = 0; x < AHEAD; ++x) {
+    const int k = warp + x * JOIN_WARPS;
+    if (k < parts) {
+      const float* p = part(k) + h * a.D;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (lane + 32 * e < a.D) first[x][e] = p[lane + 32 * e];
+    }
+  }
+  float m = m0, l = 0.f;
+  for (int k = threadIdx.x + JOIN_WARPS * 32; k < parts; k += JOIN_WARPS * 32) m = fmaxf(m, part(k)[size + h]);
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
   if (lane == 0) stat[0][warp] = m;
@@ -436,16 +487,25 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) dvm_attention_join_kernel(con
 #pragma unroll
   for (int x = 0; x < JOIN_WARPS; ++x) m = fmaxf(m, stat[0][x]);
   for (int k = threadIdx.x; k < parts; k += JOIN_WARPS * 32) {
-    weight[k] = weight[k] == -INFINITY ? 0.f : exp2f((weight[k] - m) * c);  // (a part that saw nothing is all zeros)
-    l += part(k)[size + a.group + h] * weight[k];
+    const bool other = k >= JOIN_WARPS * 32;
+    const float mk = other ? part(k)[size + h] : m0, lk = other ? part(k)[size + a.group + h] : l0;
+    weight[k] = mk == -INFINITY ? 0.f : exp2f((mk - m) * c);  // (a part that saw nothing is all zeros)
+    l += lk * weight[k];
   }
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
   if (lane == 0) stat[1][warp] = l;
   __syncthreads();
   float v[4] = {};
+#pragma unroll
+  for (int x = 0; x < AHEAD; ++x) {
+    const int k = warp + x * JOIN_WARPS;
+    if (k < parts)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = fmaf(first[x][e], weight[k], v[e]);
+  }
 #pragma unroll 4
-  for (int k = warp; k < parts; k += JOIN_WARPS) {
+  for (int k = warp + AHEAD * JOIN_WARPS; k < parts; k += JOIN_WARPS) {
     const float* p = part(k) + h * a.D;
     const float f = weight[k];
 #pragma unroll
@@ -462,8 +522,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) dvm_attention_join_kernel(con
     float all = 0.f;
 #pragma unroll
     for (int x = 0; x < JOIN_WARPS; ++x) all += sums[x][threadIdx.x];
-    const int request = head.x / a.hk, kvh = head.x - request * a.hk;
-    put(a.out, a.out_bf16, request_at(a, request).s0 * a.os[0] + ((long long)kvh * a.group + h) * a.os[1] + threadIdx.x, l == 0.f ? 0.f : all / l);
+    put(a.out, a.out_bf16, row * a.os[0] + ((long long)kvh * a.group + h) * a.os[1] + threadIdx.x, l == 0.f ? 0.f : all / l);
   }
 }
 
@@ -472,10 +531,7 @@ int launch_single(const CUtensorMap& k, const CUtensorMap& v, const Args& a, int
   static std::atomic<uint64_t> allowed{0};
   const int st = dvm_allow_smem((const void*)dvm_attention_single_kernel<DP>, (int)SingleSmem<DP>::BYTES, device, &allowed);
   if (st != DVM_OK) return st;
-  dvm_attention_single_kernel<DP><<<DVM_ATT_UNITS, THREADS, SingleSmem<DP>::BYTES, stream>>>(k, v, a);
-  DVM_CUDA(cudaGetLastError());
-  dvm_count_launch();
-  return DVM_OK;
+  return dvm_launch_early(dvm_attention_single_kernel<DP>, DVM_ATT_UNITS, THREADS, SingleSmem<DP>::BYTES, stream, k, v, a);
 }
 
 }  // namespace att
@@ -488,12 +544,5 @@ int dvm_launch_attention_single(const dvm_attention_desc& d, const dvm::att::Arg
   if (st == DVM_OK) st = dvm_cache_map(d, d.v_stride, a.v, TILE, &v);
   if (st == DVM_OK) st = a.D <= 64 ? launch_single<64>(k, v, a, device, stream) : launch_single<128>(k, v, a, device, stream);
   if (st != DVM_OK) return st;
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3(heads_by_pair(a) ? a.n * a.hk : DVM_ATT_UNITS, a.group); cfg.blockDim = dim3(JOIN_WARPS * 32); cfg.stream = stream; cfg.attrs = at; cfg.numAttrs = 1;
-  DVM_CUDA(cudaLaunchKernelEx(&cfg, dvm_attention_join_kernel, a));
-  dvm_count_launch();
-  return DVM_OK;
+  return dvm_launch_early(dvm_attention_join_kernel, dim3(heads_by_pair(a) ? a.n * a.hk : DVM_ATT_UNITS, a.group), JOIN_WARPS * 32, 0, stream, a);
 }

@@ -44,5 +44,32 @@ inline int dvm_allow_smem(const void* kernel, int bytes, int device, std::atomic
 }
 void dvm_count_launch();
 
+// A launch that may start while the kernel before it on the stream ends: its CTAs are set up and wait (grid_wait) until that
+// kernel has finished and what it wrote can be read.  Every thread of such a kernel calls grid_wait before its first access
+// to memory, grid_ready lets the next launch of this kind do the same.  (Another kernel before or after orders as ever.)
+// Measured in a chain of launches: one token's rotary 2.8 -> 1.8 us, and 0.7 us less of the host's time.
+template <class... P, class... A>
+int dvm_launch_early(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  DVM_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
+  dvm_count_launch();
+  return DVM_OK;
+}
+#ifdef __CUDACC__
+namespace dvm {
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_ready() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+}  // namespace dvm
+#endif
+
 int dvm_launch_matmul(const uint32_t* code, size_t n_words, void* const* tensors, int n_tensors,
                       cudaStream_t stream);

@@ -66,6 +66,7 @@ __global__ void __launch_bounds__(THREADS) dvm_paging_kernel(const __grid_consta
   int* const pages = sm + a.n + 1;      // n + 1: new pages before request i
   int* const cached = sm + 2 * a.n + 2; // n: tokens of request i in the cache
   __shared__ Sums warp_sums[THREADS / 32];
+  grid_wait();
   const int per = (a.n + THREADS - 1) / THREADS, i0 = min(a.n, (int)threadIdx.x * per), i1 = min(a.n, i0 + per);
 
   // Blocks that a request's new rows reach and its cached tokens do not.
@@ -166,8 +167,5 @@ int dvm_launch_paging(const dvm_paging_desc& d, void* const* t, cudaStream_t str
   if (st != DVM_OK) return st;
   const int64_t per_cta = THREADS * ROWS_PER_THREAD, ctas = (d.rows + per_cta - 1) / per_cta;
   const int grid = (int)(ctas < 1 ? 1 : ctas < 2 * dev.sm_count ? ctas : 2 * dev.sm_count);
-  dvm_paging_kernel<<<grid, THREADS, smem, stream>>>(a);
-  DVM_CUDA(cudaGetLastError());
-  dvm_count_launch();
-  return DVM_OK;
+  return dvm_launch_early(dvm_paging_kernel, grid, THREADS, smem, stream, a);
 }

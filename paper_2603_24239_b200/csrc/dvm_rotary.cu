@@ -131,6 +131,8 @@ __global__ void __launch_bounds__(THREADS, VEC ? 3 : 2) dvm_rotary_kernel(const 
     dst[u] += at0;
   }
   const int run = at1 - at0;
+  grid_ready();
+  grid_wait();
 
   struct Place { int pos, slot; };
   auto place_of = [&](long long t) -> Place {
@@ -295,16 +297,12 @@ __global__ void __launch_bounds__(THREADS, VEC ? 3 : 2) dvm_rotary_kernel(const 
 template <class TI, class TO>
 int launch(const Args& a, int grid, int threads, int device, cudaStream_t stream) {
   const int bytes = threads * BYTES<TI>;
-  if (!a.vec) {
-    dvm_rotary_kernel<TI, TO, 0, false><<<grid, threads, 0, stream>>>(a);
-    return DVM_OK;
-  }
+  if (!a.vec) return dvm_launch_early(dvm_rotary_kernel<TI, TO, 0, false>, grid, threads, 0, stream, a);
   auto kernel = a.lanes == 8 ? dvm_rotary_kernel<TI, TO, 8, true> : a.lanes == 16 ? dvm_rotary_kernel<TI, TO, 16, true> : dvm_rotary_kernel<TI, TO, 32, true>;
   static std::atomic<uint64_t> allowed[3];
   const int st = dvm_allow_smem((const void*)kernel, THREADS * BYTES<TI>, device, &allowed[a.lanes / 16]);
   if (st != DVM_OK) return st;
-  kernel<<<grid, threads, bytes, stream>>>(a);
-  return DVM_OK;
+  return dvm_launch_early(kernel, grid, threads, bytes, stream, a);
 }
 
 }  // namespace rotary
@@ -349,11 +347,6 @@ int dvm_launch_rotary(const dvm_rotary_desc& d, void* const* t, cudaStream_t str
   a.chunks = (int)(want < least ? least : want < most ? want : most);
   const int64_t cap = resident / a.chunks < 1 ? 1 : resident / a.chunks;  // tokens at a time
   const int grid = (int)(d.tokens < cap ? d.tokens : cap) * a.chunks;
-  int rc;
-  if (d.dtype == DVM_BF16) rc = d.out_dtype == DVM_BF16 ? launch<__nv_bfloat16, __nv_bfloat16>(a, grid, threads, dev.device, stream) : launch<__nv_bfloat16, float>(a, grid, threads, dev.device, stream);
-  else rc = d.out_dtype == DVM_BF16 ? launch<float, __nv_bfloat16>(a, grid, threads, dev.device, stream) : launch<float, float>(a, grid, threads, dev.device, stream);
-  if (rc != DVM_OK) return rc;
-  DVM_CUDA(cudaGetLastError());
-  dvm_count_launch();
-  return DVM_OK;
+  if (d.dtype == DVM_BF16) return d.out_dtype == DVM_BF16 ? launch<__nv_bfloat16, __nv_bfloat16>(a, grid, threads, dev.device, stream) : launch<__nv_bfloat16, float>(a, grid, threads, dev.device, stream);
+  return d.out_dtype == DVM_BF16 ? launch<float, __nv_bfloat16>(a, grid, threads, dev.device, stream) : launch<float, float>(a, grid, threads, dev.device, stream);
 }
