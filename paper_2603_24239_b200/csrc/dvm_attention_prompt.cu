@@ -204,9 +204,11 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)words)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  if (warp == 9 && lane < 3) tma_prefetch(lane == 0 ? &tm_q : lane == 1 ? &tm_k : &tm_v);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  grid_wait();
   const uint32_t tmem = words[0], tmem_o = tmem + 4 * KT;  // S_x at place b: 64 (2 x + b)
 
   // A block: up to 2 x tokens rows of query tokens of one request, for one kv head, described by 16 words of shared memory
@@ -694,10 +696,7 @@ int launch_prompt(const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap&
   static std::atomic<uint64_t> allowed{0};
   const int st = dvm_allow_smem((const void*)dvm_attention_prompt_kernel<DP>, (int)PromptSmem<DP>::BYTES, device, &allowed);
   if (st != DVM_OK) return st;
-  dvm_attention_prompt_kernel<DP><<<grid, PROMPT_THREADS, PromptSmem<DP>::BYTES, stream>>>(q, k, v, a);
-  DVM_CUDA(cudaGetLastError());
-  dvm_count_launch();
-  return DVM_OK;
+  return dvm_launch_early(dvm_attention_prompt_kernel<DP>, grid, PROMPT_THREADS, PromptSmem<DP>::BYTES, stream, q, k, v, a);
 }
 
 }  // namespace att
