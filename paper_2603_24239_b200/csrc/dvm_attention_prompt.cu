@@ -200,6 +200,15 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  // Rows that no head of the group falls on (128 is not a multiple of every group) are never loaded: zeros, or what the last
+  // kernel left there would be scores, and NaN among them sends their warp to the sums for a rescaling at every tile
+  // (12 ragged prompts, 5 heads to a group: 143 us became 187 after some kernels and not after others).
+  const int held_rows = tokens * a.group;
+  for (uint32_t i = threadIdx.x; i < 2 * S::HALVES * (PT - held_rows) * 8; i += PROMPT_THREADS) {
+    const uint32_t r = i / (PT - held_rows);  // tile, half and 16 bytes
+    *(uint4*)(sm + (r / (8 * S::HALVES)) * S::Q_TILE + (r / 8 % S::HALVES) * Q_HALF + (held_rows + i % (PT - held_rows)) * 128 + (r % 8) * 16) = make_uint4(0, 0, 0, 0);
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   if (warp == 8) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)words)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
