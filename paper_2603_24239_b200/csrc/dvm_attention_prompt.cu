@@ -240,7 +240,17 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
   if (warp == 11) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
     // ---------------- blocks: those of all requests in a row, a request's last block first ----------------
-    int chunk = -32, before = 0, all = 0, mine = 0, upto = 0;  // 32 requests, the blocks before them, theirs
+    // (Up to 32 requests: the longest first, so that short blocks are left for the end: 12 ragged prompts 143 -> 135 us.  With
+    // more of them the end is a small part, and sorting every 32 cost 592 short prompts 37.6 -> 39.7 us.)
+    int chunk = -32, before = 0, all = 0, mine = 0, upto = 0, who = 0, sorted = -1;  // 32 requests, the blocks before them, theirs
+    auto sum_up = [&](int v) -> int {
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, v, d);
+        if (lane >= d) v += y;
+      }
+      return v;
+    };
     // The grid has a CTA for every block.  One that runs takes its own, then those of CTAs that have not started, in their
     // order, by cancelling their launch: whoever is free takes the next, longest first, without a counter in memory.
     const uint32_t answer = base + S::WORK + 128;
@@ -249,25 +259,39 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     for (int k = 0, asked = 0; ok;) {
       const long long block = id < 0 ? -1 : id / a.hk;
       bool any = id >= 0;
-      if (any && block < before) chunk = -32, before = all = 0;  // (an order that the hardware does not promise)
+      if (any && block < before) chunk = -32, before = all = 0, sorted = -1;  // (an order that the hardware does not promise)
       while (any && block >= (long long)before + all) {
         before += all;
         chunk += 32;
         any = chunk < a.n;
         const int i = chunk + lane;
         mine = i < a.n ? (min(request_at(a, i).q_len, a.max_q) + 2 * tokens - 1) / (2 * tokens) : 0;
-        upto = mine;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-          const int y = __shfl_up_sync(0xffffffffu, upto, d);
-          if (lane >= d) upto += y;
-        }
+        who = i;
+        upto = sum_up(mine);
         all = __shfl_sync(0xffffffffu, upto, 31);
+      }
+      if (any && a.n > 1 && a.n <= 32 && sorted != chunk) {
+        sorted = chunk;
+        const int i = chunk + lane, length = i < a.n ? (a.window ? min(a.lengths[i], a.window) : a.lengths[i]) : -1;
+        int rank = 0, from = 0;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const int other = __shfl_sync(0xffffffffu, length, j);
+          rank += other > length || (other == length && j < lane);
+        }
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const uint32_t is = __ballot_sync(0xffffffffu, rank == j);
+          if (lane == j) from = __ffs(is) - 1;
+        }
+        mine = __shfl_sync(0xffffffffu, mine, from);
+        who = chunk + from;
+        upto = sum_up(mine);
       }
       const int at = (int)(block - before);
       const uint32_t owner = __ballot_sync(0xffffffffu, any && at >= upto - mine && at < upto);
       const int src = owner ? __ffs(owner) - 1 : 0;
-      const int tok0 = __shfl_sync(0xffffffffu, upto - 1 - at, src) * 2 * tokens, request = chunk + src;
+      const int tok0 = __shfl_sync(0xffffffffu, upto - 1 - at, src) * 2 * tokens, request = __shfl_sync(0xffffffffu, who, src);
       const bool beyond = !owner && id >= 0;  // (the grid is sized for the most blocks that `rows` rows can make)
       if (!beyond) {
       ok = k < 2 || mbar_wait_flat(bar_we + 8 * (k & 1), ((k >> 1) & 1) ^ 1, abort_flag);
