@@ -14,7 +14,9 @@
 // of each tile: scores and sums by mma.m16n8k16 with the query heads as the 16 rows (up to 16 share a kv head), fragments
 // by ldmatrix.  Each warp keeps its own maximum, sum and output, so the warps only meet when a pair ends.  The tensor
 // work is far below what the bytes take, which is why tcgen05 with its 128-row tiles and tensor-memory round trips is not
-// used here.  Weights are rounded to bf16 for the second product, their sum is not: the error is that of one bf16
+// used here.  64 requests of up to 8192 tokens, 64 / 8 heads of 128: 212 us, 6.2 TB/s; 32 requests of up to 16384 under a
+// window of 4096, 32 / 32 heads: 330 us, 6.5 TB/s; one request of 8192, 32 / 8 heads: 15 us, of which the bytes take 5.
+// Weights are rounded to bf16 for the second product, their sum is not: the error is that of one bf16
 // rounding per weight, which averages out over the tokens.
 //
 // Tokens a row does not see: pages outside the pool, behind the last token or wholly hidden are never read (TMA fills

@@ -12,7 +12,8 @@
 // instruction); the store rounds once.  With the head's place worked out anew for every token, the same kernel took 744
 // instructions per warp and token and was bound by them: 80 us for 8192 tokens of 32 + 8 + 8 heads of 128.  With the next
 // token's data in registers (one token ahead, two CTAs per SM) it was bound by what is in flight: 50 us.  Now each
-// thread copies its own runs into shared memory (cp.async, DEPTH tokens ahead) and reads them from there.
+// thread copies its own runs into shared memory (cp.async, DEPTH tokens ahead) and reads them from there: 42 us, 4.9 TB/s,
+// 73 % of the SMs' issue slots; 1531 tokens of 40 + 8 + 8 fp32 heads of 96 19 us, 3.5 TB/s; one token 1.8 us in a chain.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
