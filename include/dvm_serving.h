@@ -15,7 +15,8 @@
  * Conventions as in dvm.h: every call returns DVM_OK or a negative DVM_ERR_*; the caller owns every tensor, workspaces too;
  * nothing is allocated, nothing synchronised; launches are asynchronous on the stream given to dvm_launch and may be
  * captured.  Tensors are named by their place in the launch's list (inputs, then outputs).  Index tensors are int32.
- * Strides are in elements.  An output must not overlap another tensor of the launch.
+ * Strides are in elements.  An output must not overlap another tensor of the launch; dvm_launch refuses what it can see
+ * of that (outputs that begin where another tensor does, any overlap of paging's) with DVM_ERR_INVALID_ARG.
  */
 #ifndef DVM_SERVING_H_
 #define DVM_SERVING_H_
@@ -67,7 +68,7 @@ int dvm_encode_paging(const dvm_paging_desc* d, void* code, size_t code_capacity
  * Tensors: q [tokens, q_heads, head_dim], k, v [tokens, kv_heads, head_dim] (v: `paged` only), q weight, k weight
  * [head_dim] (`norm` only), angles [angle_rows, rotary_dim] fp32 dense, positions [tokens], slots [tokens] (`paged` only)
  * -> q_out, then k_cache, v_cache [pages, page_size, kv_heads, head_dim] or k_out [tokens, kv_heads, head_dim].
- * The last dimension of every tensor is adjacent.  q_out may be q itself (same pointer and strides), and k_out k.
+ * The last dimension of every tensor is adjacent.  q_out may be q itself (same pointer, strides and type), and k_out k.
  * DVM_ERR_UNSUPPORTED: head_dim not a multiple of 8 or above 256, rotary_dim not a multiple of 8. */
 typedef struct {
   int64_t tokens, q_heads, kv_heads, head_dim;

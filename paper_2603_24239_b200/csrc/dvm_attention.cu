@@ -134,6 +134,23 @@ int dvm_launch_serving(const uint32_t* w, void* const* tensors, int n_tensors, c
   for (int i = 0; i < nt; ++i)
     if (need[i] > 0 && !tensors[i]) return DVM_ERR_INVALID_ARG;
   const uint32_t type = w[DVM_H_KERNEL_TYPE];
+  // An output that begins where another tensor does overlaps it (the dense ones of paging: that shares a byte with it).
+  // Rotary may work in place: each run is read and written by one thread.
+  int may[2][2] = {{-1, -1}, {-1, -1}};
+  if (type == DVM_KERNEL_ROTARY) {
+    dvm_rotary_desc d;
+    dvm_serving_desc(w, &d);
+    const RotarySlots s = dvm_rotary_slots(d);
+    auto same = [&](const int64_t* x, const int64_t* y) { return d.dtype == d.out_dtype && x[0] == y[0] && x[1] == y[1]; };
+    if (same(d.q_stride, d.q_out_stride)) { may[0][0] = s.q; may[0][1] = s.q_out; }
+    if (!d.paged && same(d.k_stride, d.k_out_stride)) { may[1][0] = s.k; may[1][1] = s.k_out; }
+  }
+  for (int i = (w[DVM_H_COUNTS] >> 8) & 0xff; i < nt; ++i)
+    for (int j = 0; j < nt; ++j) {
+      if (i == j || need[i] <= 0 || need[j] <= 0 || (j == may[0][0] && i == may[0][1]) || (j == may[1][0] && i == may[1][1])) continue;
+      const uintptr_t x = (uintptr_t)tensors[i], y = (uintptr_t)tensors[j];
+      if (type == DVM_KERNEL_PAGING ? x < y + (uintptr_t)need[j] && y < x + (uintptr_t)need[i] : x == y) return DVM_ERR_INVALID_ARG;
+    }
   auto aligned = [&](int slot, int dtype) { return slot < 0 || ((uintptr_t)tensors[slot] & (dtype == DVM_BF16 ? 1 : 3)) == 0; };
   if (type == DVM_KERNEL_PAGING) {
     dvm_paging_desc d;

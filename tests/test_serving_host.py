@@ -155,3 +155,38 @@ def test_binding_checks_tensors():
                    dict(k=k[:3]), dict(q_out=q[:, :, ::2])):
         with pytest.raises(dvm.DvmError):
             dvm.encode_rotary(**{**good, **change})
+
+
+def launched(fn, d, places):
+    """dvm_launch's status for tensors at these addresses: a refusal, or on a machine without a device its CUDA error."""
+    st, buf, size = _encode(getattr(binding.lib, "dvm_encode_" + fn), d)
+    assert st == OK
+    return binding.lib.dvm_launch(buf, size, (C.c_void_p * len(places))(*places), len(places), None)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are made up: only for a machine that cannot launch")
+def test_outputs_that_overlap_are_refused():
+    CUDA = -6
+    far = [0x100000 * (i + 1) for i in range(16)]
+    at = lambda n, **kw: [kw.get(f"t{i}", far[i]) for i in range(n)]   # noqa: E731
+    # paging: cached, fresh, free, table, starts, lengths, positions, slots, taken; 5 requests, 100 rows, a table of 5 x 7
+    assert launched("paging", paging(), at(9)) == CUDA
+    assert launched("paging", paging(), at(9, t5=far[0])) == INVALID             # lengths over cached
+    assert launched("paging", paging(), at(9, t5=far[0] + 16)) == INVALID        # its last element
+    assert launched("paging", paging(), at(9, t5=far[0] + 20)) == CUDA           # just behind it
+    assert launched("paging", paging(), at(9, t6=far[7] + 396)) == INVALID
+    assert launched("paging", paging(free_pages=0), at(9, t8=far[2])) == CUDA    # an empty tensor overlaps nothing
+    assert launched("paging", paging(), at(9, t1=far[0])) == CUDA                # inputs may
+    # rotary, not paged, no norm: q, k, angles, positions, q_out, k_out
+    kw = dict(norm=0, paged=0, k_out_stride=(128, 64))
+    assert launched("rotary", rotary(**kw), at(6)) == CUDA
+    assert launched("rotary", rotary(**kw), at(6, t4=far[0], t5=far[1])) == CUDA           # in place
+    assert launched("rotary", rotary(**kw), at(6, t5=far[0])) == INVALID                   # keys over queries
+    assert launched("rotary", rotary(**kw), at(6, t5=far[4])) == INVALID
+    assert launched("rotary", rotary(**kw, q_out_stride=(512, 64)), at(6, t4=far[0])) == INVALID
+    assert launched("rotary", rotary(**kw, out_dtype=0), at(6, t4=far[0])) == INVALID      # fp32 over bf16
+    # attention: q, k, v, table, starts, lengths, out, workspace
+    assert launched("attention", attention(), at(8)) == CUDA
+    assert launched("attention", attention(), at(8, t2=far[1])) == CUDA                    # values in the keys' cache: inputs
+    assert launched("attention", attention(), at(8, t6=far[0])) == INVALID
+    assert launched("attention", attention(max_q=1), at(8, t7=far[6])) == INVALID          # the workspace over the output
