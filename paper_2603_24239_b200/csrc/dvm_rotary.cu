@@ -1,10 +1,12 @@
 // Rotary meta-kernel: norms of the query and key heads, rotation by position, keys and values into the paged cache.
 //
 // One pass, bound by memory: a head of D elements is read once and written once, by a group of 8, 16 or 32 lanes with two
-// runs of 4 elements each.  The runs are laid so that a pair is always in one lane: lane l < R / 8 holds the elements
-// [4 l, 4 l + 4) and [R / 2 + 4 l, R / 2 + 4 l + 4) of a head whose halves are paired, [8 l, 8 l + 8) where neighbours
-// are, and every lane from R / 8 on holds [8 l, 8 l + 8), which stay.  Rotation then takes no exchange between lanes, and
-// either way a lane needs cos and sin of the pairs [4 l, 4 l + 4): 16 bytes each.  Only the mean of squares crosses lanes.
+// runs of 4 elements each, so laid that a pair is always in one lane and that the lanes' runs lie side by side: lane
+// l < R / 8 holds the elements [4 l, 4 l + 4) and [R / 2 + 4 l, R / 2 + 4 l + 4) of the part that turns, the lanes from
+// R / 8 on hold the rest, which stays, in the same manner.  Rotation then takes no exchange between lanes, whether halves
+// or neighbours are paired.  Only the mean of squares crosses lanes.  (8 elements in a row per lane where
+// fp32 neighbours are paired, so that every access left out every other 16 bytes: 1531 tokens of 40 + 8 + 8 heads of 96 17.6 us
+// on the device, 13.0 now.)
 // A CTA keeps the same heads for all tokens it takes -- all of them, or a part where there are more than its groups can
 // have in flight -- so what a thread reads and writes is found once and moves by a stride; position, slot and angles are
 // read once per thread and token, and while one token is computed the heads and angles of the next are on their way, and
@@ -12,8 +14,8 @@
 // instruction); the store rounds once.  With the head's place worked out anew for every token, the same kernel took 744
 // instructions per warp and token and was bound by them: 80 us for 8192 tokens of 32 + 8 + 8 heads of 128.  With the next
 // token's data in registers (one token ahead, two CTAs per SM) it was bound by what is in flight: 50 us.  Now each
-// thread copies its own runs into shared memory (cp.async, DEPTH tokens ahead) and reads them from there: 42 us, 4.9 TB/s,
-// 73 % of the SMs' issue slots; 1531 tokens of 40 + 8 + 8 fp32 heads of 96 19 us, 3.5 TB/s; one token 1.8 us in a chain.
+// thread copies its own runs into shared memory (cp.async, DEPTH tokens ahead) and reads them from there: 38 us, 5.3 TB/s;
+// one token 1.8 us in a chain of launches.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -45,6 +47,8 @@ struct Args {
   float eps, inv_D;
 };
 
+__device__ __forceinline__ void copy8(uint32_t dst, const void* p) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(p) : "memory"); }
+
 // Four elements as they lie in memory, and as fp32.
 template <class T> struct Run;
 template <> struct Run<__nv_bfloat16> {
@@ -58,7 +62,7 @@ template <> struct Run<__nv_bfloat16> {
     }
   }
   static __device__ __forceinline__ void copy(uint32_t dst, const __nv_bfloat16* p) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(p) : "memory");
+    copy8(dst, p);
   }
   __device__ __forceinline__ void get(float2* x) const {
     x[0] = make_float2(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u));
@@ -89,15 +93,23 @@ __device__ __forceinline__ void store4(float* p, bool vec, const float2* x) {
   }
 }
 
-// LANES: lanes of a group, VEC: runs of 4 elements are aligned everywhere; 0, false: the kernel for the other layouts.
-template <class TI, class TO, int LANES, bool VEC>
+// LANES: lanes of a group, VEC: runs of 4 elements are aligned everywhere, INTER: neighbours are paired; 0, false, false: the
+// kernel for the other layouts.
+template <class TI, class TO, int LANES, bool VEC, bool INTER>
 __global__ void __launch_bounds__(THREADS, VEC ? 3 : 2) dvm_rotary_kernel(const __grid_constant__ Args a) {
   constexpr int U = UNROLL;
   extern __shared__ __align__(16) uint8_t smem[];
   const int L = LANES ? LANES : a.lanes, group = threadIdx.x / L, lane = threadIdx.x & (L - 1), groups = blockDim.x / L;
   const bool live = 8 * lane < a.D, turned = 8 * lane < a.rot;
-  const bool halves = turned && !a.interleaved;
-  const int at0 = halves ? 4 * lane : 8 * lane, at1 = halves ? (a.rot >> 1) + 4 * lane : 8 * lane + 4;  // this lane's two runs
+  // this lane's two runs, and where the cosines of their pairs are: two from c0 on, two from c1 on
+  const int from = turned ? 0 : a.rot, width = turned ? a.rot : a.D - a.rot, nth = turned ? lane : lane - (a.rot >> 3);
+  // bf16 neighbours stay in a row: their 8 elements are 16 bytes, and so are their cosines (40.2 us in two runs, 38.5 in one,
+  // for the 8192 tokens above)
+  constexpr bool IN_A_ROW = VEC && INTER && sizeof(TI) == 2 && sizeof(TO) == 2;
+  const bool interleaved = VEC ? INTER : a.interleaved;
+  const int at0 = IN_A_ROW && turned ? 8 * lane : from + 4 * nth, at1 = at0 + (IN_A_ROW && turned ? 4 : width >> 1);
+  const bool apart = interleaved && !IN_A_ROW;
+  const int c0 = apart ? 2 * lane : 4 * lane, c1 = apart ? (a.rot >> 2) + 2 * lane : 4 * lane + 2;
   const int heads = a.hq + a.hk * (a.paged ? 2 : 1);
 
   __shared__ float4 weight[2][2][32];  // [query, key][run][lane]
@@ -157,10 +169,18 @@ __global__ void __launch_bounds__(THREADS, VEC ? 3 : 2) dvm_rotary_kernel(const 
           Run<TI>::copy(base + place + mine + (2 * u) * blockDim.x * RUN, src[u]);
           Run<TI>::copy(base + place + mine + (2 * u + 1) * blockDim.x * RUN, src[u] + run);
         }
-      if (turned && in_table(p)) {  // cos and sin of the pairs [4 lane, 4 lane + 4)
-        const float* row = a.angles + (long long)p.pos * a.rot + 4 * lane;
-        Run<float>::copy(base + place + mine_cs, row);
-        Run<float>::copy(base + place + mine_cs + blockDim.x * 16, row + (a.rot >> 1));
+      if (turned && in_table(p)) {
+        const float* row = a.angles + (long long)p.pos * a.rot;
+        const uint32_t to = base + place + mine_cs;
+#pragma unroll
+        for (int i = 0; i < 2; ++i, row += a.rot >> 1) {  // cos, sin
+          if (apart) {
+            copy8(to + i * blockDim.x * 16, row + c0);
+            copy8(to + i * blockDim.x * 16 + 8, row + c1);
+          } else {
+            Run<float>::copy(to + i * blockDim.x * 16, row + c0);
+          }
+        }
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -185,9 +205,9 @@ __global__ void __launch_bounds__(THREADS, VEC ? 3 : 2) dvm_rotary_kernel(const 
           x[u][1].load(src[u] + run, false);
         }
       if (turned) {
-        const float* row = a.angles + (long long)p.pos * a.rot + 4 * lane;
-        dc.load(row, false);
-        ds.load(row + (a.rot >> 1), false);
+        const float *row = a.angles + (long long)p.pos * a.rot, *sines = row + (a.rot >> 1);
+        dc.w = make_float4(row[c0], row[c0 + 1], row[c1], row[c1 + 1]);
+        ds.w = make_float4(sines[c0], sines[c0 + 1], sines[c1], sines[c1 + 1]);
       }
     }
     const long long q_at = t * a.qo[0];
@@ -235,7 +255,7 @@ __global__ void __launch_bounds__(THREADS, VEC ? 3 : 2) dvm_rotary_kernel(const 
       }
       if (kind[u] == NONE || (kind[u] != QUERY && !stored)) continue;
       if (turned && kind[u] != VALUE) {
-        if (a.interleaved) {  // y[i] is pair i
+        if (interleaved) {  // y[i] is pair i
           const float cc[4] = {c[0].x, c[0].y, c[1].x, c[1].y}, ss[4] = {s[0].x, s[0].y, s[1].x, s[1].y};
 #pragma unroll
           for (int i = 0; i < 4; ++i) y[i] = fma2(make_float2(-y[i].y, y[i].x), make_float2(ss[i], ss[i]), mul2(y[i], make_float2(cc[i], cc[i])));
@@ -295,13 +315,17 @@ __global__ void __launch_bounds__(THREADS, VEC ? 3 : 2) dvm_rotary_kernel(const 
   if (VEC) asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
+template <class TI, class TO, bool INTER> auto aligned_kernel(int lanes) {
+  return lanes == 8 ? dvm_rotary_kernel<TI, TO, 8, true, INTER> : lanes == 16 ? dvm_rotary_kernel<TI, TO, 16, true, INTER> : dvm_rotary_kernel<TI, TO, 32, true, INTER>;
+}
+
 template <class TI, class TO>
 int launch(const Args& a, int grid, int threads, int device, cudaStream_t stream) {
   const int bytes = threads * BYTES<TI>;
-  if (!a.vec) return dvm_launch_early(dvm_rotary_kernel<TI, TO, 0, false>, grid, threads, 0, stream, a);
-  auto kernel = a.lanes == 8 ? dvm_rotary_kernel<TI, TO, 8, true> : a.lanes == 16 ? dvm_rotary_kernel<TI, TO, 16, true> : dvm_rotary_kernel<TI, TO, 32, true>;
-  static std::atomic<uint64_t> allowed[3];
-  const int st = dvm_allow_smem((const void*)kernel, THREADS * BYTES<TI>, device, &allowed[a.lanes / 16]);
+  if (!a.vec) return dvm_launch_early(dvm_rotary_kernel<TI, TO, 0, false, false>, grid, threads, 0, stream, a);
+  auto kernel = a.interleaved ? aligned_kernel<TI, TO, true>(a.lanes) : aligned_kernel<TI, TO, false>(a.lanes);
+  static std::atomic<uint64_t> allowed[2][3];
+  const int st = dvm_allow_smem((const void*)kernel, THREADS * BYTES<TI>, device, &allowed[a.interleaved][a.lanes / 16]);
   if (st != DVM_OK) return st;
   return dvm_launch_early(kernel, grid, threads, bytes, stream, a);
 }
