@@ -12,7 +12,7 @@ import torch
 import paper_2603_24239_b200 as dvm
 from tests import serving_oracle as orc
 from tests.serving_oracle import f64
-from tests.test_gpu_serving import BF16, F32, I32, Batch, angles, ints, normal, ok, paging_case, run_paging
+from tests.test_gpu_serving import BF16, F32, I32, Batch, angles, check_rotary, ints, normal, ok, paging_case, run_paging
 
 pytestmark = pytest.mark.gpu
 
@@ -25,6 +25,14 @@ def test_paging_with_all_requests_and_rows_that_end_early(seed):
     run_paging(c, f, free, table, page, rows)
     run_paging(c, f, free, table, page, rows // 2)     # the rows hold half of the new tokens
     run_paging(c - 40, f - 1, free, table, page, rows)  # lengths below zero count as nothing
+
+
+@pytest.mark.parametrize("dtype,out_dtype", [(BF16, BF16), (BF16, F32), (F32, BF16), (F32, F32)])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,rot", [(128, 128), (128, 56), (96, 64), (64, 8), (24, 0), (256, 248)])
+def test_rotary_types_pairings_and_parts(dtype, out_dtype, interleaved, dim, rot):
+    check_rotary(19, 9, 3, dim, rot, dtype=dtype, out_dtype=out_dtype, interleaved=interleaved, seed=dim)
+    check_rotary(19, 9, 3, dim, rot, dtype=dtype, out_dtype=out_dtype, interleaved=interleaved, seed=rot, shift=4, paged=False)
 
 
 @pytest.mark.parametrize("n,hq,hk,length", [(200, 6, 2, 150), (300, 1, 1, 70), (40, 32, 16, 200), (2, 512, 512, 200), (1, 300, 300, 700), (1, 3, 1, 9000)])
