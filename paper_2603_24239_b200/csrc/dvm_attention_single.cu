@@ -64,9 +64,9 @@ struct Walk {
   Request r;
   Span p;
   long long base;   // place of the pair's first tile on the line
-  int length;       // places of a pair on the line: its tiles, or `whole` (where not 0)
+  int length;       // places of a pair on the line: its tiles; of one request alone, rounded up to whole ranges
   int j0, j1;
-  __device__ __forceinline__ void load(const Args& a, int whole) { r = request_at(a, request); p = span_of(a, r); length = whole ? whole : p.count; }
+  __device__ __forceinline__ void load(const Args& a) { r = request_at(a, request); p = span_of(a, r); length = p.count; }
   __device__ __forceinline__ void cut(long long begin, long long stop) {
     j0 = (int)max(0ll, begin - base);
     j1 = (int)min((long long)p.count, stop - base);
@@ -75,7 +75,7 @@ struct Walk {
     base += length;
     if (++kvh == a.hk) {
       kvh = 0;
-      do { ++request; load(a, 0); } while (p.count == 0);  // (only called while tiles are left: some later request has them)
+      do { ++request; load(a); } while (p.count == 0);  // (only called while tiles are left: some later request has them)
     }
     cut(begin, stop);
   }
@@ -151,65 +151,79 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
   grid_ready();  // (the second kernel waits for this grid's end before it reads)
   grid_wait();
 
-  // ---- this CTA's range of the line: thread t counts the tiles of requests [t per, (t + 1) per) ----
-  const int per = (a.n + THREADS - 1) / THREADS;
-  long long mine = 0;
-  int count = 0;  // of the last one (with up to THREADS requests: the only one)
-  for (int i = threadIdx.x * per; i < min(a.n, (int)(threadIdx.x + 1) * per); ++i) mine += count = span_of(a, request_at(a, i)).count;
-  long long upto = mine;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, upto, d);
-    if (lane >= d) upto += y;
-  }
-  if (lane == 31) scan[warp] = upto;
-  __syncthreads();
-  long long total = 0;
-#pragma unroll
-  for (int w = 0; w <= WARPS; ++w) {
-    if (w < warp) upto += scan[w];
-    total += scan[w];
-  }
-  const long long count_all = total;
-  total *= a.hk;
-  long long chunk = max((total + DVM_ATT_UNITS - 1) / DVM_ATT_UNITS, (long long)MIN_TILES);
-  int whole = 0;
-  if (a.n == 1 && a.hk <= DVM_ATT_UNITS) {
-    const int units = DVM_ATT_UNITS / a.hk;  // per kv head
-    chunk = max((count_all + units - 1) / units, (long long)MIN_TILES);
-    whole = (int)((count_all + chunk - 1) / chunk * chunk);
-    total = (long long)whole * a.hk;
-  }
-  const long long begin = min(total, blockIdx.x * chunk), stop = min(total, begin + chunk);
-  if (begin == stop) {
-    if (threadIdx.x == 0 && !heads_by_pair(a)) *head_of(a, blockIdx.x) = make_int4(0, 0, 0, 0);
-    return;
-  }
-  // the thread whose requests hold tile `begin` walks to it
-  const long long from = (upto - mine) * a.hk, to = whole ? (threadIdx.x ? 0 : total) : upto * a.hk;
-  if (begin >= from && begin < to) {
-    long long at = from;
-    for (int i = threadIdx.x * per;; ++i) {
-      if (per > 1) count = span_of(a, request_at(a, i)).count;
-      const long long each = whole ? whole : count, after = at + each * a.hk;
-      if (begin < after) {
-        const long long kvh = (begin - at) / each;
-        scan[8] = i;
-        scan[9] = kvh;
-        scan[10] = at + kvh * each;
-        scan[11] = chunk;
-        scan[12] = stop;
-        break;
-      }
-      at = after;
-    }
-  }
-  __syncthreads();
   Walk w;
-  w.request = (int)scan[8];
-  w.kvh = (int)scan[9];
-  w.base = scan[10];
-  w.load(a, whole);
+  long long begin, stop;
+  if (a.n == 1 && a.hk <= DVM_ATT_UNITS) {
+    // ---- one request: every thread finds the range for itself ----
+    w.request = 0;
+    w.r = request_at(a, 0);
+    w.p = span_of(a, w.r);
+    const int count = w.p.count, units = DVM_ATT_UNITS / a.hk;  // per kv head
+    const int chunk = max((count + units - 1) / units, MIN_TILES), ranges = (count + chunk - 1) / chunk;
+    begin = (long long)blockIdx.x * chunk;
+    stop = begin + chunk;
+    w.kvh = ranges ? blockIdx.x / ranges : a.hk;
+    if (w.kvh >= a.hk) return;
+    w.length = ranges * chunk;
+    w.base = (long long)w.kvh * w.length;
+    if (threadIdx.x == 0) {
+      scan[11] = chunk;
+      scan[12] = stop;
+    }
+    __syncthreads();
+  } else {
+    // ---- thread t counts the tiles of requests [t per, (t + 1) per) ----
+    const int per = (a.n + THREADS - 1) / THREADS;
+    long long mine = 0;
+    int count = 0;  // of the last one (with up to THREADS requests: the only one)
+    for (int i = threadIdx.x * per; i < min(a.n, (int)(threadIdx.x + 1) * per); ++i) mine += count = span_of(a, request_at(a, i)).count;
+    long long upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += y;
+    }
+    if (lane == 31) scan[warp] = upto;
+    __syncthreads();
+    long long total = 0;
+#pragma unroll
+    for (int x = 0; x <= WARPS; ++x) {
+      if (x < warp) upto += scan[x];
+      total += scan[x];
+    }
+    total *= a.hk;
+    const long long chunk = max((total + DVM_ATT_UNITS - 1) / DVM_ATT_UNITS, (long long)MIN_TILES);
+    begin = min(total, blockIdx.x * chunk);
+    stop = min(total, begin + chunk);
+    if (begin == stop) {
+      if (threadIdx.x == 0 && !heads_by_pair(a)) *head_of(a, blockIdx.x) = make_int4(0, 0, 0, 0);
+      return;
+    }
+    // the thread whose requests hold tile `begin` walks to it
+    const long long from = (upto - mine) * a.hk, to = upto * a.hk;
+    if (begin >= from && begin < to) {
+      long long at = from;
+      for (int i = threadIdx.x * per;; ++i) {
+        if (per > 1) count = span_of(a, request_at(a, i)).count;
+        const long long after = at + (long long)count * a.hk;
+        if (begin < after) {
+          const long long kvh = (begin - at) / count;
+          scan[8] = i;
+          scan[9] = kvh;
+          scan[10] = at + kvh * count;
+          scan[11] = chunk;
+          scan[12] = stop;
+          break;
+        }
+        at = after;
+      }
+    }
+    __syncthreads();
+    w.request = (int)scan[8];
+    w.kvh = (int)scan[9];
+    w.base = scan[10];
+    w.load(a);
+  }
   w.cut(begin, stop);
 
   if (warp == WARPS) {
