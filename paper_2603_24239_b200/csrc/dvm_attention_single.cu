@@ -6,7 +6,7 @@
 // group of query heads that share them.  So the work is cut by bytes: the tiles of DVM_ATT_TOKEN_TILE tokens of all
 // (request, kv head) pairs form one line, and each of DVM_ATT_UNITS CTAs (two per SM) takes an equal range of it, whatever
 // the lengths are -- they live on the device, so every CTA finds its range itself.  (One request alone: ranges begin where a
-// head's tiles do, so that no CTA ends two pairs: 8000 tokens, 8 kv heads 16.5 -> 15.3 us.)  A pair that lies in one range is
+// head's tiles do, so that no CTA ends two pairs: 8000 tokens, 8 kv heads 16.5 -> 15.3 us, and 14.0 with no scan.)  A pair that lies in one range is
 // finished there; the parts of one that spans several go to the workspace and a second kernel joins them (a dependent
 // launch that starts while the first one drains).  The cut depends on the lengths alone: results do not vary.
 //
@@ -15,7 +15,7 @@
 // by ldmatrix.  Each warp keeps its own maximum, sum and output, so the warps only meet when a pair ends.  The tensor
 // work is far below what the bytes take, which is why tcgen05 with its 128-row tiles and tensor-memory round trips is not
 // used here.  64 requests of up to 8192 tokens, 64 / 8 heads of 128: 212 us, 6.2 TB/s; 32 requests of up to 16384 under a
-// window of 4096, 32 / 32 heads: 330 us, 6.5 TB/s; one request of 8192, 32 / 8 heads: 15 us, of which the bytes take 5.
+// window of 4096, 32 / 32 heads: 330 us, 6.5 TB/s; one request of 8192, 32 / 8 heads: 14 us, of which the bytes take 5.
 // Weights are rounded to bf16 for the second product, their sum is not: the error is that of one bf16
 // rounding per weight, which averages out over the tokens.
 //
