@@ -120,6 +120,33 @@ def test_launches_read_what_the_work_before_them_wrote():
         assert (lengths == 16 * (i + 1) + 1).all() and (positions == 16 * (i + 1)).all() and int(taken) == n
 
 
+def test_launches_wait_for_the_events_of_other_streams():
+    """A kernel of its own stream right before, an event of another stream's long work between them."""
+    n = 16
+    code = dvm.encode_paging(n, 40, 16, n, 4096)
+    cached, fresh, free = ints(np.zeros(n)), ints(np.ones(n)), torch.arange(4096, dtype=I32, device="cuda")
+    outs = [torch.zeros(m, dtype=I32, device="cuda") for m in ((n, 40), n + 1, n, n, n, 1)]
+    other = [torch.zeros_like(o) for o in outs]
+    big = torch.zeros(1 << 26, device="cuda")
+    mine, theirs = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    seen = []
+    for i in range(20):
+        with torch.cuda.stream(theirs):
+            for _ in range(5):
+                big.add_(0.2)
+            cached.copy_((big[:n] + 0.5).to(I32) * 16)
+            done = theirs.record_event()
+        dvm.launch(code, [fresh, fresh, free, *other], mine)
+        mine.wait_event(done)
+        dvm.launch(code, [cached, fresh, free, *outs], mine)
+        with torch.cuda.stream(mine):
+            seen.append(outs[2].clone())
+        theirs.wait_stream(mine)
+    ok()
+    assert all((x == 16 * (i + 1) + 1).all() for i, x in enumerate(seen))
+
+
 @pytest.mark.parametrize("first", ["alone", "memset", "fork", "copy"])
 def test_graphs_with_other_nodes(first):
     """A step (rotary, then attention of single tokens) captured behind nothing, a memset, a fork and a copy."""
