@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(THREADS) dvm_paging_kernel(const __grid_consta
   int* const pages = sm + a.n + 1;      // n + 1: new pages before request i
   int* const cached = sm + 2 * a.n + 2; // n: tokens of request i in the cache
   __shared__ Sums warp_sums[THREADS / 32];
-  grid_wait();
+  grid_wait();  // (no grid_ready: 256 prompts in a chain of launches took 7.5 us with it)
   const int per = (a.n + THREADS - 1) / THREADS, i0 = min(a.n, (int)threadIdx.x * per), i1 = min(a.n, i0 + per);
 
   // Blocks that a request's new rows reach and its cached tokens do not.

@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(THREADS, VEC ? 3 : 2) dvm_rotary_kernel(const 
     dst[u] += at0;
   }
   const int run = at1 - at0;
-  grid_ready();
+  grid_ready();  // (one token in a chain of launches 1.75 us, 2.17 without)
   grid_wait();
 
   struct Place { int pos, slot; };
