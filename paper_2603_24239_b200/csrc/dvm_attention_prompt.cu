@@ -140,7 +140,8 @@ __device__ __forceinline__ float max_nan(float a, float b, float c) {
 // 2^x without the special function unit, for part of the weights: the unit's 16 results a cycle are what the weights take
 // longest for, while multiply-adds are to spare.  x = f + r with f the nearest integer (1.5 2^23 added and taken away) and
 // |r| <= 1/2; 2^r by a polynomial of degree 5 fitted for least relative error (1.7e-7 in fp32) with constant term 1, so
-// that x <= -127 gives exactly 0; f is added to the exponent field.  For x below 128; not for NaN (see `top` below).
+// that x <= -127 gives exactly 0; f is added to the exponent field.  For x below 128.  A NaN gives 0: it comes only from a row's
+// maximum of NaN or +inf, which makes the other weights and their sum NaN (see `top` below).
 __device__ __forceinline__ float2 ex2_by_polynomial(float2 x) {
   const float2 big = make_float2(12582912.f, 12582912.f);
   x.x = fmaxf(x.x, -127.f);
@@ -581,13 +582,13 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       tmem_landed(s_lo);
       tmem_landed(hi_now);
       if (!whole) { hide(s_lo, seen[0]); hide(hi_now, seen[1]); }
-      // a NaN score makes the maximum NaN and with it every weight of the row, as the quotient has it
+      // a NaN score makes the maximum NaN and with it the weights of the row and their sum, as the quotient has it; +inf does too
       const float top = highest(hi_now, highest(s_lo, -INFINITY));
       const float m_new = max_nan(m, top);
       if (__any_sync(0xffffffffu, (m_new - m) * c > GROWTH || m_new != m_new)) {  // (from -inf: yes, unless it stays there)
         const float keep = m_new == m ? 1.f : ex2((m - m_new) * c);
         l *= keep;
-        m = m_new;
+        m = m_new == INFINITY ? NAN : m_new;  // (inf - inf in the exponent: NaN, which not every weight's arithmetic would keep)
         if (t > 0) {
           // PV(t - 1) is done; PV(t) waits for this tile's weights
           if (!__all_sync(0xffffffffu, mbar_poll(bar_o + 16 * x + 8 * (b ^ 1), ((g + t - 1) >> 1) & 1, abort_flag))) return false;
