@@ -91,6 +91,7 @@ int dvm_encode_rotary(const dvm_rotary_desc* d, void* code, size_t code_capacity
  *   and a page id table[i, s / page_size] inside [0, pages);
  * for query head h, with kv head h / (q_heads / kv_heads):
  *   out[t, h] = sum_s softmax_s(scale * q[t, h] . k[s]) v[s];   a row that sees nothing gives 0.
+ * (Infinite scores as the quotient has them: one of +inf makes its row NaN, and so do scores that are all -inf.)
  * Tokens a row does not see have no influence on it, whatever the cache holds there.  Query rows outside every request
  * are left as they were in `out`, and so are a request's rows beyond the first max_q.
  * fp32 accumulation; the bf16 kernels round the unnormalised probabilities to bf16 for the second product.

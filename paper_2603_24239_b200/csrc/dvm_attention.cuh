@@ -57,10 +57,12 @@ __device__ void attend_row(const Args& a, int request, long long pos, int row, i
   const long long end = min(pos + 1, held);                                   // visible: s < end and (s >= low or s < sinks)
   const long long low = a.window ? max(0ll, pos - a.window + 1) : 0;
   float m = -INFINITY, sum = 0.f;
+  bool any = false;  // the row sees a token
   for (long long s = 0; s < end; ++s) {
     if (s >= a.sinks && s < low) { s = low - 1; continue; }
     const int page = table[s >> a.page_log];
     if (page < 0 || page >= a.pages) { s |= (1ll << a.page_log) - 1; continue; }  // the whole page is hidden
+    any = true;
     const long long off = s & ((1ll << a.page_log) - 1);
     const T* k = (const T*)a.k + page * a.ks[0] + off * a.ks[1] + kvh * a.ks[2];
     float x = 0.f;
@@ -78,7 +80,7 @@ __device__ void attend_row(const Args& a, int request, long long pos, int row, i
     sum = sum * keep + p;
     m = m_new;
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const float inv = any ? 1.f / sum : 0.f;  // (tokens, but every score -inf: 0 / 0)
   const long long at = row * a.os[0] + head * a.os[1];
 #pragma unroll
   for (int e = 0; e < 8; ++e)

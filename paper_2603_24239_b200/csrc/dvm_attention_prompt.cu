@@ -502,6 +502,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     const int hi_at = cut(min(p0 + tok, held - 1)), lo_at = a.window ? max(0, cut(p0 + tok - a.window + 1)) : 0;
     const int all_hi = cut(min(p0, held - 1)), all_lo = a.window ? max(0, cut(p0 + n_rows - a.window)) : 0;
     float m = -INFINITY, l = 0.f;
+    uint32_t any = 0;  // tokens that this row sees
     if (row == 0) dirty[4 * x + ((k + 2) & 3)] = 0;  // (block k - 2 is through in every warp, or k were not here; k + 2 not before all let k go)
     // The scores of tile t + 1 are on their way while the second half of tile t's weights is formed: the lower half goes to
     // the registers that tile t's lower half has left, the upper half to those of the tile before.
@@ -568,6 +569,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
       }
+      any |= seen[0] | seen[1];
       auto hide = [&](float* s, uint32_t bits) {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
@@ -660,14 +662,14 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       tc_fence_after();
     }
     if (ok && n_rows > 0) {
-      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const float inv = 1.f / l;  // (tokens, but every score -inf: 0 / 0)
       const long long at = (long long)(w[B_ROW0] + x * tokens + tok) * a.os[0] + (long long)(w[B_KVH] * a.group + head) * a.os[1];
 #pragma unroll
       for (int q = 0; q < DP / 32; ++q) {
         float o[32];
         if (nx > 0) { tmem_load32(t_o + 32 * q, o); tmem_landed(o); }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) o[i] = nx > 0 && l != 0.f ? o[i] * inv : 0.f;
+        for (int i = 0; i < 32; ++i) o[i] = any ? o[i] * inv : 0.f;
         if (tok >= n_rows) continue;
         if (a.out_vec) {
           __nv_bfloat16* const out = (__nv_bfloat16*)a.out + at + 32 * q;

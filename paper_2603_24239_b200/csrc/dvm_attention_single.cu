@@ -24,6 +24,7 @@
 // the product, so nothing they hold, NaN included, reaches the result.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <float.h>
 
 #include "dvm_attention.cuh"
 #include "dvm_attention_launch.h"
@@ -307,6 +308,7 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
 #pragma unroll
         for (int x = 0; x < 4; ++x) o[n][x] = 0.f;
       float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+      uint32_t any = 0;  // tokens of this lane that the rows see
 
       for (int j = w.j0; j < w.j1; ++j) {
         ok = __all_sync(0xffffffffu, ok && mbar_wait(bar_full + 8 * stage, phase, abort_flag));
@@ -340,6 +342,7 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
             }
           }
         }
+        any |= keep[0] | keep[1];
         uint32_t p[4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {  // rows g and g + 8
@@ -375,8 +378,11 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
       }
 
       // ---- the pair's part is done: the four warps' results become one ----
+      // From here on a maximum of -inf says that no token was seen; tokens whose scores are all -inf have the lowest finite one.
+      any = __any_sync(0xffffffffu, any != 0);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
+        if (any) m[h] = fmaxf(m[h], -FLT_MAX);
         l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
         l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
         if (t4 == 0) {
@@ -426,7 +432,7 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
       float* const part = slot_of(a, blockIdx.x, slot);
       for (int head = warp; head < a.group; head += WARPS) {
         const float top = stats[2 * WARPS * 16 + head], all = stats[(2 * WARPS + 1) * 16 + head];
-        const float by = all == 0.f ? 0.f : 1.f / all;
+        const float by = top == -INFINITY ? 0.f : 1.f / all;  // (tokens, but every score -inf: 0 / 0)
         const long long at = w.r.s0 * a.os[0] + ((long long)w.kvh * a.group + head) * a.os[1];
 #pragma unroll
         for (int e = 0; e < DP / 32; ++e) {
@@ -538,7 +544,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) dvm_attention_join_kernel(con
     float all = 0.f;
 #pragma unroll
     for (int x = 0; x < JOIN_WARPS; ++x) all += sums[x][threadIdx.x];
-    put(a.out, a.out_bf16, row * a.os[0] + ((long long)kvh * a.group + h) * a.os[1] + threadIdx.x, l == 0.f ? 0.f : all / l);
+    put(a.out, a.out_bf16, row * a.os[0] + ((long long)kvh * a.group + h) * a.os[1] + threadIdx.x, m == -INFINITY ? 0.f : all / l);
   }
 }
 
