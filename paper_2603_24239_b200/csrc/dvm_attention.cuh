@@ -41,9 +41,10 @@ __device__ __forceinline__ void put(void* out, int bf16, long long at, float v) 
 }
 
 // One row of one head, by one warp: lane l holds the elements l, l + 32, ... of q, of the sum and of each key.  Running
-// maximum and sum over the visible tokens, one after another.
+// maximum and sum over the visible tokens, one after another.  beat: a word of shared memory that is counted up on the way, for
+// a kernel in which others wait meanwhile.
 template <class T>
-__device__ void attend_row(const Args& a, int request, long long pos, int row, int head) {
+__device__ void attend_row(const Args& a, int request, long long pos, int row, int head, uint32_t* beat = nullptr) {
   const int lane = threadIdx.x & 31, kvh = head / a.group;
   const int* table = a.table + (long long)request * a.max_blocks;
   const T* q = (const T*)a.q + row * a.qs[0] + head * a.qs[1];
@@ -58,7 +59,9 @@ __device__ void attend_row(const Args& a, int request, long long pos, int row, i
   const long long low = a.window ? max(0ll, pos - a.window + 1) : 0;
   float m = -INFINITY, sum = 0.f;
   bool any = false;  // the row sees a token
+  uint32_t steps = 0;
   for (long long s = 0; s < end; ++s) {
+    if (beat && (++steps & 255) == 0 && lane == 0) atomicAdd(beat, 1u);
     if (s >= a.sinks && s < low) { s = low - 1; continue; }
     const int page = table[s >> a.page_log];
     if (page < 0 || page >= a.pages) { s |= (1ll << a.page_log) - 1; continue; }  // the whole page is hidden

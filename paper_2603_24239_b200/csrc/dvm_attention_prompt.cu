@@ -32,8 +32,9 @@
 // the power cap; 32 / 32 heads under a window of 1024: 191 us; 12 ragged prompts on cached ones, 40 / 8 heads of 96: 135 us;
 // 8 prompts of up to 1531 tokens, 16 / 4 heads of 64, window 128: 41 us.
 //
-// Every wait is bounded; when one runs out the CTA raises its abort flag, all roles leave, what is in flight is awaited,
-// tensor memory is released and the status word reports DVM_ERR_DEVICE_TIMEOUT.
+// Every wait is bounded: it gives up when 2 s pass in which the CTA neither fetched a tile nor went on doing rows again (one
+// warp, 32 rows, token after token: 134 ms on 8192 tokens, 2.5 s on 153600).  Then the CTA raises its abort flag, all roles
+// leave, what is in flight is awaited, tensor memory is released and the status word reports DVM_ERR_DEVICE_TIMEOUT.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -67,7 +68,7 @@ struct PromptSmem {
   static constexpr uint32_t STAGES = DP == 128 ? 10 : 16;
   static constexpr uint32_t RING = 2 * Q_TILE;                   // behind the queries of both row tiles
   static constexpr uint32_t BARS = RING + STAGES * STAGE;        // see the kernel
-  static constexpr uint32_t WORDS = BARS + 16 * STAGES + 192;    // tensor memory address, abort, dirty[2][4], holes[]
+  static constexpr uint32_t WORDS = BARS + 16 * STAGES + 192;    // tensor memory address, abort, dirty[2][4], holes[], signs of work
   static constexpr uint32_t WORK = WORDS + 48 + 4 * HOLES;       // two descriptions of blocks, the answer of a cancelled launch
   static constexpr uint32_t BYTES = WORK + 2 * 64 + 16 + 1024;
   static_assert(WORK % 16 == 0, "an answer is 16 bytes, aligned");
@@ -180,6 +181,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
   volatile uint32_t* const abort_flag = words + 1;
   volatile uint32_t* const dirty = words + 2;  // [x][block mod 4]
   volatile uint32_t* const holes = words + 10;
+  volatile uint32_t* const signs = words + 10 + HOLES;  // of work: tiles fetched, tokens that rows were done again with
   volatile int* const work = (volatile int*)(sm + S::WORK);
   const int tokens = PT / a.group;  // of a row tile
   const long long held = (long long)a.max_blocks << a.page_log;
@@ -203,7 +205,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     }
     mbar_init(bar_c, 1);
     for (int i = 0; i < 8; ++i) dirty[i] = 0;
-    *abort_flag = 0;
+    *abort_flag = signs[0] = signs[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   // Rows that no head of the group falls on (128 is not a multiple of every group) are never loaded: zeros, or what the last
@@ -232,7 +234,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
   enum { B_REQUEST, B_KVH, B_ROW0, B_TOKENS, B_N0, B_N1, B_NS, B_FIRST, B_END, B_LOW, B_P_LO, B_P_HI };
   // the k-th block of this CTA, or none (also when a wait ran out)
   auto take = [&](int k) -> volatile const int* {
-    const bool got = mbar_wait_flat(bar_w + 8 * (k & 1), (k >> 1) & 1, abort_flag);
+    const bool got = mbar_wait_flat(bar_w + 8 * (k & 1), (k >> 1) & 1, abort_flag, signs);
     volatile const int* const w = work + 16 * (k & 1);
     return __all_sync(0xffffffffu, got) && w[B_TOKENS] > 0 ? w : nullptr;
   };
@@ -300,7 +302,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       const int tok0 = __shfl_sync(0xffffffffu, upto - 1 - at, src) * 2 * tokens, request = __shfl_sync(0xffffffffu, who, src);
       const bool beyond = !owner && id >= 0;  // (the grid is sized for the most blocks that `rows` rows can make)
       if (!beyond) {
-      ok = k < 2 || mbar_wait_flat(bar_we + 8 * (k & 1), ((k >> 1) & 1) ^ 1, abort_flag);
+      ok = k < 2 || mbar_wait_flat(bar_we + 8 * (k & 1), ((k >> 1) & 1) ^ 1, abort_flag, signs);
       if (!__all_sync(0xffffffffu, ok)) break;
       if (lane == 0) {
         volatile int* const w = work + 16 * (k & 1);
@@ -335,7 +337,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer), "r"(bar_c) : "memory");
       }
       __syncwarp();
-      ok = __all_sync(0xffffffffu, mbar_wait_flat(bar_c, asked++ & 1, abort_flag));
+      ok = __all_sync(0xffffffffu, mbar_wait_flat(bar_c, asked++ & 1, abort_flag, signs));
       uint32_t got = 0, cta = 0;
       asm volatile(
           "{\n\t.reg .pred p;\n\t.reg .b128 r;\n\tld.shared.b128 r, [%2];\n\tclusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
@@ -369,7 +371,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         return page >= 0 && page < a.pages ? page : -1;
       };
       int page = page_of(0);
-      ok = __all_sync(0xffffffffu, q_loads == 0 || mbar_wait_flat(bar_qe, (q_loads - 1) & 1, abort_flag));
+      ok = __all_sync(0xffffffffu, q_loads == 0 || mbar_wait_flat(bar_qe, (q_loads - 1) & 1, abort_flag, signs));
       if (!ok) break;
       if (lane == 0) {
         const int active = n_tok > tokens ? 2 : 1;
@@ -386,11 +388,14 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         const int off = (int)(((long long)tile_at(j) * KT + ((long long)lane << copy_log)) & ((1ll << a.page_log) - 1));
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
-          ok = __all_sync(0xffffffffu, ok && mbar_wait_flat(bar_empty + 8 * f_stage, f_phase ^ 1, abort_flag));
+          ok = __all_sync(0xffffffffu, ok && mbar_wait_flat(bar_empty + 8 * f_stage, f_phase ^ 1, abort_flag, signs));
           if (!ok) break;
           const uint32_t full = bar_full + 8 * f_stage, at = base + S::RING + f_stage * S::STAGE;
           if (lane == 0) {
-            if (kv == 0) holes[(seen + j) % HOLES] = missing;
+            if (kv == 0) {
+              holes[(seen + j) % HOLES] = missing;
+              signs[0] = (uint32_t)(seen + j);  // (a block of a very long cache: others wait for its end)
+            }
             mbar_expect_tx(full, S::STAGE);
           }
           __syncwarp();
@@ -448,9 +453,9 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       const int n_tiles = max(w[B_N0], w[B_N1]), nx = w[x ? B_N1 : B_N0];
       let_go(k);
       if (n_tiles == 0) continue;
-      ok = __all_sync(0xffffffffu, mbar_wait_flat(bar_q, queries++ & 1, abort_flag));
+      ok = __all_sync(0xffffffffu, mbar_wait_flat(bar_q, queries++ & 1, abort_flag, signs));
       auto scores = [&](int t) -> bool {  // QK(t), if this row tile walks that far; else the keys are let go unread
-        if (!__all_sync(0xffffffffu, mbar_wait_flat(bar_full + 8 * k_stage, k_phase, abort_flag))) return false;
+        if (!__all_sync(0xffffffffu, mbar_wait_flat(bar_full + 8 * k_stage, k_phase, abort_flag, signs))) return false;
         tc_fence_after();
         if (t < nx) qk((g + t) & 1);
         else if (leader) mbar_arrive(bar_empty + 8 * k_stage);
@@ -464,8 +469,8 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       for (int t = 0; ok && t < min(2, n_tiles); ++t) ok = scores(t);
       for (int t = 0; ok && t < n_tiles; ++t) {
         const int b = (g + t) & 1;
-        ok = mbar_wait_flat(bar_full + 8 * v_stage, v_phase, abort_flag);
-        if (t < nx) ok = ok && mbar_wait_flat(bar_p + 16 * x + 8 * b, ((g + t) >> 1) & 1, abort_flag);
+        ok = mbar_wait_flat(bar_full + 8 * v_stage, v_phase, abort_flag, signs);
+        if (t < nx) ok = ok && mbar_wait_flat(bar_p + 16 * x + 8 * b, ((g + t) >> 1) & 1, abort_flag, signs);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tc_fence_after();
@@ -508,7 +513,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     // the registers that tile t's lower half has left, the upper half to those of the tile before.
     float s_lo[32], s_hi[2][32];
     auto scores = [&](int t) -> bool {  // tile t's scores are in tensor memory
-      const bool got = mbar_poll(bar_s + 16 * x + 8 * ((g + t) & 1), ((g + t) >> 1) & 1, abort_flag);
+      const bool got = mbar_poll(bar_s + 16 * x + 8 * ((g + t) & 1), ((g + t) >> 1) & 1, abort_flag, signs);
       tc_fence_after();
       return __all_sync(0xffffffffu, got);
     };
@@ -537,7 +542,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         // The values of this tile, two threads per token.  Hidden tokens meet weights of 0, which does it unless their values
         // are not finite: then they are cleared if no row of the CTA sees the token, else the block's rows are done again.
         const uint32_t vi = 2 * (seen_tiles + t) + 1;
-        if (!__all_sync(0xffffffffu, mbar_wait_flat(bar_full + 8 * (vi % S::STAGES), (vi / S::STAGES) & 1, abort_flag))) return false;
+        if (!__all_sync(0xffffffffu, mbar_wait_flat(bar_full + 8 * (vi % S::STAGES), (vi / S::STAGES) & 1, abort_flag, signs))) return false;
         const int vrow = row & (KT - 1);
         uint8_t* const v = sm + S::RING + (vi % S::STAGES) * S::STAGE + vrow * 128;
         auto chunk_of = [&](uint32_t i) -> uint4* {
@@ -593,7 +598,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         m = m_new == INFINITY ? NAN : m_new;  // (inf - inf in the exponent: NaN, which not every weight's arithmetic would keep)
         if (t > 0) {
           // PV(t - 1) is done; PV(t) waits for this tile's weights
-          if (!__all_sync(0xffffffffu, mbar_poll(bar_o + 16 * x + 8 * (b ^ 1), ((g + t - 1) >> 1) & 1, abort_flag))) return false;
+          if (!__all_sync(0xffffffffu, mbar_poll(bar_o + 16 * x + 8 * (b ^ 1), ((g + t - 1) >> 1) & 1, abort_flag, signs))) return false;
           tc_fence_after();
 #pragma unroll
           for (int q = 0; q < DP / 32; ++q) {
@@ -658,7 +663,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     }
     const int last = g + nx - 1;
     if (ok && nx > 0) {
-      ok = __all_sync(0xffffffffu, mbar_poll(bar_o + 16 * x + 8 * (last & 1), (last >> 1) & 1, abort_flag));
+      ok = __all_sync(0xffffffffu, mbar_poll(bar_o + 16 * x + 8 * (last & 1), (last >> 1) & 1, abort_flag, signs));
       tc_fence_after();
     }
     if (ok && n_rows > 0) {
@@ -701,7 +706,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     __syncwarp();
     if (ok && dirty[4 * x + (k & 3)])
       for (int r = (warp & 3) * 32; r < min((warp & 3) * 32 + 32, n_rows * a.group); ++r)
-        attend_row<__nv_bfloat16>(a, w[B_REQUEST], position() + r / a.group, w[B_ROW0] + x * tokens + r / a.group, w[B_KVH] * a.group + r % a.group);
+        attend_row<__nv_bfloat16>(a, w[B_REQUEST], position() + r / a.group, w[B_ROW0] + x * tokens + r / a.group, w[B_KVH] * a.group + r % a.group, (uint32_t*)signs + 1);
     g += nx;
     seen_tiles += max(w[B_N0], w[B_N1]);
     let_go(k);

@@ -85,13 +85,17 @@ static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity
 }
 // The same without a call, for kernels that deal out registers by role (setmaxnreg), where a callee has no count of its own;
 // and with the clock and the flag looked at every 16th time only: a read of the clock takes longer than most of these waits.
-__device__ __forceinline__ bool mbar_wait_flat(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag) {
+// The limit runs from the last sign of work: two words of the CTA that roles count up while they do what others may wait
+// for at length.
+__device__ __forceinline__ bool mbar_wait_flat(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, const volatile uint32_t* work) {
   unsigned long long t0 = 0;
+  uint32_t done = 0;
   for (uint32_t spin = 0; spin < WAIT_SPINS; ++spin) {
     if (mbar_try(bar, parity)) return true;
     if ((spin & 15) != 15) continue;
     if (*abort_flag) return false;
-    if (t0 == 0) t0 = gtimer();
+    const uint32_t now = work[0] + work[1];
+    if (t0 == 0 || now != done) { t0 = gtimer(); done = now; spin = 15; }
     else if (gtimer() - t0 > WAIT_NS) break;
   }
   *abort_flag = 1;
@@ -99,13 +103,15 @@ __device__ __forceinline__ bool mbar_wait_flat(uint32_t bar, uint32_t parity, vo
 }
 // The same for waits that are short and on the critical path: the first polls do not sleep (a warp that sleeps takes
 // hundreds of cycles to be back).
-__device__ __forceinline__ bool mbar_poll(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag) {
+__device__ __forceinline__ bool mbar_poll(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, const volatile uint32_t* work) {
   unsigned long long t0 = 0;
+  uint32_t done = 0;
   for (uint32_t spin = 0; spin < WAIT_SPINS; ++spin) {
     if (spin < 64 ? mbar_test(bar, parity) : mbar_try(bar, parity)) return true;
     if ((spin & 63) != 63) continue;
     if (*abort_flag) return false;
-    if (t0 == 0) t0 = gtimer();
+    const uint32_t now = work[0] + work[1];
+    if (t0 == 0 || now != done) { t0 = gtimer(); done = now; spin = 63; }
     else if (gtimer() - t0 > WAIT_NS) break;
   }
   *abort_flag = 1;
