@@ -373,7 +373,9 @@ int dvm_launch_checked(const void* code, size_t code_size, void* const* tensors,
 /* Self-test of the bounded device-side waits (no counterpart in the paper): launches one CTA that waits on
  * an mbarrier nobody completes, with the very wait routine of the interpreter (which = 0) or of the matmul
  * kernel (which = 1), or on a tile counter nobody advances with the level wait of dvm_launch_stacked_levels
- * (which = 2).  The wait gives up after its limit (about 2 s), the kernel sets the status word and
+ * (which = 2), or with the two waits of the attention kernels of dvm_serving.h (which = 3, 4; 5: what they do at
+ * the end of a CTA that gave up, which is to wait for the copies in flight: a ring of which one fill lands 20 ms
+ * late).  The wait gives up after its limit (about 2 s), the kernel sets the status word and
  * returns: dvm_last_device_status then reports DVM_ERR_DEVICE_TIMEOUT and the context stays usable. */
 int dvm_selftest_bounded_wait(int which, void* cuda_stream);
 /* Synchronises `cuda_stream`, then reads and clears the device status word of

@@ -9,6 +9,7 @@
 #include "dvm_attention.cuh"
 #include "dvm_attention_launch.h"
 #include "dvm_launch.h"
+#include "dvm_sm100.cuh"
 
 namespace dvm {
 namespace att {
@@ -121,6 +122,56 @@ int dvm_launch_attention(const dvm_attention_desc& d, void* const* t, cudaStream
   DVM_CUDA(cudaGetLastError());
   dvm_count_launch();
   t_last_kernel = 0;
+  return DVM_OK;
+}
+
+// ---- self-tests of the attention kernels' bounded waits (see dvm_selftest_bounded_wait) ----
+namespace dvm {
+namespace att {
+using namespace sm100;
+constexpr int WAIT_FLAT = 3, WAIT_POLL = 4, WAIT_DRAIN = 5;  // `which`
+__global__ void dvm_selftest_attention_wait_kernel(int which, unsigned int* status) {
+  constexpr uint32_t STAGES = 3, LATE_NS = 20000000;
+  __shared__ __align__(8) unsigned long long bars[1 + STAGES];
+  __shared__ volatile uint32_t words[3];  // abort flag, signs of work
+  const uint32_t never = smem_u32(bars), full = never + 8;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    words[0] = words[1] = words[2] = 0;
+    mbar_init(never, 2);  // two arrivals expected, one ever made: the phase never completes
+    for (uint32_t s = 0; s < STAGES; ++s) mbar_init(full + 8 * s, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    mbar_arrive(never);
+    mbar_arrive(full);       // five fills of three stages, of which the last will land long after the wait below has run out:
+    mbar_arrive(full + 8);   // in stages 0 and 1 the second one
+    mbar_arrive(full + 16);
+    mbar_arrive(full);
+  }
+  __syncthreads();
+  bool ok = true;
+  if (warp == 0) ok = which == WAIT_FLAT ? mbar_wait_flat(never, 0, words, words + 1) : which == WAIT_POLL ? mbar_poll(never, 0, words, words + 1) : mbar_wait(never, 0, words);
+  __syncthreads();
+  if (!words[0]) return;
+  if (which == WAIT_DRAIN) {
+    if (warp == 1 && lane == 0) {  // the fill that is late
+      const unsigned long long t0 = gtimer();
+      for (uint32_t i = 0; i < WAIT_SPINS && gtimer() - t0 < LATE_NS; ++i) {}
+      mbar_arrive(full + 8);
+    }
+    if (threadIdx.x == 0) {
+      mbar_drain(full, STAGES, 5, 2, 1, words);
+      ok = !(mbar_test(full, 1) && mbar_test(full + 8, 1) && mbar_test(full + 16, 0));
+    }
+  }
+  if (threadIdx.x == 0) atomicMax(status, (unsigned int)(ok ? ST_BAD_CODE : ST_TIMEOUT));
+}
+}  // namespace att
+}  // namespace dvm
+
+int dvm_selftest_attention_wait(int which, unsigned int* status, cudaStream_t stream) {
+  dvm::att::dvm_selftest_attention_wait_kernel<<<1, 64, 0, stream>>>(which, status);
+  DVM_CUDA(cudaGetLastError());
+  dvm_count_launch();
   return DVM_OK;
 }
 

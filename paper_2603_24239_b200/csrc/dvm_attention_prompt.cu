@@ -243,8 +243,8 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     if (lane == 0) mbar_arrive(bar_we + 8 * (k & 1));
   };
 
-  uint32_t issued = 0, f_stage = 0, f_phase = 0;  // the fetching warp's ring and queries, kept for the abort path
-  int q_loads = 0;
+  uint32_t issued = 0, f_stage = 0, f_phase = 0;  // the fetching warp's ring and queries, and the answers asked for, kept for the abort path
+  int q_loads = 0, asked = 0;
   if (warp == 11) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
     // ---------------- blocks: those of all requests in a row, a request's last block first ----------------
@@ -264,7 +264,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     const uint32_t answer = base + S::WORK + 128;
     bool ok = true;
     long long id = blockIdx.x;
-    for (int k = 0, asked = 0; ok;) {
+    for (int k = 0; ok;) {
       const long long block = id < 0 ? -1 : id / a.hk;
       bool any = id >= 0;
       if (any && block < before) chunk = -32, before = all = 0, sorted = -1;  // (an order that the hardware does not promise)
@@ -718,12 +718,10 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
   __syncthreads();
   if (*abort_flag) {
     if (warp == 10 && lane == 0) {  // the latest fill of every stage, and the queries
-      for (uint32_t k = min(issued, S::STAGES); k > 0; --k) {
-        if (f_stage == 0) { f_stage = S::STAGES - 1; f_phase ^= 1; } else --f_stage;
-        if (!mbar_try(bar_full + 8 * f_stage, f_phase)) mbar_spin(bar_full + 8 * f_stage, f_phase, abort_flag, DRAIN_NS, false);
-      }
-      if (q_loads > 0 && !mbar_try(bar_q, (q_loads - 1) & 1)) mbar_spin(bar_q, (q_loads - 1) & 1, abort_flag, DRAIN_NS, false);
+      mbar_drain(bar_full, S::STAGES, issued, f_stage, f_phase, abort_flag);
+      mbar_drain(bar_q, 1, q_loads, 0, q_loads & 1, abort_flag);
     }
+    if (warp == 11 && lane == 0) mbar_drain(bar_c, 1, asked, 0, asked & 1, abort_flag);  // (a cancelled launch's answer)
     if ((warp == 8 || warp == 9) && elect_one()) {  // (the lanes that issued)
       umma_commit(bar_drain + 8 * (warp - 8));
       if (!mbar_try(bar_drain + 8 * (warp - 8), 0)) mbar_spin(bar_drain + 8 * (warp - 8), 0, abort_flag, DRAIN_NS, false);

@@ -227,11 +227,10 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
   }
   w.cut(begin, stop);
 
+  uint32_t f_stage = 0, f_phase = 0, issued = 0;  // the fetching warp's ring, kept for the abort path
   if (warp == WARPS) {
     // ---------------- one warp fetches: a copy of min(page, TILE) tokens per lane and 64 elements ----------------
     const int copy_log = min(a.page_log, 6), copies = TILE >> copy_log;
-    int stage = 0;
-    uint32_t phase = 0, issued = 0;
     bool ok = true;
     for (;;) {
       const int* table = a.table + (long long)w.request * a.max_blocks;
@@ -245,12 +244,12 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
       int page = page_of(w.j0);
       for (int j = w.j0; ok && j < w.j1; ++j) {
         const int page_next = page_of(j + 1);  // (its latency hides behind the wait below)
-        ok = mbar_wait(bar_empty + 8 * stage, phase ^ 1, abort_flag);
+        ok = mbar_wait(bar_empty + 8 * f_stage, f_phase ^ 1, abort_flag);
         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
         const uint32_t holes = __ballot_sync(0xffffffffu, lane < copies && page < 0);
-        const uint32_t full = bar_full + 8 * stage, at = base + stage * S::STAGE;
+        const uint32_t full = bar_full + 8 * f_stage, at = base + f_stage * S::STAGE;
         if (lane == 0) {
-          bad[stage] = holes;
+          bad[f_stage] = holes;
           mbar_expect_tx(full, S::STAGE);
         }
         __syncwarp();
@@ -265,17 +264,11 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
           }
         }
         ++issued;
-        if (++stage == S::STAGES) { stage = 0; phase ^= 1; }
+        if (++f_stage == S::STAGES) { f_stage = 0; f_phase ^= 1; }
         page = page_next;
       }
       if (!ok || w.base + w.length >= stop) break;
       w.next(a, begin, stop);
-    }
-    if (!ok && lane == 0) {  // given up: the copies in flight land before the CTA ends (bounded again)
-      for (uint32_t k = min(issued, (uint32_t)S::STAGES); k > 0; --k) {
-        if (stage == 0) { stage = S::STAGES - 1; phase ^= 1; } else --stage;
-        if (!mbar_try(bar_full + 8 * stage, phase)) mbar_wait_slow(bar_full + 8 * stage, phase, abort_flag, DRAIN_NS, false);
-      }
     }
     __syncwarp();
   } else {
@@ -460,7 +453,11 @@ dvm_attention_single_kernel(const __grid_constant__ CUtensorMap tm_k, const __gr
       w.next(a, begin, stop);
     }
   }
-  if (*abort_flag && lane == 0) atomicMax(a.status, (unsigned int)ST_TIMEOUT);
+  __syncthreads();
+  if (*abort_flag) {  // whoever's wait ran out: the copies in flight land first
+    if (threadIdx.x == WARPS * 32) mbar_drain(bar_full, S::STAGES, issued, f_stage, f_phase, abort_flag);
+    if (threadIdx.x == 0) atomicMax(a.status, (unsigned int)ST_TIMEOUT);
+  }
 }
 
 // Joins the parts of a pair that spans several ranges: one CTA per head (grid x) and query head of the pair (grid y).

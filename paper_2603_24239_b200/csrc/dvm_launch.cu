@@ -1027,6 +1027,7 @@ __global__ void dvm_selftest_level_wait_kernel(unsigned int* status) {
 }  // namespace
 
 int dvm_selftest_mm_wait(unsigned int* status, cudaStream_t stream);
+int dvm_selftest_attention_wait(int which, unsigned int* status, cudaStream_t stream);
 
 extern "C" int dvm_selftest_bounded_wait(int which, void* cuda_stream) {
   DvmDeviceInfo dev;
@@ -1039,6 +1040,7 @@ extern "C" int dvm_selftest_bounded_wait(int which, void* cuda_stream) {
     return DVM_OK;
   }
   if (which == 1) return dvm_selftest_mm_wait(dev.scratch, (cudaStream_t)cuda_stream);
+  if (which >= 3 && which <= 5) return dvm_selftest_attention_wait(which, dev.scratch, (cudaStream_t)cuda_stream);
   if (which == 2) {
     dvm_selftest_level_wait_kernel<<<1, 32, 0, (cudaStream_t)cuda_stream>>>(dev.scratch);
     DVM_CUDA(cudaGetLastError());

@@ -122,6 +122,16 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   return mbar_wait_slow(bar, parity, abort_flag, WAIT_NS, true);
 }
 
+// For the end of a CTA that gave up: copies in flight land before it leaves its shared memory to the next one.  Waits (bounded) for
+// the latest fill of every stage of a ring, whose next fill, with the wait parity `phase`, would have been stage `stage`.  By
+// one thread, once every role is through: no fill is issued after that.
+__device__ __forceinline__ void mbar_drain(uint32_t bar_full, uint32_t stages, uint32_t issued, uint32_t stage, uint32_t phase, volatile uint32_t* abort_flag) {
+  for (uint32_t k = issued < stages ? issued : stages; k > 0; --k) {
+    if (stage == 0) { stage = stages - 1; phase ^= 1; } else --stage;
+    if (!mbar_try(bar_full + 8 * stage, phase)) mbar_spin(bar_full + 8 * stage, phase, abort_flag, DRAIN_NS, false);
+  }
+}
+
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
   asm volatile(
       "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
