@@ -234,6 +234,10 @@ void dvm_set_lean_kernel(int on);
  * realignment of reads); 6 two slots and aligned operands with row-by-row copies; 7 as 5 for rows that fill the
  * tile's slots exactly (no slot masks); 8 as 6 for such rows; 9 aligned programs with one tile slot.  DVM_ERR_INVALID_ARG before the thread's first launch. */
 int dvm_last_launch_variant(int out[8]);
+/* Launches on the current device so far that took one of the library's 504 work-queue slots (for tests and tools): stacked
+ * launches, and programs with one tile slot on the general interpreter.  Slots go round, so that many such launches may be pending
+ * or captured at a time; no other launch takes one. */
+int dvm_queue_slots_taken(int64_t* taken);
 
 /* Matmul launches (Sec. 4.2, matrix operations): the tiles of a last, partial wave are shared along k -- a small
  * wave gives each tile up to four CTAs (or CTA pairs), a larger one is cut into equal ranges of its k blocks over

@@ -85,6 +85,7 @@ _sig = {
     "dvm_get_min_resident_ctas": ([], _i),
     "dvm_set_lean_kernel": ([_i], None),
     "dvm_last_launch_variant": ([C.POINTER(C.c_int)], _i),
+    "dvm_queue_slots_taken": ([C.POINTER(C.c_int64)], _i),
     "dvm_set_stacked_one_slot": ([_i], None),
     "dvm_set_matmul_tail_split": ([_i], None),
     "dvm_set_matmul_cta_pairs": ([_i], None),
@@ -658,6 +659,13 @@ def last_launch_variant() -> dict:
     out = (C.c_int * 8)()
     _check(lib.dvm_last_launch_variant(out), "dvm_last_launch_variant")
     return dict(zip(("V", "large", "single", "ext", "levels", "lean", "heavy", "ctas"), list(out)))
+
+
+def queue_slots_taken() -> int:
+    """dvm_queue_slots_taken: launches on the current device that took a work-queue slot."""
+    out = C.c_int64(0)
+    _check(lib.dvm_queue_slots_taken(C.byref(out)), "dvm_queue_slots_taken")
+    return out.value
 
 
 def set_matmul_cta_pairs(mode: int):

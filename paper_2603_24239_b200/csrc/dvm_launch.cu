@@ -33,7 +33,7 @@ struct DeviceState {
   // resident CTAs per SM, per (kernel variant, bytes of dynamic shared memory / DVM_LOCAL_UNIT): occupancy depends
   // on exactly these two, so a one-slot and a two-slot launch of the same program never share an entry
   std::unordered_map<uint64_t, int> occ;
-  unsigned queue_slot = 0;
+  long long queue_slots_taken = 0;
 };
 
 DeviceState g_dev[MAX_DEVICES];
@@ -60,8 +60,23 @@ int dvm_device_state(DvmDeviceInfo* info) {
   info->scratch = d.scratch;
   info->sm_count = d.sm_count;
   info->device = dev;
-  info->queue_slot = d.queue_slot;
-  d.queue_slot = (d.queue_slot + 1) % QUEUE_SLOTS;
+  return DVM_OK;
+}
+
+// The work-queue counters of a launch that has a queue, and of no other: the slots go round, so a launch that took one without need
+// would bring the next round -- counters that a launch still pending holds -- nearer.
+static unsigned int* take_queue_slot(const DvmDeviceInfo& info) {
+  std::lock_guard<std::mutex> lk(g_mu);
+  return info.scratch + 8 + 4 * (g_dev[info.device].queue_slots_taken++ % QUEUE_SLOTS);
+}
+
+extern "C" int dvm_queue_slots_taken(int64_t* taken) {
+  if (!taken) return DVM_ERR_INVALID_ARG;
+  DvmDeviceInfo dev;
+  const int st = dvm_device_state(&dev);
+  if (st != DVM_OK) return st;
+  std::lock_guard<std::mutex> lk(g_mu);
+  *taken = g_dev[dev.device].queue_slots_taken;
   return DVM_OK;
 }
 
@@ -725,7 +740,7 @@ int launch_vec(int n_programs, const void* const* codes, void* const* const* ten
   P.tile_begin = tile_begin;
   P.row_tiles = row_tiles;
   P.status = dev.scratch;
-  P.queue = dev.scratch + 8 + 4 * dev.queue_slot;
+  P.queue = use_queue ? take_queue_slot(dev) : nullptr;
 
   const bool large = pos > PW_SMALL;
   const size_t smem = ((one_slot ? 1 : 2) * (size_t)units + 1) * DVM_LOCAL_UNIT;  // one spare unit, two tile slots (or one)

@@ -29,10 +29,10 @@ struct DvmDeviceInfo {
   unsigned int* scratch;  // library-owned device words: [0] status, then work-queue counter pairs
   int sm_count;
   int device;
-  unsigned queue_slot;    // work-queue slot reserved for this launch
 };
 
-// Per-device lazy set-up (scratch allocation, occupancy) for the current device.
+// Per-device lazy set-up (scratch allocation, occupancy) for the current device.  Reserves nothing: launches with a work queue
+// take their slot themselves.
 int dvm_device_state(DvmDeviceInfo* info);
 // Lets `kernel` have `bytes` of dynamic shared memory; `done` (a bit per device) spares the driver call from the second time on.
 inline int dvm_allow_smem(const void* kernel, int bytes, int device, std::atomic<uint64_t>* done) {
