@@ -208,15 +208,6 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     *abort_flag = signs[0] = signs[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  // Rows that no head of the group falls on (128 is not a multiple of every group) are never loaded: zeros, or what the last
-  // kernel left there would be scores, and NaN among them sends their warp to the sums for a rescaling at every tile
-  // (12 ragged prompts, 5 heads to a group: 143 us became 187 after some kernels and not after others).
-  const int held_rows = tokens * a.group;
-  for (uint32_t i = threadIdx.x; i < 2 * S::HALVES * (PT - held_rows) * 8; i += PROMPT_THREADS) {
-    const uint32_t r = i / (PT - held_rows);  // tile, half and 16 bytes
-    *(uint4*)(sm + (r / (8 * S::HALVES)) * S::Q_TILE + (r / 8 % S::HALVES) * Q_HALF + (held_rows + i % (PT - held_rows)) * 128 + (r % 8) * 16) = make_uint4(0, 0, 0, 0);
-  }
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   if (warp == 8) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)words)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -506,6 +497,10 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     auto cut = [](long long v) -> int { return (int)max(-1ll, min(v, 0x7fffffffll)); };
     const int hi_at = cut(min(p0 + tok, held - 1)), lo_at = a.window ? max(0, cut(p0 + tok - a.window + 1)) : 0;
     const int all_hi = cut(min(p0, held - 1)), all_lo = a.window ? max(0, cut(p0 + n_rows - a.window)) : 0;
+    // Rows of no query of this request -- other requests' queries, padding, what an earlier kernel left where no head of the group
+    // falls -- have scores too, which are never stored.  They have no say in when their warp rescales its sums: answers would
+    // depend on them in their last bits, and NaN among them would rescale at every tile (12 ragged prompts: 187 us, not 143).
+    const bool live = tok < n_rows;
     float m = -INFINITY, l = 0.f;
     uint32_t any = 0;  // tokens that this row sees
     if (row == 0) dirty[4 * x + ((k + 2) & 3)] = 0;  // (block k - 2 is through in every warp, or k were not here; k + 2 not before all let k go)
@@ -592,7 +587,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
       // a NaN score makes the maximum NaN and with it the weights of the row and their sum, as the quotient has it; +inf does too
       const float top = highest(hi_now, highest(s_lo, -INFINITY));
       const float m_new = max_nan(m, top);
-      if (__any_sync(0xffffffffu, (m_new - m) * c > GROWTH || m_new != m_new)) {  // (from -inf: yes, unless it stays there)
+      if (__any_sync(0xffffffffu, live && ((m_new - m) * c > GROWTH || m_new != m_new))) {  // (from -inf: yes, unless it stays there)
         const float keep = m_new == m ? 1.f : ex2((m - m_new) * c);
         l *= keep;
         m = m_new == INFINITY ? NAN : m_new;  // (inf - inf in the exponent: NaN, which not every weight's arithmetic would keep)
@@ -675,7 +670,7 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
         if (nx > 0) { tmem_load32(t_o + 32 * q, o); tmem_landed(o); }
 #pragma unroll
         for (int i = 0; i < 32; ++i) o[i] = any ? o[i] * inv : 0.f;
-        if (tok >= n_rows) continue;
+        if (!live) continue;
         if (a.out_vec) {
           __nv_bfloat16* const out = (__nv_bfloat16*)a.out + at + 32 * q;
 #pragma unroll
