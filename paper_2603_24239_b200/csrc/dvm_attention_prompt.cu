@@ -208,15 +208,17 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     *abort_flag = signs[0] = signs[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  if (warp == 9 && lane < 3) tma_prefetch(lane == 0 ? &tm_q : lane == 1 ? &tm_k : &tm_v);
+  // Tensor memory too is asked for behind the wait only: the kernel before may still be about to ask for its own on this SM (one
+  // that lets dependents start first), and would wait for what this CTA holds while this CTA waits for it.
+  grid_wait();
   if (warp == 8) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void*)words)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  if (warp == 9 && lane < 3) tma_prefetch(lane == 0 ? &tm_q : lane == 1 ? &tm_k : &tm_v);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  grid_wait();
   const uint32_t tmem = words[0], tmem_o = tmem + 4 * KT;  // S_x at place b: 64 (2 x + b)
 
   // A block: up to 2 x tokens rows of query tokens of one request, for one kv head, described by 16 words of shared memory
