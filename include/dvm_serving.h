@@ -40,8 +40,8 @@ extern "C" {
  *                  max_blocks; they take the entries of `free` in order, request by request, -1 once these run out.
  *                  Other entries are left as they were.
  *   positions[t]   position in its request of the token in row t; -1 in rows behind the last one
- *   slots[t]       table[i, position / P] P + position % P; -1 behind the last row and where there is no page (a
- *                  negative entry, a block beyond max_blocks)
+ *   slots[t]       table[i, position / P] P + position % P; -1 behind the last row, where there is no page (a
+ *                  negative entry, a block beyond max_blocks) and for a slot beyond 2^31 - 2, which no cache has
  *   taken[0]       entries of `free` that were asked for: beyond free_pages, the batch did not fit
  * Tensors: cached [n], fresh [n], free [free_pages] -> table [n, max_blocks] (also read), starts [n + 1], lengths [n],
  * positions [rows], slots [rows], taken [1]; all int32, dense.  A position or length beyond 2^31 - 1 is cut there. */
