@@ -9,6 +9,8 @@
  *   (the query / key / value product: dvm_program_matmul)
  *   dvm_encode_rotary      norms of the query and key heads, rotation by position, keys and values into the cache
  *   dvm_encode_attention   the new tokens attend to the cache: causal, with a sliding window and first tokens that stay
+ * A step that uses all three has a page_size that is a power of two and at least 8: attention takes no other, though
+ * paging and rotary do.
  * Only sizes are encoded.  Lengths, positions, tables live on the device and may change between launches of one code (also
  * between replays of a graph that captured the launch); the kernels stay inside the tensors whatever these hold.
  *
@@ -101,13 +103,16 @@ int dvm_encode_rotary(const dvm_rotary_desc* d, void* code, size_t code_capacity
  * between launches: dvm_tensor_extents gives its bytes (16-byte aligned; any pointer, NULL too, where that is 0).
  * Launches that may run at the same time, in two captured graphs say, need workspaces of their own.
  * bf16 inputs with head_dim a multiple of 8 up to 128, strides that are multiples of 8 and pointers to 16 bytes run on
- * the tensor cores; other inputs on a kernel without them.
+ * the tensor cores; other inputs on a kernel without them, which reads a row's tokens one after another (milliseconds).
+ * Single tokens of up to 16 query heads per kv head share the device evenly whatever their lengths; otherwise one CTA walks
+ * the cache for 2 floor(128 / heads per kv head) rows of one kv head, so few such rows on long caches leave most of it idle.
+ * An infinite or NaN value that some rows of such a block see and others do not makes its rows take the slow way.
  * DVM_ERR_UNSUPPORTED: head_dim above 256; page_size not a power of two or below 8; more than 128 query heads per kv head. */
 typedef struct {
   int64_t requests, rows, q_heads, kv_heads, head_dim;
   int64_t pages, page_size, max_blocks;
   int64_t window, sinks;                           /* window 0: every earlier token is visible */
-  int64_t max_q;                                   /* most query rows of one request; 1: the kernel for single tokens */
+  int64_t max_q;                                   /* most query rows of one request, >= 1; 1: the kernel for single tokens */
   int64_t q_stride[2], out_stride[2];              /* token, head */
   int64_t k_stride[3], v_stride[3];                /* page, token, head */
   int32_t dtype, out_dtype;                        /* DVM_F32 or DVM_BF16: of q and the caches; of out */

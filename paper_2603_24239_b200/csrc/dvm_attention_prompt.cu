@@ -27,10 +27,14 @@
 // a page, pages given back), and if a value that some rows see and others do not is not finite, the CTA's rows are done
 // again without tensor cores (attend_row), exactly.
 //
-// Bound by the weights: 16 exponentials a cycle and SM, their scaling, conversion and way through tensor memory take as long
-// as the products.  One prompt of 8192 tokens, 32 / 8 heads of 128: 475 to 487 us in bursts (1130 to 1160 TFLOP/s), 559 us at
-// the power cap; 32 / 32 heads under a window of 1024: 191 us; 12 ragged prompts on cached ones, 40 / 8 heads of 96: 135 us;
-// 8 prompts of up to 1531 tokens, 16 / 4 heads of 64, window 128: 41 us.
+// Bound by the chain that a row goes through at every tile -- scores, their maximum, the warp's vote, weights, their way to
+// tensor memory, the products -- with two row tiles to hide each other's.  No unit is full: a tile of 64 tokens takes 2050
+// cycles, its products 1240 of them when issued alone, its exponentials 900 at 16 a cycle; profiled on 2 prompts of 2048 tokens
+// tensor cores 41 %, the exponentials' unit 36 %, issue 39 % of their peaks.  Calls in a row (bursts of a dozen after a pause):
+// one prompt of 8192 tokens, 32 / 8 heads of 128: 553 to 569 us at the power cap (490; 970 to 1120 TFLOP/s); 32 / 32 heads under a window of
+// 1024: 214 to 222 us (195); 12 ragged prompts on cached ones, 40 / 8 heads of 96: 146 us (140); 8 prompts of up to 1531
+// tokens, 16 / 4 heads of 64, window 128: 41 us.  A block's cache is walked by one CTA: few rows on a long cache leave most of the
+// device idle (4 rows on 16384 tokens: 270 us).
 //
 // Every wait is bounded: it gives up when 2 s pass in which the CTA neither fetched a tile nor went on doing rows again (one
 // warp, 32 rows, token after token: 134 ms on 8192 tokens, 2.5 s on 153600).  Then the CTA raises its abort flag, all roles

@@ -6,7 +6,7 @@
 // R / 8 on hold the rest, which stays, in the same manner.  Rotation then takes no exchange between lanes, whether halves
 // or neighbours are paired.  Only the mean of squares crosses lanes.  (8 elements in a row per lane where
 // fp32 neighbours are paired, so that every access left out every other 16 bytes: 1531 tokens of 40 + 8 + 8 heads of 96 17.6 us
-// on the device, 13.0 now.)
+// on the device, 13.0 now, with data that stays in L2; 14.6 with three sets of it in turn.)
 // A CTA keeps the same heads for all tokens it takes -- all of them, or a part where there are more than its groups can
 // have in flight -- so what a thread reads and writes is found once and moves by a stride; position, slot and angles are
 // read once per thread and token, and while one token is computed the heads and angles of the next are on their way, and
@@ -14,8 +14,8 @@
 // instruction); the store rounds once.  With the head's place worked out anew for every token, the same kernel took 744
 // instructions per warp and token and was bound by them: 80 us for 8192 tokens of 32 + 8 + 8 heads of 128.  With the next
 // token's data in registers (one token ahead, two CTAs per SM) it was bound by what is in flight: 50 us.  Now each
-// thread copies its own runs into shared memory (cp.async, DEPTH tokens ahead) and reads them from there: 38 us, 5.3 TB/s;
-// one token 1.8 us in a chain of launches.
+// thread copies its own runs into shared memory (cp.async, DEPTH tokens ahead) and reads them from there: 41 us in calls in a
+// row, 5.0 TB/s (37 us in a chain of captured launches, 39 in bursts); one token 1.8 us in such a chain.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
