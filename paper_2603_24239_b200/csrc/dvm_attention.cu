@@ -52,6 +52,7 @@ int encode_map(CUtensorMap* map, const void* ptr, const cuuint64_t (&dims)[4], c
     const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found);
     if (e != cudaSuccess || found != cudaDriverEntryPointSuccess || !p) {
       dvm_note_cuda_error(e != cudaSuccess ? (int)e : (int)cudaErrorNotSupported);
+      (void)cudaGetLastError();
       return DVM_ERR_CUDA;
     }
     fn = (EncodeTiledFn)p;

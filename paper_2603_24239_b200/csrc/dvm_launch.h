@@ -15,12 +15,14 @@ enum { ST_OK = 0, ST_BAD_CODE = 1, ST_TIMEOUT = 2 };
 
 void dvm_note_cuda_error(int e);
 
-// Records a failed CUDA runtime call (dvm_last_cuda_error) and returns DVM_ERR_CUDA from the caller.
+// Records a failed CUDA runtime call (dvm_last_cuda_error) and returns DVM_ERR_CUDA from the caller.  The runtime's own record
+// of it is cleared: the check behind a later launch would find it there and report a launch that did not fail.
 #define DVM_CUDA(call)                \
   do {                                \
     cudaError_t e_ = (call);          \
     if (e_ != cudaSuccess) {          \
       dvm_note_cuda_error((int)e_);   \
+      (void)cudaGetLastError();       \
       return DVM_ERR_CUDA;            \
     }                                 \
   } while (0)

@@ -1166,6 +1166,7 @@ int mm_encode_fn(EncodeTiledFn* out) {
     cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
     if (e != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn) {
       dvm_note_cuda_error(e != cudaSuccess ? (int)e : (int)cudaErrorNotSupported);
+      (void)cudaGetLastError();
       return DVM_ERR_CUDA;
     }
     g_encode_tiled = (EncodeTiledFn)fn;
