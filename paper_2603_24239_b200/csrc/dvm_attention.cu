@@ -150,7 +150,8 @@ __global__ void dvm_selftest_attention_wait_kernel(int which, unsigned int* stat
   }
   __syncthreads();
   bool ok = true;
-  if (warp == 0) ok = which == WAIT_FLAT ? mbar_wait_flat(never, 0, words, words + 1) : which == WAIT_POLL ? mbar_poll(never, 0, words, words + 1) : mbar_wait(never, 0, words);
+  if (warp == 0)
+    ok = which == WAIT_FLAT ? mbar_wait_flat(never, 0, words, words + 1) : which == WAIT_POLL ? mbar_poll(never, 0, words, words + 1) : mbar_wait(never, 0, words);
   __syncthreads();
   if (!words[0]) return;
   if (which == WAIT_DRAIN) {

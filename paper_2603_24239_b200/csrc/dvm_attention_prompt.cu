@@ -29,12 +29,12 @@
 //
 // Bound by the chain that a row goes through at every tile -- scores, their maximum, the warp's vote, weights, their way to
 // tensor memory, the products -- with two row tiles to hide each other's.  No unit is full: a tile of 64 tokens takes 2050
-// cycles, its products 1240 of them when issued alone, its exponentials 900 at 16 a cycle; profiled on 2 prompts of 2048 tokens
-// tensor cores 41 %, the exponentials' unit 36 %, issue 39 % of their peaks.  Calls in a row (bursts of a dozen after a pause):
-// one prompt of 8192 tokens, 32 / 8 heads of 128: 553 to 569 us at the power cap (490; 970 to 1120 TFLOP/s); 32 / 32 heads under a window of
-// 1024: 214 to 222 us (195); 12 ragged prompts on cached ones, 40 / 8 heads of 96: 146 us (140); 8 prompts of up to 1531
-// tokens, 16 / 4 heads of 64, window 128: 41 us.  A block's cache is walked by one CTA: few rows on a long cache leave most of the
-// device idle (4 rows on 16384 tokens: 270 us).
+// cycles, its products 1240 of them when issued alone, its exponentials 900 at 16 a cycle; profiled on 2 prompts of 2048
+// tokens, tensor cores 41 %, the exponentials' unit 36 %, issue 39 % of their peaks.  Calls in a row (bursts of a dozen after
+// a pause): one prompt of 8192 tokens, 32 / 8 heads of 128: 553 to 569 us at the power cap (490), 970 to 1120 TFLOP/s; 32 / 32
+// heads under a window of 1024: 214 to 222 us (195); 12 ragged prompts on cached ones, 40 / 8 heads of 96: 146 us (140); 8
+// prompts of up to 1531 tokens, 16 / 4 heads of 64, window 128: 41 us.  A block's cache is walked by one CTA: few rows on a long
+// cache leave most of the device idle (4 rows on 16384 tokens: 270 us).
 //
 // Every wait is bounded: it gives up when 2 s pass in which the CTA neither fetched a tile nor went on doing rows again (one
 // warp, 32 rows, token after token: 134 ms on 8192 tokens, 2.5 s on 153600).  Then the CTA raises its abort flag, all roles
@@ -145,8 +145,9 @@ __device__ __forceinline__ float max_nan(float a, float b, float c) {
 // 2^x without the special function unit, for part of the weights: the unit's 16 results a cycle are what the weights take
 // longest for, while multiply-adds are to spare.  x = f + r with f the nearest integer (1.5 2^23 added and taken away) and
 // |r| <= 1/2; 2^r by the polynomial of degree 5 with constant term 1 of least largest relative error, found by Remez exchange
-// (9.15e-8; 1.7e-7 with coefficients and steps in fp32), so that x <= -127 gives exactly 0; f is added to the exponent field.  For x below 128.  A NaN gives 0: it comes only from a row's
-// maximum of NaN or +inf, which makes the other weights and their sum NaN (see `top` below).
+// (9.15e-8; 1.7e-7 with coefficients and steps in fp32), so that x <= -127 gives exactly 0; f is added to the exponent
+// field.  For x below 128.  A NaN gives 0: it comes only from a row's maximum of NaN or +inf, which makes the other weights
+// and their sum NaN (see `top` below).
 __device__ __forceinline__ float2 ex2_by_polynomial(float2 x) {
   const float2 big = make_float2(12582912.f, 12582912.f);
   x.x = fmaxf(x.x, -127.f);
@@ -707,7 +708,8 @@ dvm_attention_prompt_kernel(const __grid_constant__ CUtensorMap tm_q, const __gr
     __syncwarp();
     if (ok && dirty[4 * x + (k & 3)])
       for (int r = (warp & 3) * 32; r < min((warp & 3) * 32 + 32, n_rows * a.group); ++r)
-        attend_row<__nv_bfloat16>(a, w[B_REQUEST], position() + r / a.group, w[B_ROW0] + x * tokens + r / a.group, w[B_KVH] * a.group + r % a.group, (uint32_t*)signs + 1);
+        attend_row<__nv_bfloat16>(a, w[B_REQUEST], position() + r / a.group, w[B_ROW0] + x * tokens + r / a.group, w[B_KVH] * a.group + r % a.group,
+                                  (uint32_t*)signs + 1);
     g += nx;
     seen_tiles += max(w[B_N0], w[B_N1]);
     let_go(k);
