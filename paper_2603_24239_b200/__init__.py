@@ -18,9 +18,11 @@ _BINDING_NAMES = (
 
 _SERVING_NAMES = ("encode_paging", "encode_rotary", "encode_attention", "last_attention_kernel")
 
+_EXPERTS_NAMES = ("encode_routing", "encode_quantize", "encode_scaled_matmul", "encode_combine", "last_scaled_matmul_tile")
+
 
 def __getattr__(name):
-    for module, names in (("serving", _SERVING_NAMES), ("binding", _BINDING_NAMES)):
+    for module, names in (("serving", _SERVING_NAMES), ("experts", _EXPERTS_NAMES), ("binding", _BINDING_NAMES)):
         if name == module or name in names:
             m = importlib.import_module("." + module, __name__)
             value = m if name == module else getattr(m, name)

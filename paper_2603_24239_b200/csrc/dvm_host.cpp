@@ -16,6 +16,7 @@
 #include "dvm_format.h"
 #include "dvm_internal.h"
 #include "dvm_program.h"
+#include "dvm_experts.h"
 #include "dvm_serving.h"
 
 // ---------------------------------------------------------------------------
@@ -1702,6 +1703,7 @@ extern "C" int dvm_verify(const void* code, size_t code_size) {
   if (w[DVM_H_TOTAL_WORDS] * 4ull != code_size) return DVM_ERR_BAD_CODE;
   if (w[DVM_H_KERNEL_TYPE] == DVM_KERNEL_MATMUL) return dvm_verify_matmul(w, code_size / 4);
   if (dvm_is_serving(w[DVM_H_KERNEL_TYPE])) return dvm_verify_serving(w, code_size / 4);
+  if (dvm_is_experts(w[DVM_H_KERNEL_TYPE])) return dvm_verify_experts(w, code_size / 4);
   if (w[DVM_H_KERNEL_TYPE] != DVM_KERNEL_VEC) return DVM_ERR_BAD_CODE;
   uint32_t counts = w[DVM_H_COUNTS];
   uint32_t n_tensors = counts & 0xff, n_in = (counts >> 8) & 0xff, n_opd = (counts >> 16) & 0xff,
@@ -1910,6 +1912,7 @@ extern "C" int dvm_disassemble(const void* code, size_t code_size, char* buf, si
   const uint32_t* w = (const uint32_t*)code;
   if (w[DVM_H_KERNEL_TYPE] == DVM_KERNEL_MATMUL) return dvm_disassemble_matmul(w, code_size / 4, buf, cap);
   if (dvm_is_serving(w[DVM_H_KERNEL_TYPE])) return dvm_disassemble_serving(w, buf, cap);
+  if (dvm_is_experts(w[DVM_H_KERNEL_TYPE])) return dvm_disassemble_experts(w, buf, cap);
   Out o = {buf, cap, 0, false};
   uint32_t counts = w[DVM_H_COUNTS];
   uint32_t n_tensors = counts & 0xff, n_in = (counts >> 8) & 0xff, n_opd = (counts >> 16) & 0xff;
@@ -2012,6 +2015,10 @@ extern "C" int dvm_tensor_extents(const void* code, size_t code_size, int64_t* b
   if (w[DVM_H_N_TILES] == 0) return DVM_OK;
   if (dvm_is_serving(w[DVM_H_KERNEL_TYPE])) {
     dvm_extents_serving(w, bytes_needed);
+    return DVM_OK;
+  }
+  if (dvm_is_experts(w[DVM_H_KERNEL_TYPE])) {
+    dvm_extents_experts(w, bytes_needed);
     return DVM_OK;
   }
   auto need = [&](uint32_t slot, uint64_t last_element, uint32_t dt) {

@@ -12,6 +12,7 @@
 #include "dvm_format.h"
 #include "dvm_internal.h"
 #include "dvm_launch.h"
+#include "dvm_experts.h"
 #include "dvm_serving.h"
 #include "dvm_vm.cuh"
 #include "dvm_vm_variants.h"
@@ -832,8 +833,9 @@ extern "C" int dvm_launch(const void* code, size_t code_size, void* const* tenso
   const uint32_t* w = (const uint32_t*)code;
   if (w[DVM_H_KERNEL_TYPE] == DVM_KERNEL_MATMUL)
     return dvm_launch_matmul(w, code_size / 4, tensors, n_tensors, (cudaStream_t)cuda_stream);
-  if (dvm_is_serving(w[DVM_H_KERNEL_TYPE])) {
-    st = dvm_launch_serving(w, tensors, n_tensors, (cudaStream_t)cuda_stream);
+  const bool experts = dvm_is_experts(w[DVM_H_KERNEL_TYPE]);
+  if (experts || dvm_is_serving(w[DVM_H_KERNEL_TYPE])) {
+    st = experts ? dvm_launch_experts(w, tensors, n_tensors, (cudaStream_t)cuda_stream) : dvm_launch_serving(w, tensors, n_tensors, (cudaStream_t)cuda_stream);
     if (st != DVM_OK || !debug_mode()) return st;
     int status = DVM_OK;
     st = dvm_last_device_status(cuda_stream, &status);
@@ -926,7 +928,7 @@ extern "C" int dvm_run_host(const void* code, size_t code_size, void* const* hos
   int st = dvm_verify(code, code_size);
   if (st != DVM_OK) return st;
   const uint32_t* w = (const uint32_t*)code;
-  if (dvm_is_serving(w[DVM_H_KERNEL_TYPE])) return DVM_ERR_UNSUPPORTED;  // (their tables and caches live on the device between launches)
+  if (dvm_is_serving(w[DVM_H_KERNEL_TYPE]) || dvm_is_experts(w[DVM_H_KERNEL_TYPE])) return DVM_ERR_UNSUPPORTED;  // (their tables, caches and plans live on the device between launches)
   const uint32_t counts = w[DVM_H_COUNTS];
   const int nt = counts & 0xff, n_in = (counts >> 8) & 0xff;
   if (n_tensors != nt || nt > DVM_MAX_TENSORS) return DVM_ERR_INVALID_ARG;

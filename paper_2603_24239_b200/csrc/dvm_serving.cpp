@@ -4,50 +4,10 @@
 
 #include <math.h>
 #include <stdio.h>
-#include <string.h>
+
+#include "dvm_describe.h"
 
 namespace {
-
-constexpr int64_t kMaxDim = (1ll << 31) - 1;
-constexpr int64_t kMaxBytes = 1ll << 46;  // no tensor reaches farther from its pointer
-
-inline int64_t es_of(int dtype) { return dtype == DVM_BF16 ? 2 : 4; }
-inline bool dim_ok(int64_t v, int64_t lo = 0, int64_t hi = kMaxDim) { return v >= lo && v <= hi; }
-inline bool float_type(int dt) { return dt == DVM_F32 || dt == DVM_BF16; }
-
-// Bytes from the pointer to the end of the last element of a strided tensor with an adjacent last dim; 0 when it is
-// empty, -1 when a stride is negative or the tensor reaches too far.
-int64_t extent(const int64_t* size, const int64_t* stride, int n, int64_t last, int64_t es) {
-  __int128 far = last;
-  bool empty = last == 0;
-  for (int i = 0; i < n; ++i) {
-    if (size[i] == 0) empty = true;
-    if (size[i] > 1) {
-      if (stride[i] < 0) return -1;
-      far += (__int128)(size[i] - 1) * stride[i];
-    }
-  }
-  if (empty) return 0;
-  if (far * es > kMaxBytes) return -1;
-  return (int64_t)(far * es);
-}
-
-// Whether no element of a strided output is addressed twice: dims in the order of their strides, each stride past all
-// that the dims before it reach.
-bool distinct(const int64_t* size, const int64_t* stride, int n, int64_t last) {
-  int order[3] = {0, 1, 2};
-  for (int i = 0; i < n; ++i)
-    for (int j = i + 1; j < n; ++j)
-      if (stride[order[j]] < stride[order[i]]) { int t = order[i]; order[i] = order[j]; order[j] = t; }
-  __int128 reach = last;
-  for (int i = 0; i < n; ++i) {
-    const int k = order[i];
-    if (size[k] <= 1) continue;
-    if (stride[k] < reach) return false;
-    reach += (__int128)(size[k] - 1) * stride[k];
-  }
-  return true;
-}
 
 int check_paging(const dvm_paging_desc& d) {
   if (!dim_ok(d.requests) || !dim_ok(d.max_blocks) || !dim_ok(d.page_size, 1) || !dim_ok(d.rows) || !dim_ok(d.free_pages)) return DVM_ERR_INVALID_ARG;
@@ -98,32 +58,13 @@ int check_attention(const dvm_attention_desc& d) {
 }
 
 template <class D> int emit(const D& d, uint32_t type, int n_in, int n_out, int64_t tiles, void* code, size_t cap, size_t* size) {
-  const int nt = n_in + n_out;
-  const size_t total = DVM_HDR_WORDS + 2 * (size_t)nt + (sizeof(D) + 3) / 4;
-  static_assert((DVM_HDR_WORDS + 2 * 16) * 4 + sizeof(D) + 4 <= DVM_SERVING_CODE_BYTES, "the code buffer size of the header");
-  *size = total * 4;
-  if (!code || cap < total * 4) return DVM_ERR_BUFFER_TOO_SMALL;
-  uint32_t* w = (uint32_t*)code;
-  memset(w, 0, total * 4);
-  w[DVM_H_MAGIC] = DVM_MAGIC;
-  w[DVM_H_KERNEL_TYPE] = type;
-  w[DVM_H_N_TILES] = (uint32_t)tiles;
-  w[DVM_H_TOTAL_WORDS] = (uint32_t)total;
-  w[DVM_H_COUNTS] = (uint32_t)nt | ((uint32_t)n_in << 8) | ((uint32_t)n_out << 24);
-  w[DVM_H_PRIMARY] = 0xffffffffu;
-  memcpy(w + DVM_HDR_WORDS + 2 * nt, &d, sizeof(D));
-  return DVM_OK;
+  return dvm_emit_descriptor<DVM_SERVING_CODE_BYTES>(d, type, n_in, n_out, tiles, code, cap, size);
 }
 
 // Pieces of work, 0 for an instance that launches nothing.
 int64_t tiles_of(const dvm_paging_desc& d) { return 1 + d.rows / 1024; }  // (an empty batch still writes starts, taken and the padding rows)
 int64_t tiles_of(const dvm_rotary_desc& d) { return d.q_heads + d.kv_heads ? d.tokens : 0; }
 int64_t tiles_of(const dvm_attention_desc& d) { return d.requests ? d.rows : 0; }
-
-template <class D> bool well_formed(const uint32_t* w, size_t n_words, int nt, int n_in, int64_t tiles) {
-  return n_words == DVM_HDR_WORDS + 2 * (size_t)nt + (sizeof(D) + 3) / 4 && w[DVM_H_N_TILES] == (uint32_t)tiles && w[DVM_H_CODE_WORDS] == 0 &&
-         w[DVM_H_COUNTS] == ((uint32_t)nt | ((uint32_t)n_in << 8) | ((uint32_t)(nt - n_in) << 24));
-}
 
 }  // namespace
 
@@ -182,7 +123,7 @@ int dvm_verify_serving(const uint32_t* w, size_t n_words) {
     dvm_paging_desc d;
     if (desc_bytes < sizeof d) return DVM_ERR_BAD_CODE;
     dvm_serving_desc(w, &d);
-    return check_paging(d) == DVM_OK && well_formed<dvm_paging_desc>(w, n_words, PG_N, PG_TABLE, tiles_of(d)) ? DVM_OK : DVM_ERR_BAD_CODE;
+    return check_paging(d) == DVM_OK && dvm_descriptor_well_formed<dvm_paging_desc>(w, n_words, PG_N, PG_TABLE, tiles_of(d)) ? DVM_OK : DVM_ERR_BAD_CODE;
   }
   if (w[DVM_H_KERNEL_TYPE] == DVM_KERNEL_ROTARY) {
     dvm_rotary_desc d;
@@ -190,12 +131,12 @@ int dvm_verify_serving(const uint32_t* w, size_t n_words) {
     dvm_serving_desc(w, &d);
     if (check_rotary(d) != DVM_OK) return DVM_ERR_BAD_CODE;
     const RotarySlots s = dvm_rotary_slots(d);
-    return well_formed<dvm_rotary_desc>(w, n_words, s.n, s.n_in, tiles_of(d)) ? DVM_OK : DVM_ERR_BAD_CODE;
+    return dvm_descriptor_well_formed<dvm_rotary_desc>(w, n_words, s.n, s.n_in, tiles_of(d)) ? DVM_OK : DVM_ERR_BAD_CODE;
   }
   dvm_attention_desc d;
   if (desc_bytes < sizeof d) return DVM_ERR_BAD_CODE;
   dvm_serving_desc(w, &d);
-  return check_attention(d) == DVM_OK && well_formed<dvm_attention_desc>(w, n_words, AT_N, AT_OUT, tiles_of(d)) ? DVM_OK : DVM_ERR_BAD_CODE;
+  return check_attention(d) == DVM_OK && dvm_descriptor_well_formed<dvm_attention_desc>(w, n_words, AT_N, AT_OUT, tiles_of(d)) ? DVM_OK : DVM_ERR_BAD_CODE;
 }
 
 void dvm_extents_serving(const uint32_t* w, int64_t* b) {
