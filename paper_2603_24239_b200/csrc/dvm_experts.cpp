@@ -206,11 +206,11 @@ CombineSlots dvm_slots(const dvm_combine_desc& d) {
   return s;
 }
 
-// Which rows a tile has goes by the rows of a group if they were dealt out evenly: a tile is not wider than needed, as its
-// accumulators are scaled one by one whether a row fills them or not.
+// The kernel goes by the rows of a group if they were dealt out evenly.  For few of them a tile is not wider than needed, as
+// its sums are scaled one by one whether a row fills them or not.
 int dvm_scaled_tile(const dvm_scaled_matmul_desc& d) {
   const int64_t each = dvm_up(d.rows, d.groups);
-  return each <= 16 ? 16 : each <= 32 ? 32 : each <= 64 ? 64 : 128;
+  return each <= 16 ? 16 : each <= 32 ? 32 : each <= 64 ? 64 : each <= 160 ? 128 : 256;
 }
 
 extern "C" int dvm_encode_routing(const dvm_routing_desc* d, void* code, size_t code_capacity, size_t* code_size) { return encode(d, code, code_capacity, code_size); }

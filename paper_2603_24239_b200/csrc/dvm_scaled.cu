@@ -11,9 +11,9 @@ namespace {
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// Codes as a tensor map of `rank` dims, k first; a box is 128 codes of k and `rows` rows, 128-byte swizzle.  What a box reaches
-// beyond the tensor is filled with zeros.
-int encode_map(CUtensorMap* map, const void* ptr, int rank, const cuuint64_t* dims, const cuuint64_t* strides, int rows) {
+// A tensor map of `rank` dims, columns first; a box is 128 bytes of `rows` rows, 128-byte swizzle.  What a box reaches beyond the
+// tensor is filled with zeros when loaded, and left out when stored.
+int encode_map(CUtensorMap* map, CUtensorMapDataType type, int width, const void* ptr, int rank, const cuuint64_t* dims, const cuuint64_t* strides, int rows) {
   static std::atomic<EncodeTiledFn> cached{nullptr};
   EncodeTiledFn fn = cached.load();
   if (!fn) {
@@ -28,8 +28,8 @@ int encode_map(CUtensorMap* map, const void* ptr, int rank, const cuuint64_t* di
     fn = (EncodeTiledFn)p;
     cached.store(fn);
   }
-  const cuuint32_t box[3] = {DVM_SCALE_BLOCK, (cuuint32_t)rows, 1}, one[3] = {1, 1, 1};
-  if (fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, rank, const_cast<void*>(ptr), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  const cuuint32_t box[3] = {(cuuint32_t)(128 / width), (cuuint32_t)rows, 1}, one[3] = {1, 1, 1};
+  if (fn(map, type, rank, const_cast<void*>(ptr), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
     dvm_note_cuda_error((int)cudaErrorInvalidValue);
     return DVM_ERR_CUDA;
@@ -60,15 +60,17 @@ int dvm_launch_scaled_matmul(const dvm_scaled_matmul_desc& d, void* const* t, cu
   a.rows = (int)d.rows; a.n = (int)d.n; a.groups = (int)d.groups;
   a.k_blocks = (int)dvm_up(d.k, DVM_SCALE_BLOCK); a.n_blocks = (int)dvm_up(d.n, DVM_SCALE_BLOCK);
   a.out_bf16 = d.out_dtype == DVM_BF16;
-  const int run = a.out_bf16 ? 8 : 4;
-  a.out_vec = (uintptr_t)a.out % 16 == 0 && (d.rows <= 1 || d.out_stride % run == 0);
-  const int tile = dvm_scaled_tile(d);
-  CUtensorMap x, w;
+  const int tile = dvm_scaled_tile(d), es = a.out_bf16 ? 2 : 4;
+  const bool many = tile > 128;
+  a.out_tma = (uintptr_t)a.out % 16 == 0 && (d.rows <= 1 || (d.out_stride * es % 16 == 0 && d.out_stride * es < (1ll << 40)));
+  CUtensorMap x, w, out = {};
   const cuuint64_t xd[2] = {(cuuint64_t)d.k, (cuuint64_t)d.rows}, xt[1] = {map_stride(d.rows, d.x_stride)};
   const cuuint64_t wd[3] = {(cuuint64_t)d.k, (cuuint64_t)d.n, (cuuint64_t)d.groups}, wt[2] = {map_stride(d.n, d.w_stride[1]), map_stride(d.groups, d.w_stride[0])};
-  st = encode_map(&x, t[s.x], 2, xd, xt, tile);
-  if (st == DVM_OK) st = encode_map(&w, t[s.w], 3, wd, wt, DVM_SCALE_BLOCK);
-  if (st == DVM_OK) st = dvm_launch_scaled_few(x, w, a, tile, dev.device, stream);
+  const cuuint64_t od[2] = {(cuuint64_t)d.n, (cuuint64_t)d.rows}, ot[1] = {map_stride(d.rows, d.out_stride * es)};
+  st = encode_map(&x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, t[s.x], 2, xd, xt, many ? 128 : tile);
+  if (st == DVM_OK) st = encode_map(&w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, t[s.w], 3, wd, wt, many ? 256 : 128);
+  if (st == DVM_OK && many && a.out_tma) st = encode_map(&out, a.out_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, es, a.out, 2, od, ot, 32);
+  if (st == DVM_OK) st = many ? dvm_launch_scaled_many(x, w, out, a, dev.sm_count, dev.device, stream) : dvm_launch_scaled_few(x, w, a, tile, dev.device, stream);
   if (st == DVM_OK) t_last_tile = tile;
   return st;
 }

@@ -23,7 +23,7 @@ struct Args {
   unsigned int* status;
   long long xs_stride, out_stride;
   int rows, n, k_blocks, n_blocks, groups;   // n_blocks: blocks of 128 columns of the result
-  int out_bf16, out_vec;                     // out_vec: 16 bytes of a row's columns can be stored at once
+  int out_bf16, out_tma;                     // out_tma: there is a tensor map of the result
 };
 
 struct Rows { int first, last; };
@@ -85,9 +85,16 @@ __device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t adesc, uint6
       ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// Shared-memory matrix descriptor of a K-major tile: rows of 128 bytes, 128-byte swizzle, groups of 8 rows 1024 bytes apart.
-__device__ __forceinline__ uint64_t desc_k_major(uint32_t addr) {
-  return (uint64_t)((addr >> 4) & 0x3fff) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+// Shared-memory matrix descriptors of K-major tiles: rows of 128 bytes, 128-byte swizzle, groups of 8 rows 1024 bytes apart;
+// from their low word, the address, to which steps along k and stages are added.  The warp that issues products walks as a
+// whole, so that descriptors and barriers stay in uniform registers, and one elected lane issues: from a branch of lane 0 alone
+// a product took 70 cycles to issue, a wait 200.
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr) { return ((addr >> 4) & 0x3fff) | (1u << 16); }
+__device__ __forceinline__ uint64_t desc_of(uint32_t lo) { return lo | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61); }
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
 }
 // Instruction descriptor: e4m3 x e4m3, both K-major, fp32 sums, M x N
 template <int M, int N> constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
@@ -96,3 +103,5 @@ template <int M, int N> constexpr uint32_t IDESC = (1u << 4) | ((uint32_t)(N >> 
 }  // namespace dvm
 
 int dvm_launch_scaled_few(const CUtensorMap& x, const CUtensorMap& w, const dvm::scaled::Args& a, int tile, int device, cudaStream_t stream);
+int dvm_launch_scaled_many(const CUtensorMap& x, const CUtensorMap& w, const CUtensorMap& out, const dvm::scaled::Args& a, int sm_count, int device,
+                           cudaStream_t stream);

@@ -131,28 +131,28 @@ dvm_scaled_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_con
       });
   } else if (warp == 5) {
     // ---------------- one thread multiplies ----------------
-    if (lane == 0) {
-      uint32_t stage = 0, phase = 0, buffer = 0, b_phase = 0;
-      bool some = false;
-      walk([&](int, int, int, int, int kb0, int kb1, long long) {
-        for (int kb = kb0; kb < kb1; ++kb) {
-          if (!mbar_wait(bar_free + 8 * buffer, b_phase ^ 1, abort_flag) || !mbar_wait(bar_full + 8 * stage, phase, abort_flag)) return false;
-          tc_fence_after();
-          const uint64_t w = desc_k_major(base + stage * S::STAGE), x = desc_k_major(base + stage * S::STAGE + S::W);
+    const bool leader = elect_one();
+    const uint32_t w0 = desc_lo(base), x0 = desc_lo(base + S::W);
+    uint32_t stage = 0, phase = 0, buffer = 0, b_phase = 0;
+    walk([&](int, int, int, int, int kb0, int kb1, long long) {
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!__all_sync(0xffffffffu, mbar_wait(bar_free + 8 * buffer, b_phase ^ 1, abort_flag) && mbar_wait(bar_full + 8 * stage, phase, abort_flag))) return false;
+        tc_fence_after();
+        if (leader) {
+          const uint32_t w = w0 + stage * (S::STAGE >> 4), x = x0 + stage * (S::STAGE >> 4);
 #pragma unroll
-          for (int k = 0; k < BLOCK / 32; ++k) umma_e4m3(tmem + buffer * ROWS, w + 2 * k, x + 2 * k, IDESC<BLOCK, ROWS>, k != 0);
+          for (int k = 0; k < BLOCK / 32; ++k) umma_e4m3(tmem + buffer * ROWS, desc_of(w + 2 * k), desc_of(x + 2 * k), IDESC<BLOCK, ROWS>, k != 0);
           umma_commit(bar_empty + 8 * stage);
           umma_commit(bar_done + 8 * buffer);
-          some = true;
-          if (++stage == S::STAGES) { stage = 0; phase ^= 1; }
-          if (++buffer == BUFFERS) { buffer = 0; b_phase ^= 1; }
         }
-        return true;
-      });
-      if (some) {   // every product has ended before tensor memory is given back, whatever else ended early
-        umma_commit(bar_last);
-        mbar_spin(bar_last, 0, abort_flag, DRAIN_NS, false);
+        if (++stage == S::STAGES) { stage = 0; phase ^= 1; }
+        if (++buffer == BUFFERS) { buffer = 0; b_phase ^= 1; }
       }
+      return true;
+    });
+    if (leader) {   // every product has ended before tensor memory is given back, whatever else ended early
+      umma_commit(bar_last);
+      mbar_spin(bar_last, 0, abort_flag, DRAIN_NS, false);
     }
     __syncwarp();
   } else {
