@@ -31,10 +31,10 @@ inline int64_t dvm_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Routing: tokens are taken in rounds of 32, by chunks of whole rounds; a chunk is one CTA.
 #define DVM_ROUTE_ROUND 32
-#define DVM_ROUTE_CHUNKS 148
+#define DVM_ROUTE_CHUNKS 296
 inline int64_t dvm_route_rounds(const dvm_routing_desc& d) {  // rounds of one chunk
   const int64_t rounds = dvm_up(d.tokens, DVM_ROUTE_ROUND);
-  return rounds <= 2 ? 2 : dvm_up(rounds, DVM_ROUTE_CHUNKS);
+  return rounds <= 1 ? 1 : dvm_up(rounds, DVM_ROUTE_CHUNKS);
 }
 inline int64_t dvm_route_chunks(const dvm_routing_desc& d) {
   const int64_t n = dvm_up(d.tokens, DVM_ROUTE_ROUND * dvm_route_rounds(d));

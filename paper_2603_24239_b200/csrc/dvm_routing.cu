@@ -9,8 +9,8 @@
 //
 // The plan is a counting sort without atomics whose order could change it.  Tokens go in rounds of 32, and a round's choices
 // are a bit per token in a word per expert: a token's rank at its expert is the number of bits below its own, plus what
-// earlier rounds of the chunk counted.  With up to 64 tokens one CTA does it all; else every CTA leaves its chunk's counts in
-// the workspace and a second launch adds up those of the chunks before it.
+// earlier rounds of the chunk counted.  With up to 32 tokens one CTA does it all; else every CTA leaves its chunk's counts in
+// the workspace and a second launch adds up those of the chunks before.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -20,7 +20,8 @@
 namespace dvm {
 namespace routing {
 
-constexpr int WARPS = 16, THREADS = WARPS * 32, ROUND = DVM_ROUTE_ROUND, PER_WARP = ROUND / WARPS;
+constexpr int ROUND = DVM_ROUTE_ROUND, WARPS = ROUND, THREADS = WARPS * 32;   // a warp to a token of a round
+constexpr int PLAN = 4, PLAN_THREADS = 512;                                    // of the second launch: chunks of a CTA
 constexpr uint32_t ALL = 0xffffffffu;
 
 struct Args {
@@ -33,6 +34,7 @@ struct Args {
   long long stride;
   int tokens, experts, top_k, groups, top_groups, chunks, rounds;
   int bf16, sigmoid, renormalise;
+  int lanes;           // of a warp to a group: the largest power of two
   float factor;
 };
 
@@ -56,10 +58,30 @@ template <class T> __device__ __forceinline__ T warp_sum(T v) {
   return v;
 }
 
-// How near two values c are when 32 bits may have swapped them: twice what each may be off, in units of 2^-24.  A sigmoid: one
-// ulp of the exponential, a sum, a quotient: less than 6.  Of a softmax every score is at most 1 / sum; the exponential and its
-// argument, up to 16 + 5 additions and the quotient are less than 28 of that.  The bias adds a rounding of c itself.
+// How near two values c are when 32 bits may have swapped them: twice what each may be off, in units of 2^-24.  A sigmoid: the
+// exponential's error, 2 ulp and 1.2 per unit of its argument, times s (1 - s), a sum and a quotient (2 ulp): less than 10.  Of a
+// softmax every score is at most 1 / sum; exponentials (at most 5), up to 16 + 5 additions and the quotient are less than 36
+// of that.  The bias adds a rounding of c itself.
 __device__ __forceinline__ float doubt(float unit, float c) { return 0x1p-23f * (unit + 2.f * fabsf(c)); }
+// Score of a logit: 1 / (1 + exp(-l)), or exp(l - top) / sum.
+__device__ __forceinline__ float score(const Args& a, float l, float top, float sum) {
+  return a.sigmoid ? __fdividef(1.f, 1.f + __expf(-l)) : __fdividef(__expf(l - top), sum);
+}
+
+// The group of every expert of this lane (experts behind the last: group 32, which is none).
+template <int V> __device__ __forceinline__ void groups_of(const Args& a, int (&group)[V]) {
+  const float inv = (float)a.groups / (float)a.experts;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int e = 32 * i + (threadIdx.x & 31);
+    group[i] = e < a.experts ? (int)((e + 0.5f) * inv) : 32;   // (exact: e + 1/2 is half an expert away from any border, e < 512)
+  }
+}
+// The two largest of two pairs, larger one first.
+template <class T> __device__ __forceinline__ void merge2(T& first, T& second, T of, T os) {
+  if (of > first) { second = first > os ? first : os; first = of; }
+  else second = second > of ? second : of;
+}
 
 // The token again in 64 bits; returns lane j's choice.
 template <int V> __device__ __noinline__ int choose_exactly(const Args& a, long long t) {
@@ -91,34 +113,38 @@ template <int V> __device__ __noinline__ int choose_exactly(const Args& a, long 
     if (a.bias && e < a.experts) v[i] += (double)a.bias[e];
   }
   uint32_t stay = ALL;
+  int group[V];
+  groups_of<V>(a, group);
   if (a.groups > 1) {
-    double first = -INFINITY, second = -INFINITY;
-    nan = false;
+    double mine = -INFINITY;   // of group `lane`
+    bool mine_nan = false;
+    for (int g = 0; g < a.groups; ++g) {
+      double first = -INFINITY, second = -INFINITY;
+      bool bad = false;
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      for (int k = 0; k < 32; ++k) {
-        const double x = __shfl_sync(ALL, v[i], k);
-        const int e = 32 * i + k;
-        if (e >= a.experts || e / per != lane) continue;
-        nan |= x != x;
-        if (x > first) { second = first; first = x; } else if (x > second) second = x;
+      for (int i = 0; i < V; ++i)
+        if (group[i] == g) { bad |= v[i] != v[i]; merge2(first, second, v[i], (double)-INFINITY); }
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) {
+        const double of = __shfl_xor_sync(ALL, first, d), os = __shfl_xor_sync(ALL, second, d);
+        merge2(first, second, of, os);
       }
-    const double mine = nan ? -INFINITY : per > 1 ? first + second : first;
+      bad = __any_sync(ALL, bad);
+      if (lane == g) { mine = bad ? -INFINITY : per > 1 ? first + second : first; mine_nan = bad; }
+    }
     int before = 0;
     for (int g = 0; g < a.groups; ++g) {
       const double other = __shfl_sync(ALL, mine, g);
-      const bool other_nan = __shfl_sync(ALL, (int)nan, g);
-      const bool more = nan != other_nan ? nan : other > mine || (other == mine && g < lane);
-      if (g != lane && (more || (nan && other_nan && g < lane))) ++before;
+      const bool other_nan = __shfl_sync(ALL, (int)mine_nan, g);
+      const bool more = mine_nan != other_nan ? mine_nan : other > mine || ((other == mine || mine_nan) && g < lane);
+      if (g != lane && more) ++before;
     }
     stay = __ballot_sync(ALL, lane < a.groups && before < a.top_groups);
   }
   uint32_t free = 0;   // bits of the experts of this lane that may be chosen
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int e = 32 * i + lane;
-    if (e < a.experts && ((stay >> (a.groups > 1 ? e / per : 0)) & 1u)) free |= 1u << i;
-  }
+  for (int i = 0; i < V; ++i)
+    if (group[i] < 32 && ((stay >> group[i]) & 1u)) free |= 1u << i;
   int mine = -1;
   for (int j = 0; j < a.top_k; ++j) {
     int at = 0x7fffffff;     // this lane's best; NaN is worse than anything
@@ -142,113 +168,176 @@ template <int V> __device__ __noinline__ int choose_exactly(const Args& a, long 
   return mine;
 }
 
-// Lane j's choice of token t and its weight.  V: experts of a lane at most; c: this warp's row of shared memory.
-template <int V> __device__ __forceinline__ int choose(const Args& a, long long t, float* c, float* weight) {
-  const int lane = threadIdx.x & 31, per = a.experts / a.groups;
-  const float inv_per = 1.f / per;
-  float l[V], top = -INFINITY, sum = 0.f;
-  bool nan = false;
+// This lane's logits of a token.
+template <int V> __device__ __forceinline__ void load_logits(const Args& a, long long t, float (&l)[V]) {
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int e = 32 * i + lane;
+    const int e = 32 * i + (threadIdx.x & 31);
     l[i] = e < a.experts ? logit_at(a, t, e) : -INFINITY;
-    top = fmaxf(top, l[i]);
-    nan |= l[i] != l[i];
   }
+}
+
+// The first `found` lanes hold the largest values of a token in nearly their order: the j-th in exact order goes to lane j.  (NaN
+// keep their places: they are the last.)
+template <int V> __device__ __noinline__ int order_exactly(const Args& a, const float (&l)[V], float top, float mine_l, float b, int mine, uint32_t key, int found) {
+  const int lane = threadIdx.x & 31;
+  double c;
+  if (a.sigmoid) {
+    c = 1.0 / (1.0 + exp(-(double)mine_l));
+  } else {
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (32 * i + lane < a.experts) sum += exp((double)l[i] - top);
+    c = exp((double)mine_l - top) / warp_sum(sum);
+  }
+  c += (double)b;
+  int before = 0;
+  for (int j = 0; j < found; ++j) {
+    const double o = __shfl_sync(ALL, c, j);
+    const int oi = __shfl_sync(ALL, mine, j);
+    const bool o_nan = __shfl_sync(ALL, key, j) <= 1u, nan = key <= 1u;
+    before += o_nan || nan ? j < lane : o > c || (o == c && oi < mine);
+  }
+  int result = -1;
+  for (int j = 0; j < found; ++j) {
+    const int place = __shfl_sync(ALL, before, j), e = __shfl_sync(ALL, mine, j);
+    if (lane == place) result = e;
+  }
+  return lane < a.top_k ? result : -1;
+}
+
+// The largest of a lane's keys and its expert, of equal ones the lowest.
+template <int V> __device__ __forceinline__ void largest(const uint32_t (&key)[V], uint32_t* best, int* at) {
+  uint32_t k[V];
+  int e[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) { k[i] = key[i]; e[i] = 32 * i + (threadIdx.x & 31); }
+#pragma unroll
+  for (int d = 1; d < V; d <<= 1)
+#pragma unroll
+    for (int i = 0; i < V; i += 2 * d)
+      if (k[i + d] > k[i]) { k[i] = k[i + d]; e[i] = e[i + d]; }
+  *best = k[0];
+  *at = e[0];
+}
+
+// Lane j's choice of token t and its weight.  V: experts of a lane at most; l: this lane's logits; bias: all of them, in shared
+// memory; row: this warp's row of shared memory.
+template <int V> __device__ __forceinline__ int choose(const Args& a, long long t, const float (&l)[V], const float* bias, float* row, float* weight) {
+  const int lane = threadIdx.x & 31;
+  float top = -INFINITY, sum = 0.f;
   uint32_t key[V];
   if (!a.sigmoid) {
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      top = fmaxf(top, l[i]);
+      nan |= l[i] != l[i];
+    }
     top = warp_max(top);
     if (__any_sync(ALL, nan)) top = NAN;
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      if (32 * i + lane < a.experts) sum += expf(l[i] - top);
+      if (32 * i + lane < a.experts) sum += __expf(l[i] - top);
     sum = warp_sum(sum);
   }
-  uint32_t stay = ALL;
   bool unsure = false;
-  const float unit = a.sigmoid ? 6.f : 28.f / sum;
+  const float unit = a.sigmoid ? 10.f : 36.f / sum;
   if (a.bias || a.groups > 1) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int e = 32 * i + lane;
-      float s = a.sigmoid ? 1.f / (1.f + expf(-l[i])) : expf(l[i] - top) / sum;
-      if (a.bias && e < a.experts) s += a.bias[e];
-      key[i] = e < a.experts ? key_of(a.bias ? s : l[i]) : 0u;
-      if (a.groups > 1 && e < a.experts) c[e] = s;
+      key[i] = 0u;
+      if (e < a.experts) {
+        const float c = score(a, l[i], top, sum) + (a.bias ? bias[e] : 0.f);
+        key[i] = key_of(a.bias ? c : l[i]);
+        if (a.groups > 1) row[e + (e >> 5)] = c;   // (a word left out of every 33: groups of 32 in different banks)
+      }
     }
     if (a.groups > 1) {
+      // every group by a.lanes lanes, which take its experts in turn and merge what they found
       __syncwarp();
+      const int per = a.experts / a.groups, g = lane / a.lanes, sub = lane - g * a.lanes;
       float first = -INFINITY, second = -INFINITY;
       bool bad = false;
-      if (lane < a.groups)
-        for (int k = 0; k < per; ++k) {
-          const float x = c[lane * per + k];
+      if (g < a.groups)
+        for (int k = sub; k < per; k += a.lanes) {
+          const int e = g * per + k;
+          const float x = row[e + (e >> 5)];
           bad |= x != x;
           second = fmaxf(second, fminf(first, x));
           first = fmaxf(first, x);
         }
-      const uint32_t mine = lane < a.groups ? (bad ? 1u : key_of(per > 1 ? first + second : first)) : 0u;
-      int before = 0;
-      for (int g = 0; g < a.groups; ++g) {
-        const uint32_t other = __shfl_sync(ALL, mine, g);
-        before += other > mine || (other == mine && g < lane);
+      for (int d = a.lanes >> 1; d > 0; d >>= 1) {
+        const float of = __shfl_xor_sync(ALL, first, d), os = __shfl_xor_sync(ALL, second, d);
+        bad |= __shfl_xor_sync(ALL, (int)bad, d) != 0;
+        second = fmaxf(fmaxf(second, os), fminf(first, of));
+        first = fmaxf(first, of);
       }
-      const bool in = lane < a.groups && before < a.top_groups;
-      stay = __ballot_sync(ALL, in);
+      // (every lane of a group has its key; lanes of no group the lowest)
+      const uint32_t mine = g < a.groups ? (bad ? 1u : key_of(per > 1 ? first + second : first)) : 0u;
+      int before = 0;
+      for (int o = 0; o < a.groups; ++o) {
+        const uint32_t other = __shfl_sync(ALL, mine, o * a.lanes);
+        before += other > mine || (other == mine && o < g);
+      }
+      const bool in = g < a.groups && before < a.top_groups;
+      const uint32_t stay = __ballot_sync(ALL, in);
       if (a.top_groups < a.groups) {
-        const uint32_t least = __reduce_min_sync(ALL, in ? mine : ALL), most = __reduce_max_sync(ALL, lane < a.groups && !in ? mine : 0u);
+        const uint32_t least = __reduce_min_sync(ALL, in ? mine : ALL), most = __reduce_max_sync(ALL, in ? 0u : mine);
         if (most > 1u) {
           const float x = of_key(least), y = of_key(most);
           // (a sum of two values: both may be off, and their sum is rounded)
           unsure = x - y <= 2.f * doubt(unit, fmaxf(fabsf(x), fabsf(y)));
         }
       }
-      __syncwarp();
+      const float inv = (float)a.groups / (float)a.experts;   // (e + 1/2 is half an expert away from any border, e < 512)
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (!((stay >> min((int)((32 * i + lane + 0.5f) * inv) * a.lanes, 31)) & 1u)) key[i] = 0u;
+      __syncwarp();   // (the row is the next token's)
     }
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) key[i] = 32 * i + lane < a.experts ? key_of(l[i]) : 0u;
   }
-  if (a.groups > 1) {
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (!((stay >> min((int)((32 * i + lane + 0.5f) * inv_per), 31)) & 1u)) key[i] = 0u;
-  }
-  // ---- the largest keys, one after another; with a bias one more, to see how near it is ----
-  uint32_t mine_key = 0u, extra_key = 0u;
-  int mine = -1, extra = 0;
-  const int rounds = a.top_k + (a.bias ? 1 : 0);
-  for (int j = 0; j < rounds; ++j) {
-    uint32_t best = key[0];
-    int at = lane;
-#pragma unroll
-    for (int i = 1; i < V; ++i)
-      if (key[i] > best) { best = key[i]; at = 32 * i + lane; }
+  // ---- the largest keys, one after another; with a bias also those so near the last one that they may be above it ----
+  uint32_t mine_key = 0u, last_key = 0u, best = 0u;
+  int mine = -1, at = 0, found = 0;
+  largest<V>(key, &best, &at);
+  for (;;) {
     const uint32_t most = __reduce_max_sync(ALL, best);
-    if (most == 0u) break;   // (no further expert: only where one more than top_k was asked for)
-    at = (int)__reduce_min_sync(ALL, best == most ? (uint32_t)at : ALL);
+    if (found >= a.top_k) {
+      if (!a.bias || most <= 1u || last_key <= 1u || of_key(last_key) - of_key(most) > doubt(unit, fmaxf(fabsf(of_key(last_key)), fabsf(of_key(most))))) break;
+      if (found == 32) { unsure = true; break; }
+    }
+    const int won = (int)__reduce_min_sync(ALL, best == most ? (uint32_t)at : ALL);
+    if (lane == found) { mine = won; mine_key = most; }
+    if (++found == a.top_k) last_key = most;
+    if (lane == (won & 31)) {
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (at == 32 * i + lane) key[i] = 0u;
-    if (j == a.top_k) { extra = at; extra_key = most; }
-    else if (lane == j) { mine = at; mine_key = most; }
+      for (int i = 0; i < V; ++i)
+        if (32 * i + lane == won) key[i] = 0u;
+      largest<V>(key, &best, &at);
+    }
+    __syncwarp();
   }
   float mine_l = mine >= 0 ? logit_at(a, t, mine) : 0.f;
   if (a.bias) {
-    const float b = mine >= 0 ? a.bias[mine] : 0.f;
-    uint32_t next_key = __shfl_down_sync(ALL, mine_key, 1);
-    float next_l = __shfl_down_sync(ALL, mine_l, 1), next_b = __shfl_down_sync(ALL, b, 1);
-    if (lane == a.top_k - 1) { next_key = extra_key; next_l = logit_at(a, t, extra); next_b = a.bias[extra]; }
-    if (lane < a.top_k && next_key > 1u && mine_key > 1u) {
+    const float b = mine >= 0 ? bias[mine] : 0.f;
+    const uint32_t next_key = __shfl_down_sync(ALL, mine_key, 1);
+    const float next_l = __shfl_down_sync(ALL, mine_l, 1), next_b = __shfl_down_sync(ALL, b, 1);
+    bool near = false;
+    if (lane < found - 1 && next_key > 1u && mine_key > 1u) {
       const float x = of_key(mine_key), y = of_key(next_key);
       // (the same logit and bias: the index decides, here as in 64 bits)
-      if (x - y <= doubt(unit, fmaxf(fabsf(x), fabsf(y))) && !(mine_l == next_l && b == next_b)) unsure = true;
+      near = x - y <= doubt(unit, fmaxf(fabsf(x), fabsf(y))) && !(mine_l == next_l && b == next_b);
     }
+    if (__any_sync(ALL, near) && !__any_sync(ALL, unsure)) mine = order_exactly<V>(a, l, top, mine_l, b, mine, mine_key, found);
   }
-  if (__any_sync(ALL, unsure)) {
-    mine = choose_exactly<V>(a, t);
-    mine_l = mine >= 0 ? logit_at(a, t, mine) : 0.f;
-  }
+  if (__any_sync(ALL, unsure)) mine = choose_exactly<V>(a, t);
+  mine_l = mine >= 0 ? logit_at(a, t, mine) : 0.f;
   float s = a.sigmoid ? 1.f / (1.f + expf(-mine_l)) : expf(mine_l - top) / sum;
   if (a.renormalise) {
     const float total = warp_sum(lane < a.top_k ? s : 0.f);
@@ -268,7 +357,7 @@ __device__ __forceinline__ uint32_t warp_scan(uint32_t v) {  // inclusive
   return v;
 }
 // starts of the experts from their counts (thread e: expert e), by all threads of the CTA
-__device__ __forceinline__ uint32_t block_scan(uint32_t count, uint32_t* warp_sums, uint32_t* total) {  // exclusive
+template <int WARPS> __device__ __forceinline__ uint32_t block_scan(uint32_t count, uint32_t* warp_sums, uint32_t* total) {  // exclusive
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t upto = warp_scan(count);
   if (lane == 31) warp_sums[warp] = upto;
@@ -283,39 +372,33 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t count, uint32_t* warp_su
   return before + upto - count;
 }
 
-template <int V> __global__ void __launch_bounds__(THREADS) dvm_routing_kernel(const __grid_constant__ Args a) {
+template <int V> __global__ void __launch_bounds__(THREADS, 1) dvm_routing_kernel(const __grid_constant__ Args a) {
   __shared__ uint32_t chosen[DVM_MAX_EXPERTS], carry[DVM_MAX_EXPERTS], sums[WARPS];
-  __shared__ float rows[WARPS][V * 32];
+  __shared__ float bias[DVM_MAX_EXPERTS];
+  extern __shared__ float rows[];   // V * 33 to a warp, where there are groups
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int e = threadIdx.x; e < DVM_MAX_EXPERTS; e += THREADS) chosen[e] = carry[e] = 0u;
   grid_ready();
   grid_wait();
+  if (a.bias)
+    for (int e = threadIdx.x; e < a.experts; e += THREADS) bias[e] = a.bias[e];
   __syncthreads();
   const long long first = (long long)blockIdx.x * a.rounds * ROUND;
   for (int r = 0; r < a.rounds && first + r * ROUND < a.tokens; ++r) {
-    int mine[PER_WARP];
-#pragma unroll
-    for (int x = 0; x < PER_WARP; ++x) {
-      const int in_round = x * WARPS + warp;
-      const long long t = first + r * ROUND + in_round;
-      mine[x] = -1;
-      if (t >= a.tokens) continue;
-      float weight = 0.f;
-      if (!a.positions || a.positions[t] >= 0) mine[x] = choose<V>(a, t, rows[warp], &weight);
-      if (mine[x] >= 0) atomicOr(&chosen[mine[x]], 1u << in_round);
+    const long long t = first + r * ROUND + warp;
+    int mine = -1;
+    if (t < a.tokens) {
+      float l[V], weight = 0.f;
+      load_logits<V>(a, t, l);
+      if (!a.positions || a.positions[t] >= 0) mine = choose<V>(a, t, l, bias, rows + warp * (V * 33), &weight);
+      if (mine >= 0) atomicOr(&chosen[mine], 1u << warp);
       if (lane < a.top_k) {
-        a.ids[t * a.top_k + lane] = mine[x];
+        a.ids[t * a.top_k + lane] = mine;
         a.weights[t * a.top_k + lane] = weight;
       }
     }
     __syncthreads();
-#pragma unroll
-    for (int x = 0; x < PER_WARP; ++x) {
-      const int in_round = x * WARPS + warp;
-      const long long t = first + r * ROUND + in_round;
-      if (t < a.tokens && lane < a.top_k)
-        a.places[t * a.top_k + lane] = mine[x] < 0 ? -1 : (int)(carry[mine[x]] + __popc(chosen[mine[x]] & ((1u << in_round) - 1u)));
-    }
+    if (t < a.tokens && lane < a.top_k) a.places[t * a.top_k + lane] = mine < 0 ? -1 : (int)(carry[mine] + __popc(chosen[mine] & ((1u << warp) - 1u)));
     __syncthreads();
     for (int e = threadIdx.x; e < a.experts; e += THREADS) {
       carry[e] += __popc(chosen[e]);
@@ -329,10 +412,10 @@ template <int V> __global__ void __launch_bounds__(THREADS) dvm_routing_kernel(c
     return;
   }
   uint32_t total;
-  const uint32_t start = block_scan((int)threadIdx.x < a.experts ? carry[threadIdx.x] : 0u, sums, &total);
+  const uint32_t start = block_scan<WARPS>((int)threadIdx.x < a.experts ? carry[threadIdx.x] : 0u, sums, &total);
   if ((int)threadIdx.x < a.experts) a.starts[threadIdx.x] = (int)start;
   if (threadIdx.x == 0) a.starts[a.experts] = (int)total;
-  chosen[threadIdx.x] = start;
+  if (threadIdx.x < DVM_MAX_EXPERTS) chosen[threadIdx.x] = start;
   __syncthreads();
   for (int i = threadIdx.x; i < a.tokens * a.top_k; i += THREADS) {
     const int e = a.ids[i];
@@ -340,22 +423,37 @@ template <int V> __global__ void __launch_bounds__(THREADS) dvm_routing_kernel(c
   }
 }
 
-// The plan of several chunks: thread (s, p) adds up the counts of experts 2 p and 2 p + 1 over every s-th chunk.
-__global__ void __launch_bounds__(THREADS) dvm_routing_plan_kernel(const __grid_constant__ Args a) {
-  __shared__ uint32_t before[DVM_MAX_EXPERTS], all[DVM_MAX_EXPERTS], sums[WARPS];
-  for (int e = threadIdx.x; e < DVM_MAX_EXPERTS; e += THREADS) before[e] = all[e] = 0u;
+// The plan of several chunks, for PLAN of them: thread (s, p) adds up the counts of experts 2 p and 2 p + 1 over every s-th chunk.
+// The CTA's own choices and counts are on their way meanwhile.
+__global__ void __launch_bounds__(PLAN_THREADS) dvm_routing_plan_kernel(const __grid_constant__ Args a) {
+  constexpr int EACH = 2;   // choices of a thread that are asked for early
+  __shared__ uint32_t before[DVM_MAX_EXPERTS], all[DVM_MAX_EXPERTS], own[PLAN][DVM_MAX_EXPERTS], sums[PLAN_THREADS / 32];
+  for (int e = threadIdx.x; e < DVM_MAX_EXPERTS; e += PLAN_THREADS) before[e] = all[e] = 0u;
   grid_ready();
   grid_wait();
   __syncthreads();
-  const int pairs = (a.experts + 1) / 2, slices = THREADS / pairs, p = threadIdx.x % pairs, s = threadIdx.x / pairs;
+  const int pairs = (a.experts + 1) / 2, slices = PLAN_THREADS / pairs, p = threadIdx.x % pairs, s = threadIdx.x / pairs, mine = blockIdx.x * PLAN;
+  const long long chunk = (long long)a.rounds * ROUND * a.top_k, first = mine * chunk, last = min(first + PLAN * chunk, (long long)a.tokens * a.top_k);
+  int id[EACH], place[EACH];
+#pragma unroll
+  for (int x = 0; x < EACH; ++x) {
+    const long long i = first + threadIdx.x + x * PLAN_THREADS;
+    id[x] = i < last ? a.ids[i] : -1;
+    place[x] = i < last ? a.places[i] : 0;
+  }
+  uint32_t mine_n[PLAN] = {};
+  if (s == 0)
+#pragma unroll
+    for (int q = 0; q < PLAN; ++q)
+      if (mine + q < a.chunks) mine_n[q] = a.counts[(long long)(mine + q) * pairs + p];
   if (s < slices) {
     uint32_t b0 = 0, b1 = 0, n0 = 0, n1 = 0;
-#pragma unroll 8
+#pragma unroll 16
     for (int c = s; c < a.chunks; c += slices) {
       const uint32_t v = a.counts[(long long)c * pairs + p];
       n0 += v & 0xffffu;
       n1 += v >> 16;
-      if (c < (int)blockIdx.x) { b0 += v & 0xffffu; b1 += v >> 16; }
+      if (c < mine) { b0 += v & 0xffffu; b1 += v >> 16; }
     }
     atomicAdd(&before[2 * p], b0);   // (whole numbers: any order gives the same)
     atomicAdd(&before[2 * p + 1], b1);
@@ -364,21 +462,42 @@ __global__ void __launch_bounds__(THREADS) dvm_routing_plan_kernel(const __grid_
   }
   __syncthreads();
   uint32_t total;
-  const uint32_t start = block_scan((int)threadIdx.x < a.experts ? all[threadIdx.x] : 0u, sums, &total);
+  const uint32_t start = block_scan<PLAN_THREADS / 32>((int)threadIdx.x < a.experts ? all[threadIdx.x] : 0u, sums, &total);
   if (blockIdx.x == 0) {
     if ((int)threadIdx.x < a.experts) a.starts[threadIdx.x] = (int)start;
     if (threadIdx.x == 0) a.starts[a.experts] = (int)total;
   }
   before[threadIdx.x] += start;
   __syncthreads();
-  const long long chunk = (long long)a.rounds * ROUND * a.top_k, first = blockIdx.x * chunk;
-  const long long last = min(first + chunk, (long long)a.tokens * a.top_k);
-  for (long long i = first + threadIdx.x; i < last; i += THREADS) {
+  if (s == 0) {
+    uint32_t at0 = before[2 * p], at1 = before[2 * p + 1];
+#pragma unroll
+    for (int q = 0; q < PLAN; ++q) {
+      own[q][2 * p] = at0;
+      own[q][2 * p + 1] = at1;
+      at0 += mine_n[q] & 0xffffu;
+      at1 += mine_n[q] >> 16;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < EACH; ++x) {
+    const long long i = first + threadIdx.x + x * PLAN_THREADS;
+    if (id[x] >= 0) a.places[i] = place[x] + (int)own[(int)((i - first) / chunk)][id[x]];
+  }
+  for (long long i = first + threadIdx.x + EACH * PLAN_THREADS; i < last; i += PLAN_THREADS) {
     const int e = a.ids[i];
-    if (e >= 0) a.places[i] += (int)before[e];
+    if (e >= 0) a.places[i] += (int)own[(int)((i - first) / chunk)][e];
   }
 }
-static_assert(THREADS >= DVM_MAX_EXPERTS, "a thread per expert");
+static_assert(PLAN_THREADS >= DVM_MAX_EXPERTS, "a thread per expert");
+
+template <int V> int launch(const Args& a, int device, cudaStream_t stream) {
+  static std::atomic<uint64_t> allowed{0};
+  constexpr int BYTES = WARPS * V * 33 * 4;
+  const int st = dvm_allow_smem((const void*)dvm_routing_kernel<V>, BYTES, device, &allowed);
+  return st != DVM_OK ? st : dvm_launch_next(dvm_routing_kernel<V>, a.chunks, THREADS, a.groups > 1 ? BYTES : 0, stream, a);
+}
 
 }  // namespace routing
 }  // namespace dvm
@@ -396,9 +515,13 @@ int dvm_launch_routing(const dvm_routing_desc& d, void* const* t, cudaStream_t s
   a.tokens = (int)d.tokens; a.experts = (int)d.experts; a.top_k = d.top_k; a.groups = d.groups; a.top_groups = d.top_groups;
   a.chunks = (int)dvm_route_chunks(d); a.rounds = (int)dvm_route_rounds(d);
   a.bf16 = d.dtype == DVM_BF16; a.sigmoid = d.scoring == DVM_ROUTE_SIGMOID; a.renormalise = d.renormalise; a.factor = d.factor;
-  auto launch = [&](auto kernel) { return dvm_launch_next(kernel, a.chunks, THREADS, 0, stream, a); };
-  const int st = d.experts <= 64 ? launch(dvm_routing_kernel<2>) : d.experts <= 128 ? launch(dvm_routing_kernel<4>)
-                 : d.experts <= 256 ? launch(dvm_routing_kernel<8>) : launch(dvm_routing_kernel<16>);
+  a.lanes = 32;
+  while (a.lanes * a.groups > 32) a.lanes >>= 1;
+  DvmDeviceInfo dev;
+  int st = dvm_device_state(&dev);
+  if (st != DVM_OK) return st;
+  st = d.experts <= 64 ? launch<2>(a, dev.device, stream) : d.experts <= 128 ? launch<4>(a, dev.device, stream) : d.experts <= 256 ? launch<8>(a, dev.device, stream)
+       : launch<16>(a, dev.device, stream);
   if (st != DVM_OK || a.chunks == 1) return st;
-  return dvm_launch_next(dvm_routing_plan_kernel, a.chunks, THREADS, 0, stream, a);
+  return dvm_launch_next(dvm_routing_plan_kernel, (a.chunks + PLAN - 1) / PLAN, PLAN_THREADS, 0, stream, a);
 }
