@@ -117,8 +117,8 @@ typedef struct {
 } dvm_scaled_matmul_desc;
 int dvm_encode_scaled_matmul(const dvm_scaled_matmul_desc* d, void* code, size_t code_capacity, size_t* code_size);
 
-/* Rows of the tiles that the calling thread's last launch of a scaled product worked on (for tests and tools): 16, 32, 64 or
- * 128 in the kernel for few rows, 256 in the one for many.  DVM_ERR_INVALID_ARG before the thread's first. */
+/* Rows of the tiles that the calling thread's last launch of a scaled product worked on (for tests and tools): 16 or 64 in the
+ * kernel for few rows, 128 in the one for many.  DVM_ERR_INVALID_ARG before the thread's first. */
 int dvm_last_scaled_matmul_tile(int* rows);
 
 /* ---- combine: every token's rows added up by weight -------------------------------------------------------------------

@@ -206,11 +206,17 @@ CombineSlots dvm_slots(const dvm_combine_desc& d) {
   return s;
 }
 
-// The kernel goes by the rows of a group if they were dealt out evenly.  For few of them a tile is not wider than needed, as
-// its sums are scaled one by one whether a row fills them or not.
+// Which kernel takes a scaled product, by the rows of a group if they were dealt out evenly and by the tiles that gives.
+//  16  the weights' bytes are all that counts: up to 12 rows to a group (1024 rows of 128 experts, 4096 to 2816: 244 us, 277 in
+//      tiles of 64, 302 in the kernel for many), or up to 32 where the tiles do not fill the device (32 rows, 4096 to 4096: 9.9,
+//      10.0, 17.7)
+//  64  more rows, and still no more tiles than CTAs (128 rows, 4096 to 4096: 20.8, 13.0, 18.9; 256: 37, 18.4, 19.1)
+//  else the kernel for many (128 rows, 4096 to 11008: 50, 26, 19.6; 2048 rows of 64 experts, 4096 to 2816: 256, 169, 157; 512 of
+//      8, 2048 to 4096: 49, 30, 17.7)
 int dvm_scaled_tile(const dvm_scaled_matmul_desc& d) {
-  const int64_t each = dvm_up(d.rows, d.groups);
-  return each <= 16 ? 16 : each <= 32 ? 32 : each <= 64 ? 64 : each <= 160 ? 128 : 256;
+  const int64_t each = dvm_up(d.rows, d.groups), across = dvm_up(d.n, DVM_SCALE_BLOCK) * d.groups;
+  if (each <= 12 || (each <= 32 && dvm_up(each, 16) * across <= DVM_SCALED_UNITS)) return 16;
+  return dvm_up(each, 64) * across <= DVM_SCALED_UNITS ? 64 : DVM_SCALED_MANY;
 }
 
 extern "C" int dvm_encode_routing(const dvm_routing_desc* d, void* code, size_t code_capacity, size_t* code_size) { return encode(d, code, code_capacity, code_size); }

@@ -48,8 +48,9 @@ inline int64_t dvm_routing_workspace(const dvm_routing_desc& d) {
 
 // Scaled products: CTAs that share the work of the kernel for few rows (one per SM of a B200), and the rows of its tiles.
 #define DVM_SCALED_UNITS 148
+#define DVM_SCALED_MANY 128   // rows of a tile of the kernel for many (16 or 64 in the one for few)
 int dvm_scaled_tile(const dvm_scaled_matmul_desc& d);
 inline int64_t dvm_scaled_workspace(const dvm_scaled_matmul_desc& d) {
   const int tile = dvm_scaled_tile(d);
-  return d.rows && tile <= 128 ? (int64_t)DVM_SCALED_UNITS * (32 + 2 * 128 * tile * 4) : 0;
+  return d.rows && tile != DVM_SCALED_MANY ? (int64_t)DVM_SCALED_UNITS * (32 + 2 * 128 * tile * 4) : 0;
 }

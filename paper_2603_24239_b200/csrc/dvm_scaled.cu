@@ -61,13 +61,13 @@ int dvm_launch_scaled_matmul(const dvm_scaled_matmul_desc& d, void* const* t, cu
   a.k_blocks = (int)dvm_up(d.k, DVM_SCALE_BLOCK); a.n_blocks = (int)dvm_up(d.n, DVM_SCALE_BLOCK);
   a.out_bf16 = d.out_dtype == DVM_BF16;
   const int tile = dvm_scaled_tile(d), es = a.out_bf16 ? 2 : 4;
-  const bool many = tile > 128;
+  const bool many = tile == DVM_SCALED_MANY;
   a.out_tma = (uintptr_t)a.out % 16 == 0 && (d.rows <= 1 || (d.out_stride * es % 16 == 0 && d.out_stride * es < (1ll << 40)));
   CUtensorMap x, w, out = {};
   const cuuint64_t xd[2] = {(cuuint64_t)d.k, (cuuint64_t)d.rows}, xt[1] = {map_stride(d.rows, d.x_stride)};
   const cuuint64_t wd[3] = {(cuuint64_t)d.k, (cuuint64_t)d.n, (cuuint64_t)d.groups}, wt[2] = {map_stride(d.n, d.w_stride[1]), map_stride(d.groups, d.w_stride[0])};
   const cuuint64_t od[2] = {(cuuint64_t)d.n, (cuuint64_t)d.rows}, ot[1] = {map_stride(d.rows, d.out_stride * es)};
-  st = encode_map(&x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, t[s.x], 2, xd, xt, many ? 128 : tile);
+  st = encode_map(&x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, t[s.x], 2, xd, xt, many ? 128 : 16);
   if (st == DVM_OK) st = encode_map(&w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, t[s.w], 3, wd, wt, many ? 256 : 128);
   if (st == DVM_OK && many && a.out_tma) st = encode_map(&out, a.out_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, es, a.out, 2, od, ot, 32);
   if (st == DVM_OK) st = many ? dvm_launch_scaled_many(x, w, out, a, dev.sm_count, dev.device, stream) : dvm_launch_scaled_few(x, w, a, tile, dev.device, stream);

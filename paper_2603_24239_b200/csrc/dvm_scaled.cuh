@@ -13,6 +13,7 @@ namespace scaled {
 
 using namespace sm100;
 
+constexpr uint32_t ALL = 0xffffffffu;
 constexpr int BLOCK = DVM_SCALE_BLOCK;   // columns of k of one step: they share their scales
 
 struct Args {

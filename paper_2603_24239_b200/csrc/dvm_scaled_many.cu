@@ -155,17 +155,21 @@ dvm_scaled_many_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_co
   uint32_t issued = 0, f_stage = 0, f_phase = 0;   // the fetching thread's ring, kept for the abort path
   if (warp == 0) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
-    if (lane == 0)
-      for (bool ok = tile.at(); ok; ok = ok && tile.next())
-        for (int kb = 0; kb < a.k_blocks; ++kb) {
-          if (!mbar_wait_flat(bar_done + 8 * f_stage, f_phase ^ 1, abort_flag, idle)) { ok = false; break; }
-          const uint32_t at = base + f_stage * S::STAGE, full = bar_full + 8 * f_stage;
+    const bool leader = elect_one();
+    bool ok = true;
+    for (bool some = tile.at(); ok && some; some = tile.next())
+      for (int kb = 0; kb < a.k_blocks; ++kb) {
+        ok = __all_sync(ALL, mbar_wait_flat(bar_done + 8 * f_stage, f_phase ^ 1, abort_flag, idle));
+        if (!ok) break;
+        const uint32_t at = base + f_stage * S::STAGE, full = bar_full + 8 * f_stage;
+        if (leader) {
           mbar_expect_tx(full, S::STAGE);
           tma_load_2d(at, &tm_x, full, kb * BLOCK, tile.first);
           tma_load_3d(at + S::X, &tm_w, full, kb * BLOCK, tile.n0, tile.g);
-          ++issued;
-          if (++f_stage == MANY_STAGES) { f_stage = 0; f_phase ^= 1; }
         }
+        ++issued;
+        if (++f_stage == MANY_STAGES) { f_stage = 0; f_phase ^= 1; }
+      }
     __syncwarp();
   } else if (warp == 1) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
@@ -175,7 +179,7 @@ dvm_scaled_many_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_co
     bool ok = true;
     for (bool some = tile.at(); ok && some; some = tile.next())
       for (int kb = 0; ok && kb < a.k_blocks; ++kb) {
-        ok = __all_sync(0xffffffffu, mbar_wait_flat(bar_free + 8 * buffer, b_phase ^ 1, abort_flag, idle) && mbar_wait_flat(bar_full + 8 * stage, phase, abort_flag, idle));
+        ok = __all_sync(ALL, mbar_wait_flat(bar_free + 8 * buffer, b_phase ^ 1, abort_flag, idle) && mbar_wait_flat(bar_full + 8 * stage, phase, abort_flag, idle));
         if (!ok) break;
         tc_fence_after();
         if (leader) {
@@ -204,7 +208,7 @@ dvm_scaled_many_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_co
       // threads 0 .. 2 AHEAD - 1: block i % AHEAD of half i / AHEAD
       const float* const ws = a.ws + ((long long)tile.g * a.n_blocks + min(tile.n0 / BLOCK + i / AHEAD, a.n_blocks - 1)) * a.k_blocks + i % AHEAD;
       for (int kb = 0; kb < a.k_blocks; kb += AHEAD) {
-        ok = __all_sync(0xffffffffu, mbar_wait_flat(bar_read + 8 * slot, phase ^ 1, abort_flag, idle));
+        ok = __all_sync(ALL, mbar_wait_flat(bar_read + 8 * slot, phase ^ 1, abort_flag, idle));
         if (!ok) break;
         const uint32_t x = base + S::XS + slot * (AHEAD * MANY_M * 4) + i * 4;
 #pragma unroll
@@ -234,7 +238,7 @@ dvm_scaled_many_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_co
       float by[AHEAD];
       for (int kb = 0; kb < a.k_blocks; ++kb) {
         if (kb % AHEAD == 0) {
-          ok = __all_sync(0xffffffffu, mbar_wait_flat(bar_laid + 8 * slot, s_phase, abort_flag, idle));
+          ok = __all_sync(ALL, mbar_wait_flat(bar_laid + 8 * slot, s_phase, abort_flag, idle));
           if (!ok) break;
           const float4 w = *(const float4*)(ws + slot * 2 * AHEAD);
           const float* const x = xs + slot * AHEAD * MANY_M;
@@ -243,7 +247,7 @@ dvm_scaled_many_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_co
           if (lane == 0) mbar_arrive(bar_read + 8 * slot);
           if (++slot == 2) { slot = 0; s_phase ^= 1; }
         }
-        ok = __all_sync(0xffffffffu, mbar_wait_flat(bar_done + 8 * stage, phase, abort_flag, idle));
+        ok = __all_sync(ALL, mbar_wait_flat(bar_done + 8 * stage, phase, abort_flag, idle));
         if (!ok) break;
         if (++stage == MANY_STAGES) { stage = 0; phase ^= 1; }
         tc_fence_after();
