@@ -58,8 +58,8 @@ extern "C" {
  * With `masked`, tokens of negative positions[t] (rows behind the last one of a padded batch) take no part: ids -1,
  * weights 0, places -1.
  * Tensors: logits [tokens, experts], bias [experts] fp32 (`biased` only), positions [tokens] (`masked` only) -> ids, weights
- * (fp32), places [tokens, top_k], starts [experts + 1], workspace (dvm_tensor_extents gives its bytes; any pointer, NULL too,
- * where that is 0).
+ * (fp32), places [tokens, top_k], starts [experts + 1], workspace (dvm_tensor_extents gives its bytes; 16-byte aligned; any
+ * pointer, NULL too, where that is 0).
  * DVM_ERR_TOO_LARGE: more experts or top_k than above, more than 32 groups or 2^23 tokens. */
 enum { DVM_ROUTE_SOFTMAX = 0, DVM_ROUTE_SIGMOID = 1 };
 typedef struct {

@@ -57,7 +57,7 @@ int check(const dvm_combine_desc& d) {
 }
 
 // Pieces of work, 0 for an instance that launches nothing.
-int64_t tiles_of(const dvm_routing_desc& d) { return 1 + d.tokens / DVM_ROUTE_ROUND; }  // (no tokens: starts are still written)
+int64_t tiles_of(const dvm_routing_desc& d) { return 1 + d.tokens / DVM_ROUTE_ONE; }  // (no tokens: starts are still written)
 int64_t tiles_of(const dvm_quantize_desc& d) { return d.out_rows ? d.rows : 0; }
 int64_t tiles_of(const dvm_scaled_matmul_desc& d) { return d.rows; }
 int64_t tiles_of(const dvm_combine_desc& d) { return d.rows ? d.tokens : 0; }

@@ -29,21 +29,21 @@ int dvm_launch_experts(const uint32_t* w, void* const* tensors, int n_tensors, c
 
 inline int64_t dvm_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Routing: tokens are taken in rounds of 32, by chunks of whole rounds; a chunk is one CTA.
-#define DVM_ROUTE_ROUND 32
-#define DVM_ROUTE_CHUNKS 296
+// Routing: tokens are taken in rounds, a warp to each, by chunks of whole rounds; a chunk is one CTA.  Up to DVM_ROUTE_ONE tokens
+// are one round; more go in rounds of DVM_ROUTE_ROUND, and a chunk has at most 15 of these: its counts are bytes.
+#define DVM_ROUTE_ONE 32
+#define DVM_ROUTE_ROUND 16
+#define DVM_ROUTE_CHUNKS 592
 inline int64_t dvm_route_rounds(const dvm_routing_desc& d) {  // rounds of one chunk
-  const int64_t rounds = dvm_up(d.tokens, DVM_ROUTE_ROUND);
-  return rounds <= 1 ? 1 : dvm_up(rounds, DVM_ROUTE_CHUNKS);
+  if (d.tokens <= DVM_ROUTE_ONE) return 1;
+  const int64_t rounds = dvm_up(dvm_up(d.tokens, DVM_ROUTE_ROUND), DVM_ROUTE_CHUNKS);
+  return rounds < 15 ? rounds : 15;
 }
-inline int64_t dvm_route_chunks(const dvm_routing_desc& d) {
-  const int64_t n = dvm_up(d.tokens, DVM_ROUTE_ROUND * dvm_route_rounds(d));
-  return n < 1 ? 1 : n;
-}
-// bytes of its workspace: tokens of every expert in every chunk, 16 bits each, where there are several
+inline int64_t dvm_route_chunks(const dvm_routing_desc& d) { return d.tokens <= DVM_ROUTE_ONE ? 1 : dvm_up(d.tokens, DVM_ROUTE_ROUND * dvm_route_rounds(d)); }
+// bytes of its workspace: tokens of every expert in every chunk, where there are several
 inline int64_t dvm_routing_workspace(const dvm_routing_desc& d) {
   const int64_t chunks = dvm_route_chunks(d);
-  return chunks > 1 ? chunks * dvm_up(d.experts, 2) * 4 : 0;
+  return chunks > 1 ? chunks * dvm_up(d.experts, 16) * 16 : 0;
 }
 
 // Scaled products: CTAs that share the work of the kernel for few rows (one per SM of a B200), and the rows of its tiles.

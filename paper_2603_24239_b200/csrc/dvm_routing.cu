@@ -1,16 +1,23 @@
 // Routing meta-kernel: scores of a token's experts, the best ones in exact order, their weights, and the plan: the tokens'
 // rows, expert by expert.
 //
-// A warp takes a token, lane l its experts l, l + 32, ...  The chosen ones are found one by one: the largest key of the warp,
-// keys being the values c as unsigned integers of the same order, and of equal ones the lowest index (two warp reductions
-// a round).  Without a bias the order of c is the order of the logits, which need no rounding; with one, or for groups, c is
-// rounded, so where two neighbours in the order (or the last group that stays and the first that does not) are nearer
-// than the roundings could move them, the token is done again in 64 bits: some tokens in ten thousand.
+// A warp takes a token, lane l its experts l, l + 32, ...  Keys are the values c as unsigned integers of the same order, with the
+// lowest bits given to the place in the lane: each lane sorts its keys (a maximum and a minimum to a trade), then the chosen ones
+// are found one by one: the largest head of the warp, of equal ones the lowest index (two warp reductions a round).
+// That order is exact but where two neighbours in it -- the last one chosen and those behind it included -- are as near as
+// the roundings of c and the bits left out could move them; those are put in order in 64 bits (without a bias by the logits, whose
+// order is that of c): some tokens in a thousand.
 //
-// The plan is a counting sort without atomics whose order could change it.  Tokens go in rounds of 32, and a round's choices
-// are a bit per token in a word per expert: a token's rank at its expert is the number of bits below its own, plus what
-// earlier rounds of the chunk counted.  With up to 32 tokens one CTA does it all; else every CTA leaves its chunk's counts in
-// the workspace and a second launch adds up those of the chunks before.
+// The plan is a counting sort without atomics whose order could change it.  Tokens go in rounds, a warp to each, and a round's
+// choices are a bit per token in a word per expert: a token's rank at its expert is the number of bits below its own, plus what
+// earlier rounds of the chunk counted.  Up to 32 tokens are one round of one CTA, which does it all; else every CTA leaves its
+// chunk's counts in the workspace, a byte each, and a second launch adds up those of the chunks before.
+// 8191 tokens of 256 experts in 8 groups with a bias: 32 us (19 without both), 64 tokens 9.7, one token 3.9.  Bound by
+// instructions: 2.1 us would read the logits, but a token costs 870 instructions without groups or bias (a load, a score, a sort of
+// 8 keys and 8 rounds of two reductions) and 1530 with both, 13 and 20 us of the first launch.  A warp per token was taken over a
+// CTA per token (whose barriers made 8191 tokens 96 us) and over a thread per token (64 tokens leave the GPU empty).  The second
+// launch, 8 us, reads every chunk's counts per 4 chunks; 16 bytes to a load and additions of two counts to an instruction took it
+// there from 20.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -20,8 +27,7 @@
 namespace dvm {
 namespace routing {
 
-constexpr int ROUND = DVM_ROUTE_ROUND, WARPS = ROUND, THREADS = WARPS * 32;   // a warp to a token of a round
-constexpr int PLAN = 4, PLAN_THREADS = 512;                                    // of the second launch: chunks of a CTA
+constexpr int PLAN = 4, PLAN_THREADS = 512;   // of the second launch: chunks of a CTA
 constexpr uint32_t ALL = 0xffffffffu;
 
 struct Args {
@@ -30,19 +36,23 @@ struct Args {
   const int* positions;
   int *ids, *places, *starts;
   float* weights;
-  uint32_t* counts;    // [chunks][experts / 2]: 16 bits each
+  uint32_t* counts;    // [chunks][experts, rounded up to 16]: 8 bits each
   long long stride;
   int tokens, experts, top_k, groups, top_groups, chunks, rounds;
   int bf16, sigmoid, renormalise;
   int lanes;           // of a warp to a group: the largest power of two
+  int quads, quads_up; // of the second launch
   float factor;
 };
 
-// Keys: 0 for what cannot be chosen, 1 for NaN, then the order of the values.
+// Keys: 0 for what cannot be chosen, NAN_KEY for NaN, then the order of the values.
+constexpr uint32_t NAN_KEY = 16u;
 __device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t b = __float_as_uint(x + 0.f);   // (-0 is 0)
-  return x != x ? 1u : b ^ ((uint32_t)((int)b >> 31) | 0x80000000u);
+  return x != x ? NAN_KEY : b ^ ((uint32_t)((int)b >> 31) | 0x80000000u);
 }
+// The same with the place i of V in the lane in its lowest bits, the first place the highest.
+template <int V> __device__ __forceinline__ uint32_t key_at(uint32_t key, int i) { return (key & ~(uint32_t)(V - 1)) | (uint32_t)(V - 1 - i); }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 __device__ __forceinline__ float logit_at(const Args& a, long long t, int e) {
   return a.bf16 ? __bfloat162float(((const __nv_bfloat16*)a.logits)[t * a.stride + e]) : ((const float*)a.logits)[t * a.stride + e];
@@ -59,13 +69,26 @@ template <class T> __device__ __forceinline__ T warp_sum(T v) {
 }
 
 // How near two values c are when 32 bits may have swapped them: twice what each may be off, in units of 2^-24.  A sigmoid: the
-// exponential's error, 2 ulp and 1.2 per unit of its argument, times s (1 - s), a sum and a quotient (2 ulp): less than 10.  Of a
+// exponential's error, 2 ulp and 1.2 per unit of its argument, times s (1 - s), a sum and a reciprocal (1 ulp): less than 10.  Of a
 // softmax every score is at most 1 / sum; exponentials (at most 5), up to 16 + 5 additions and the quotient are less than 36
 // of that.  The bias adds a rounding of c itself.
 __device__ __forceinline__ float doubt(float unit, float c) { return 0x1p-23f * (unit + 2.f * fabsf(c)); }
-// Score of a logit: 1 / (1 + exp(-l)), or exp(l - top) / sum.
-__device__ __forceinline__ float score(const Args& a, float l, float top, float sum) {
-  return a.sigmoid ? __fdividef(1.f, 1.f + __expf(-l)) : __fdividef(__expf(l - top), sum);
+// ... and of two keys without their lowest bits, which are less than V units in the last place (of at most 2^-23 of the value).
+// Values by logits are not rounded (unit 0).
+template <int V> __device__ __forceinline__ bool near_keys(uint32_t more, uint32_t less, float unit) {
+  if (less < 2 * NAN_KEY) return false;   // (NaN, or nothing)
+  const float x = of_key(more & ~(uint32_t)(V - 1)), y = of_key(less & ~(uint32_t)(V - 1));
+  return x - y <= fmaxf(fabsf(x), fabsf(y)) * (V * 0x1p-22f) + 0x1p-23f * unit;   // (infinite minus infinite: not near, the index decides)
+}
+__device__ __forceinline__ float exp_near(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * 1.4426950408889634f));
+  return y;
+}
+__device__ __forceinline__ float rcp_near(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 // The group of every expert of this lane (experts behind the last: group 32, which is none).
@@ -141,6 +164,9 @@ template <int V> __device__ __noinline__ int choose_exactly(const Args& a, long 
     }
     stay = __ballot_sync(ALL, lane < a.groups && before < a.top_groups);
   }
+  if (!a.bias)   // ranked by the logits, which tell apart what scores of 64 bits do not
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = 32 * i + lane < a.experts ? (double)logit_at(a, t, 32 * i + lane) : -INFINITY;
   uint32_t free = 0;   // bits of the experts of this lane that may be chosen
 #pragma unroll
   for (int i = 0; i < V; ++i)
@@ -170,33 +196,36 @@ template <int V> __device__ __noinline__ int choose_exactly(const Args& a, long 
 
 // This lane's logits of a token.
 template <int V> __device__ __forceinline__ void load_logits(const Args& a, long long t, float (&l)[V]) {
+  const int lane = threadIdx.x & 31;
+  if (a.bf16) {
+    const __nv_bfloat16* p = (const __nv_bfloat16*)a.logits + t * a.stride + lane;
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int e = 32 * i + (threadIdx.x & 31);
-    l[i] = e < a.experts ? logit_at(a, t, e) : -INFINITY;
+    for (int i = 0; i < V; ++i) l[i] = 32 * i + lane < a.experts ? __bfloat162float(p[32 * i]) : -INFINITY;
+  } else {
+    const float* p = (const float*)a.logits + t * a.stride + lane;
+#pragma unroll
+    for (int i = 0; i < V; ++i) l[i] = 32 * i + lane < a.experts ? p[32 * i] : -INFINITY;
   }
 }
 
 // The first `found` lanes hold the largest values of a token in nearly their order: the j-th in exact order goes to lane j.  (NaN
 // keep their places: they are the last.)
-template <int V> __device__ __noinline__ int order_exactly(const Args& a, const float (&l)[V], float top, float mine_l, float b, int mine, uint32_t key, int found) {
+template <int V> __device__ __noinline__ int order_exactly(const Args& a, long long t, float top, float mine_l, float b, int mine, uint32_t key, int found) {
   const int lane = threadIdx.x & 31;
-  double c;
-  if (a.sigmoid) {
-    c = 1.0 / (1.0 + exp(-(double)mine_l));
-  } else {
+  double c = (double)mine_l;
+  if (a.bias && a.sigmoid) {
+    c = 1.0 / (1.0 + exp(-c)) + (double)b;
+  } else if (a.bias) {
     double sum = 0.0;
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (32 * i + lane < a.experts) sum += exp((double)l[i] - top);
-    c = exp((double)mine_l - top) / warp_sum(sum);
+#pragma unroll 1
+    for (int i = lane; i < a.experts; i += 32) sum += exp((double)logit_at(a, t, i) - top);
+    c = exp(c - top) / warp_sum(sum) + (double)b;
   }
-  c += (double)b;
   int before = 0;
   for (int j = 0; j < found; ++j) {
     const double o = __shfl_sync(ALL, c, j);
     const int oi = __shfl_sync(ALL, mine, j);
-    const bool o_nan = __shfl_sync(ALL, key, j) <= 1u, nan = key <= 1u;
+    const bool o_nan = __shfl_sync(ALL, key, j) < 2 * NAN_KEY, nan = key < 2 * NAN_KEY;
     before += o_nan || nan ? j < lane : o > c || (o == c && oi < mine);
   }
   int result = -1;
@@ -207,24 +236,22 @@ template <int V> __device__ __noinline__ int order_exactly(const Args& a, const 
   return lane < a.top_k ? result : -1;
 }
 
-// The largest of a lane's keys and its expert, of equal ones the lowest.
-template <int V> __device__ __forceinline__ void largest(const uint32_t (&key)[V], uint32_t* best, int* at) {
-  uint32_t k[V];
-  int e[V];
+// A lane's keys in descending order.  Neighbours of every other pair trade places in turn.
+template <int V> __device__ __forceinline__ void sort_keys(uint32_t (&key)[V]) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) { k[i] = key[i]; e[i] = 32 * i + (threadIdx.x & 31); }
+  for (int round = 0; round < V; ++round)
 #pragma unroll
-  for (int d = 1; d < V; d <<= 1)
-#pragma unroll
-    for (int i = 0; i < V; i += 2 * d)
-      if (k[i + d] > k[i]) { k[i] = k[i + d]; e[i] = e[i + d]; }
-  *best = k[0];
-  *at = e[0];
+    for (int i = round & 1; i + 1 < V; i += 2) {
+      const uint32_t more = max(key[i], key[i + 1]);
+      key[i + 1] = min(key[i], key[i + 1]);
+      key[i] = more;
+    }
 }
 
-// Lane j's choice of token t and its weight.  V: experts of a lane at most; l: this lane's logits; bias: all of them, in shared
+// Lane j's choice of token t and its weight.  V: experts of a lane at most; SCORED: ranked by scores (there is a bias, or groups are
+// compared), else by the logits, which have their order; l: this lane's logits; bias: all of them, in shared
 // memory; row: this warp's row of shared memory.
-template <int V> __device__ __forceinline__ int choose(const Args& a, long long t, const float (&l)[V], const float* bias, float* row, float* weight) {
+template <int V, bool SCORED> __device__ __forceinline__ int choose(const Args& a, long long t, const float (&l)[V], const float* bias, float* row, float* weight) {
   const int lane = threadIdx.x & 31;
   float top = -INFINITY, sum = 0.f;
   uint32_t key[V];
@@ -239,22 +266,34 @@ template <int V> __device__ __forceinline__ int choose(const Args& a, long long 
     if (__any_sync(ALL, nan)) top = NAN;
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      if (32 * i + lane < a.experts) sum += __expf(l[i] - top);
+      if (32 * i + lane < a.experts) sum += exp_near(l[i] - top);
     sum = warp_sum(sum);
   }
   bool unsure = false;
   const float unit = a.sigmoid ? 10.f : 36.f / sum;
-  if (a.bias || a.groups > 1) {
+  if (SCORED) {
+    const float inv_sum = rcp_near(sum);
+    float c[V];
+    if (a.sigmoid) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int e = 32 * i + lane;
-      key[i] = 0u;
-      if (e < a.experts) {
-        const float c = score(a, l[i], top, sum) + (a.bias ? bias[e] : 0.f);
-        key[i] = key_of(a.bias ? c : l[i]);
-        if (a.groups > 1) row[e + (e >> 5)] = c;   // (a word left out of every 33: groups of 32 in different banks)
-      }
+      for (int i = 0; i < V; ++i) c[i] = rcp_near(1.f + exp_near(-l[i]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) c[i] = exp_near(l[i] - top) * inv_sum;
     }
+    if (a.bias) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        c[i] += bias[32 * i + lane];   // (of experts behind the last: anything)
+        key[i] = 32 * i + lane < a.experts ? key_at<V>(key_of(c[i]), i) : 0u;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) key[i] = 32 * i + lane < a.experts ? key_at<V>(key_of(l[i]), i) : 0u;
+    }
+    if (a.groups > 1)
+#pragma unroll
+      for (int i = 0; i < V; ++i) row[33 * i + lane] = c[i];   // (a word left out of every 33: groups of 32 in different banks)
     if (a.groups > 1) {
       // every group by a.lanes lanes, which take its experts in turn and merge what they found
       __syncwarp();
@@ -276,7 +315,7 @@ template <int V> __device__ __forceinline__ int choose(const Args& a, long long 
         first = fmaxf(first, of);
       }
       // (every lane of a group has its key; lanes of no group the lowest)
-      const uint32_t mine = g < a.groups ? (bad ? 1u : key_of(per > 1 ? first + second : first)) : 0u;
+      const uint32_t mine = g < a.groups ? (bad ? NAN_KEY : key_of(per > 1 ? first + second : first)) : 0u;
       int before = 0;
       for (int o = 0; o < a.groups; ++o) {
         const uint32_t other = __shfl_sync(ALL, mine, o * a.lanes);
@@ -286,7 +325,7 @@ template <int V> __device__ __forceinline__ int choose(const Args& a, long long 
       const uint32_t stay = __ballot_sync(ALL, in);
       if (a.top_groups < a.groups) {
         const uint32_t least = __reduce_min_sync(ALL, in ? mine : ALL), most = __reduce_max_sync(ALL, in ? 0u : mine);
-        if (most > 1u) {
+        if (most > NAN_KEY) {
           const float x = of_key(least), y = of_key(most);
           // (a sum of two values: both may be off, and their sum is rounded)
           unsure = x - y <= 2.f * doubt(unit, fmaxf(fabsf(x), fabsf(y)));
@@ -300,44 +339,39 @@ template <int V> __device__ __forceinline__ int choose(const Args& a, long long 
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) key[i] = 32 * i + lane < a.experts ? key_of(l[i]) : 0u;
+    for (int i = 0; i < V; ++i) key[i] = 32 * i + lane < a.experts ? key_at<V>(key_of(l[i]), i) : 0u;
   }
-  // ---- the largest keys, one after another; with a bias also those so near the last one that they may be above it ----
-  uint32_t mine_key = 0u, last_key = 0u, best = 0u;
-  int mine = -1, at = 0, found = 0;
-  largest<V>(key, &best, &at);
+  // ---- the largest keys, one after another, and those behind the last one that may be above it ----
+  const float rank_unit = SCORED && a.bias ? unit : 0.f;
+  uint32_t mine_key = 0u, last_key = 0u;
+  int mine = -1, found = 0;
+  sort_keys<V>(key);
   for (;;) {
-    const uint32_t most = __reduce_max_sync(ALL, best);
+    const uint32_t most = __reduce_max_sync(ALL, key[0]);
     if (found >= a.top_k) {
-      if (!a.bias || most <= 1u || last_key <= 1u || of_key(last_key) - of_key(most) > doubt(unit, fmaxf(fabsf(of_key(last_key)), fabsf(of_key(most))))) break;
+      if (!near_keys<V>(last_key, most, rank_unit)) break;
       if (found == 32) { unsure = true; break; }
     }
-    const int won = (int)__reduce_min_sync(ALL, best == most ? (uint32_t)at : ALL);
+    const uint32_t at = (V - 1 - (key[0] & (V - 1))) * 32u + lane;
+    const int won = (int)__reduce_min_sync(ALL, key[0] == most ? at : ALL);
     if (lane == found) { mine = won; mine_key = most; }
     if (++found == a.top_k) last_key = most;
-    if (lane == (won & 31)) {
+    if (at == (uint32_t)won) {   // (its lane goes on to its next)
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (32 * i + lane == won) key[i] = 0u;
-      largest<V>(key, &best, &at);
+      for (int i = 0; i + 1 < V; ++i) key[i] = key[i + 1];
+      key[V - 1] = 0u;
     }
-    __syncwarp();
   }
   float mine_l = mine >= 0 ? logit_at(a, t, mine) : 0.f;
-  if (a.bias) {
-    const float b = mine >= 0 ? bias[mine] : 0.f;
-    const uint32_t next_key = __shfl_down_sync(ALL, mine_key, 1);
-    const float next_l = __shfl_down_sync(ALL, mine_l, 1), next_b = __shfl_down_sync(ALL, b, 1);
-    bool near = false;
-    if (lane < found - 1 && next_key > 1u && mine_key > 1u) {
-      const float x = of_key(mine_key), y = of_key(next_key);
-      // (the same logit and bias: the index decides, here as in 64 bits)
-      near = x - y <= doubt(unit, fmaxf(fabsf(x), fabsf(y))) && !(mine_l == next_l && b == next_b);
-    }
-    if (__any_sync(ALL, near) && !__any_sync(ALL, unsure)) mine = order_exactly<V>(a, l, top, mine_l, b, mine, mine_key, found);
-  }
-  if (__any_sync(ALL, unsure)) mine = choose_exactly<V>(a, t);
-  mine_l = mine >= 0 ? logit_at(a, t, mine) : 0.f;
+  const float b = SCORED && a.bias && mine >= 0 ? bias[mine] : 0.f;
+  const uint32_t next_key = __shfl_down_sync(ALL, mine_key, 1);
+  const float next_l = __shfl_down_sync(ALL, mine_l, 1), next_b = __shfl_down_sync(ALL, b, 1);
+  // (the same logit and bias: the index decides, here as in 64 bits)
+  const bool near = lane < found - 1 && near_keys<V>(mine_key, next_key, rank_unit) && !(mine_l == next_l && b == next_b);
+  const bool redo = __any_sync(ALL, unsure);
+  if (redo) mine = choose_exactly<V>(a, t);
+  else if (__any_sync(ALL, near)) mine = order_exactly<V>(a, t, top, mine_l, b, mine, mine_key, found);
+  if (redo || found > a.top_k || __any_sync(ALL, near)) mine_l = mine >= 0 ? logit_at(a, t, mine) : 0.f;
   float s = a.sigmoid ? 1.f / (1.f + expf(-mine_l)) : expf(mine_l - top) / sum;
   if (a.renormalise) {
     const float total = warp_sum(lane < a.top_k ? s : 0.f);
@@ -372,7 +406,8 @@ template <int WARPS> __device__ __forceinline__ uint32_t block_scan(uint32_t cou
   return before + upto - count;
 }
 
-template <int V> __global__ void __launch_bounds__(THREADS, 1) dvm_routing_kernel(const __grid_constant__ Args a) {
+template <int V, bool SCORED, int WARPS> __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) dvm_routing_kernel(const __grid_constant__ Args a) {
+  constexpr int THREADS = WARPS * 32;
   __shared__ uint32_t chosen[DVM_MAX_EXPERTS], carry[DVM_MAX_EXPERTS], sums[WARPS];
   __shared__ float bias[DVM_MAX_EXPERTS];
   extern __shared__ float rows[];   // V * 33 to a warp, where there are groups
@@ -380,17 +415,17 @@ template <int V> __global__ void __launch_bounds__(THREADS, 1) dvm_routing_kerne
   for (int e = threadIdx.x; e < DVM_MAX_EXPERTS; e += THREADS) chosen[e] = carry[e] = 0u;
   grid_ready();
   grid_wait();
-  if (a.bias)
+  if (SCORED && a.bias)
     for (int e = threadIdx.x; e < a.experts; e += THREADS) bias[e] = a.bias[e];
   __syncthreads();
-  const long long first = (long long)blockIdx.x * a.rounds * ROUND;
-  for (int r = 0; r < a.rounds && first + r * ROUND < a.tokens; ++r) {
-    const long long t = first + r * ROUND + warp;
+  const long long first = (long long)blockIdx.x * a.rounds * WARPS;
+  for (int r = 0; r < a.rounds && first + r * WARPS < a.tokens; ++r) {
+    const long long t = first + r * WARPS + warp;
     int mine = -1;
     if (t < a.tokens) {
       float l[V], weight = 0.f;
       load_logits<V>(a, t, l);
-      if (!a.positions || a.positions[t] >= 0) mine = choose<V>(a, t, l, bias, rows + warp * (V * 33), &weight);
+      if (!a.positions || a.positions[t] >= 0) mine = choose<V, SCORED>(a, t, l, bias, rows + warp * (V * 33), &weight);
       if (mine >= 0) atomicOr(&chosen[mine], 1u << warp);
       if (lane < a.top_k) {
         a.ids[t * a.top_k + lane] = mine;
@@ -406,97 +441,143 @@ template <int V> __global__ void __launch_bounds__(THREADS, 1) dvm_routing_kerne
     }
     __syncthreads();
   }
-  if (a.chunks > 1) {
-    for (int e = 2 * threadIdx.x; e < a.experts; e += 2 * THREADS)
-      a.counts[(long long)blockIdx.x * ((a.experts + 1) / 2) + e / 2] = carry[e] | (carry[e + 1] << 16);   // (an odd last one: carry[experts] is 0)
+  if (a.chunks > 1) {   // (the counts of experts behind the last are 0)
+    const int words = (a.experts + 15) / 16 * 4;
+    for (int q = threadIdx.x; q < words; q += THREADS)
+      a.counts[(long long)blockIdx.x * words + q] = carry[4 * q] | (carry[4 * q + 1] << 8) | (carry[4 * q + 2] << 16) | (carry[4 * q + 3] << 24);
     return;
   }
-  uint32_t total;
-  const uint32_t start = block_scan<WARPS>((int)threadIdx.x < a.experts ? carry[threadIdx.x] : 0u, sums, &total);
-  if ((int)threadIdx.x < a.experts) a.starts[threadIdx.x] = (int)start;
-  if (threadIdx.x == 0) a.starts[a.experts] = (int)total;
-  if (threadIdx.x < DVM_MAX_EXPERTS) chosen[threadIdx.x] = start;
-  __syncthreads();
+  // one CTA: the starts, thread e expert e (up to 32 experts more to a warp than it has threads: a loop over the lanes' carries)
+  uint32_t before = 0u;
+  for (int e0 = 0; e0 < a.experts; e0 += THREADS) {
+    const int e = e0 + (int)threadIdx.x;
+    uint32_t total;
+    const uint32_t start = before + block_scan<WARPS>(e < a.experts ? carry[e] : 0u, sums, &total);
+    if (e < a.experts) {
+      a.starts[e] = (int)start;
+      chosen[e] = start;
+    }
+    before += total;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) a.starts[a.experts] = (int)before;
   for (int i = threadIdx.x; i < a.tokens * a.top_k; i += THREADS) {
     const int e = a.ids[i];
     if (e >= 0) a.places[i] += (int)chosen[e];
   }
 }
 
-// The plan of several chunks, for PLAN of them: thread (s, p) adds up the counts of experts 2 p and 2 p + 1 over every s-th chunk.
-// The CTA's own choices and counts are on their way meanwhile.
+// The plan of several chunks, for PLAN of them: thread (s, q) adds up the counts of experts 16 q ... 16 q + 15 (16 bytes) over
+// every s-th chunk, two to a word; the threads of a warp that share q add theirs up by exchange, the warps by atomics in shared
+// memory.  The CTA's own choices and counts are on their way meanwhile.
 __global__ void __launch_bounds__(PLAN_THREADS) dvm_routing_plan_kernel(const __grid_constant__ Args a) {
-  constexpr int EACH = 2;   // choices of a thread that are asked for early
+  constexpr int EACH = 2, DEEP = 16;   // choices of a thread that are asked for early; chunks asked for together
   __shared__ uint32_t before[DVM_MAX_EXPERTS], all[DVM_MAX_EXPERTS], own[PLAN][DVM_MAX_EXPERTS], sums[PLAN_THREADS / 32];
   for (int e = threadIdx.x; e < DVM_MAX_EXPERTS; e += PLAN_THREADS) before[e] = all[e] = 0u;
   grid_ready();
   grid_wait();
   __syncthreads();
-  const int pairs = (a.experts + 1) / 2, slices = PLAN_THREADS / pairs, p = threadIdx.x % pairs, s = threadIdx.x / pairs, mine = blockIdx.x * PLAN;
-  const long long chunk = (long long)a.rounds * ROUND * a.top_k, first = mine * chunk, last = min(first + PLAN * chunk, (long long)a.tokens * a.top_k);
+  // a.quads: 16s of experts, a.quads_up: the same rounded up to a power of two, 2 at least
+  const int quads = a.quads, slices = PLAN_THREADS / a.quads_up, q = threadIdx.x & (a.quads_up - 1), s = threadIdx.x / a.quads_up, mine = blockIdx.x * PLAN;
+  const int chunk = a.rounds * DVM_ROUTE_ROUND * a.top_k;
+  const long long first = (long long)mine * chunk;
+  const int choices = (int)min((long long)PLAN * chunk, (long long)a.tokens * a.top_k - first);
+  const int* const ids = a.ids + first;
+  int* const places = a.places + first;
   int id[EACH], place[EACH];
 #pragma unroll
   for (int x = 0; x < EACH; ++x) {
-    const long long i = first + threadIdx.x + x * PLAN_THREADS;
-    id[x] = i < last ? a.ids[i] : -1;
-    place[x] = i < last ? a.places[i] : 0;
+    const int i = threadIdx.x + x * PLAN_THREADS;
+    id[x] = i < choices ? ids[i] : -1;
+    place[x] = i < choices ? places[i] : 0;
   }
+  // thread e: the counts of expert e in the CTA's own chunks
   uint32_t mine_n[PLAN] = {};
-  if (s == 0)
+  if ((int)threadIdx.x < a.experts)
 #pragma unroll
-    for (int q = 0; q < PLAN; ++q)
-      if (mine + q < a.chunks) mine_n[q] = a.counts[(long long)(mine + q) * pairs + p];
-  if (s < slices) {
-    uint32_t b0 = 0, b1 = 0, n0 = 0, n1 = 0;
-#pragma unroll 16
-    for (int c = s; c < a.chunks; c += slices) {
-      const uint32_t v = a.counts[(long long)c * pairs + p];
-      n0 += v & 0xffffu;
-      n1 += v >> 16;
-      if (c < mine) { b0 += v & 0xffffu; b1 += v >> 16; }
+    for (int x = 0; x < PLAN; ++x)
+      if (mine + x < a.chunks) mine_n[x] = ((const uint8_t*)a.counts)[(long long)(mine + x) * (quads * 16) + threadIdx.x];
+  const uint4* const counts = (const uint4*)a.counts + q;
+  const int leader = (int)(threadIdx.x & ~31u) / a.quads_up;   // the first of the slices of this warp
+  const int many = slices * DEEP * (a.quads_up / 2);   // 32 / quads_up lanes x DEEP x quads_up / 2 chunks x 255 < 2^16
+  for (int c1 = s; c1 - s + leader < a.chunks; c1 += many) {   // (the lanes of a warp alike)
+    uint32_t n[8] = {}, b[8] = {};   // word w of the 16 bytes: bytes 0 and 2 in [2 w], 1 and 3 in [2 w + 1]
+    for (int c0 = c1; c0 - c1 < many && c0 - s + leader < a.chunks; c0 += slices * DEEP) {
+      uint4 v[DEEP];
+#pragma unroll
+      for (int x = 0; x < DEEP; ++x) v[x] = q < quads && c0 + x * slices < a.chunks ? counts[(long long)(c0 + x * slices) * quads] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int x = 0; x < DEEP; ++x) {
+        const uint32_t w[4] = {v[x].x, v[x].y, v[x].z, v[x].w}, earlier = c0 + x * slices < mine ? 0x00ff00ffu : 0u;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          n[2 * k] += w[k] & 0x00ff00ffu;
+          n[2 * k + 1] += (w[k] >> 8) & 0x00ff00ffu;
+          b[2 * k] += w[k] & earlier;
+          b[2 * k + 1] += (w[k] >> 8) & earlier;
+        }
+      }
     }
-    atomicAdd(&before[2 * p], b0);   // (whole numbers: any order gives the same)
-    atomicAdd(&before[2 * p + 1], b1);
-    atomicAdd(&all[2 * p], n0);
-    atomicAdd(&all[2 * p + 1], n1);
+    for (int d = a.quads_up; d < 32; d <<= 1) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        n[k] += __shfl_xor_sync(ALL, n[k], d);
+        b[k] += __shfl_xor_sync(ALL, b[k], d);
+      }
+    }
+    const int sharers = 32 / a.quads_up, turn = (threadIdx.x & 31) / a.quads_up;   // lanes of this warp with this q, and which of them this is
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const int shift = k & 2 ? 16 : 0, from = k / 4 * 2 + (k & 1);
+      if ((k & (sharers - 1)) == turn && q < quads) {   // (whole numbers: any order gives the same)
+        atomicAdd(&all[k * 32 + q], (n[from] >> shift) & 0xffffu);
+        atomicAdd(&before[k * 32 + q], (b[from] >> shift) & 0xffffu);
+      }
+    }
   }
   __syncthreads();
   uint32_t total;
-  const uint32_t start = block_scan<PLAN_THREADS / 32>((int)threadIdx.x < a.experts ? all[threadIdx.x] : 0u, sums, &total);
+  const int slot = (threadIdx.x & 15) * 32 + (threadIdx.x >> 4);   // of expert threadIdx.x
+  const uint32_t start = block_scan<PLAN_THREADS / 32>((int)threadIdx.x < a.experts ? all[slot] : 0u, sums, &total);
   if (blockIdx.x == 0) {
     if ((int)threadIdx.x < a.experts) a.starts[threadIdx.x] = (int)start;
     if (threadIdx.x == 0) a.starts[a.experts] = (int)total;
   }
-  before[threadIdx.x] += start;
-  __syncthreads();
-  if (s == 0) {
-    uint32_t at0 = before[2 * p], at1 = before[2 * p + 1];
+  uint32_t at = before[slot] + start;
 #pragma unroll
-    for (int q = 0; q < PLAN; ++q) {
-      own[q][2 * p] = at0;
-      own[q][2 * p + 1] = at1;
-      at0 += mine_n[q] & 0xffffu;
-      at1 += mine_n[q] >> 16;
-    }
+  for (int x = 0; x < PLAN; ++x) {
+    own[x][threadIdx.x] = at;
+    at += mine_n[x];
   }
   __syncthreads();
+  auto chunk_of = [&](int i) {
+    int x = 0;
+#pragma unroll
+    for (int k = 1; k < PLAN; ++k) x += i >= k * chunk;
+    return x;
+  };
 #pragma unroll
   for (int x = 0; x < EACH; ++x) {
-    const long long i = first + threadIdx.x + x * PLAN_THREADS;
-    if (id[x] >= 0) a.places[i] = place[x] + (int)own[(int)((i - first) / chunk)][id[x]];
+    const int i = threadIdx.x + x * PLAN_THREADS;
+    if (id[x] >= 0) places[i] = place[x] + (int)own[chunk_of(i)][id[x]];
   }
-  for (long long i = first + threadIdx.x + EACH * PLAN_THREADS; i < last; i += PLAN_THREADS) {
-    const int e = a.ids[i];
-    if (e >= 0) a.places[i] += (int)own[(int)((i - first) / chunk)][e];
+  for (int i = threadIdx.x + EACH * PLAN_THREADS; i < choices; i += PLAN_THREADS) {
+    const int e = ids[i];
+    if (e >= 0) places[i] += (int)own[chunk_of(i)][e];
   }
 }
-static_assert(PLAN_THREADS >= DVM_MAX_EXPERTS, "a thread per expert");
+static_assert(PLAN_THREADS == DVM_MAX_EXPERTS, "a thread per expert");
 
-template <int V> int launch(const Args& a, int device, cudaStream_t stream) {
+template <int V, bool SCORED, int WARPS> int launch(const Args& a, int device, cudaStream_t stream) {
   static std::atomic<uint64_t> allowed{0};
   constexpr int BYTES = WARPS * V * 33 * 4;
-  const int st = dvm_allow_smem((const void*)dvm_routing_kernel<V>, BYTES, device, &allowed);
-  return st != DVM_OK ? st : dvm_launch_next(dvm_routing_kernel<V>, a.chunks, THREADS, a.groups > 1 ? BYTES : 0, stream, a);
+  const int st = dvm_allow_smem((const void*)dvm_routing_kernel<V, SCORED, WARPS>, BYTES, device, &allowed);
+  return st != DVM_OK ? st : dvm_launch_next(dvm_routing_kernel<V, SCORED, WARPS>, a.chunks, WARPS * 32, a.groups > 1 ? BYTES : 0, stream, a);
+}
+template <int V> int launch(const Args& a, int device, cudaStream_t stream) {
+  const bool scored = a.bias || a.groups > 1;
+  if (a.chunks == 1) return scored ? launch<V, true, DVM_ROUTE_ONE>(a, device, stream) : launch<V, false, DVM_ROUTE_ONE>(a, device, stream);
+  return scored ? launch<V, true, DVM_ROUTE_ROUND>(a, device, stream) : launch<V, false, DVM_ROUTE_ROUND>(a, device, stream);
 }
 
 }  // namespace routing
@@ -516,6 +597,9 @@ int dvm_launch_routing(const dvm_routing_desc& d, void* const* t, cudaStream_t s
   a.chunks = (int)dvm_route_chunks(d); a.rounds = (int)dvm_route_rounds(d);
   a.bf16 = d.dtype == DVM_BF16; a.sigmoid = d.scoring == DVM_ROUTE_SIGMOID; a.renormalise = d.renormalise; a.factor = d.factor;
   a.lanes = 32;
+  a.quads = (a.experts + 15) / 16;
+  a.quads_up = 2;
+  while (a.quads_up < a.quads) a.quads_up <<= 1;
   while (a.lanes * a.groups > 32) a.lanes >>= 1;
   DvmDeviceInfo dev;
   int st = dvm_device_state(&dev);

@@ -101,7 +101,7 @@ int dvm_launch_experts(const uint32_t* w, void* const* tensors, int n_tensors, c
     dvm_descriptor(w, &d);
     const RoutingSlots s = dvm_slots(d);
     if (!aligned(s.logits, es(d.dtype)) || !aligned(s.bias, 4) || !aligned(s.positions, 4) || !aligned(s.ids, 4) || !aligned(s.weights, 4) || !aligned(s.places, 4) ||
-        !aligned(s.starts, 4) || !aligned(s.ws, 4))
+        !aligned(s.starts, 4) || !aligned(s.ws, 16))
       return DVM_ERR_INVALID_ARG;
     return dvm_launch_routing(d, tensors, stream);
   }

@@ -156,6 +156,22 @@ def test_routing_of_many_tokens():
     assert torch.equal(starts.long(), torch.searchsorted(by_expert, torch.arange(e + 1, device="cuda")))
 
 
+@pytest.mark.parametrize("t,e,k,alike", [(592 * 16, 33, 3, False), (592 * 16 + 1, 200, 2, True), (592 * 240, 8, 1, True), (592 * 240 + 1, 16, 2, True),
+                                         (1200001, 5, 2, True), (200000, 512, 1, False), (700003, 40, 2, True)])
+def test_routing_of_more_chunks(t, e, k, alike):
+    """More tokens than the chunks of one launch's size; with `alike` all of a chunk's tokens are at the same expert, the most that it counts."""
+    g = torch.Generator("cuda").manual_seed(t)
+    logits = torch.randn((1 if alike else t, e), generator=g, device="cuda").expand(t, e).contiguous()
+    ids, weights, places, starts = run_routing(logits, k)
+    ok()
+    assert torch.equal(ids.long(), logits.sort(dim=1, descending=True, stable=True)[1][:, :k])
+    by_expert, order = ids.reshape(-1).long().sort(stable=True)
+    rows = torch.empty_like(order)
+    rows[order] = torch.arange(t * k, device="cuda")
+    assert torch.equal(places.reshape(-1).long(), rows)
+    assert torch.equal(starts.long(), torch.searchsorted(by_expert, torch.arange(e + 1, device="cuda")))
+
+
 # ------------------------------------------------------------------------------------------------------ quantize
 
 def check_quantize(x, gated=False, copies=0, block_rows=1, pad=16, seed=0, some_outside=False):
