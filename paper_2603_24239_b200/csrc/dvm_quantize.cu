@@ -8,8 +8,11 @@
 // Quotients lie on the border between two codes often (bf16 values over their maximum are quotients of small numbers),
 // so a rounded quotient would decide by its rounding.  Each value is multiplied by a reciprocal a little too large and by one a
 // little too small: where both products have one code, it is the quotient's; where not, the sign of v - border * scale, one
-// exact multiply-add, decides.  8192 tokens of 4096 to 8 rows each: 65 us, 5.3 TB/s; 49157 rows of 1408 gated: 60 us, 5.8; weights of
-// 11008 x 4096 from fp32: 40 us, 5.6.
+// exact multiply-add, decides (the value is read again, in a loop: kept in registers and called for each of the 16, that cost
+// 4 us of the weights' 40).  A gated value is fp32 within a bound; its products take the bound in, and the largest of a block and
+// the values at a border are computed again to 2^-40: in fp32 alone 1 of 600000 codes was the neighbour of the right one.
+// 8192 tokens of 4096 to 8 rows each: 65 us, 5.3 TB/s; 49157 rows of 1408 gated: 73 us, 4.7 (the largest again 9 us, the second
+// product 4; bound by instructions and by their unit for exponentials and reciprocals); weights of 11008 x 4096 from fp32: 36 us, 6.2.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -61,6 +64,7 @@ template <int N> struct Raw<__nv_bfloat16, N> {
     for (int i = 0; i < N / 2; ++i) w[i] = 0u;
   }
   __device__ __forceinline__ float2 pair(int i) const { return make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)); }
+  __device__ __forceinline__ Raw<__nv_bfloat16, 2> raw_pair(int i) const { return {{w[i]}}; }
 };
 template <int N> struct Raw<float, N> {
   float w[N];
@@ -81,7 +85,10 @@ template <int N> struct Raw<float, N> {
     for (int i = 0; i < N; ++i) w[i] = 0.f;
   }
   __device__ __forceinline__ float2 pair(int i) const { return make_float2(w[2 * i], w[2 * i + 1]); }
+  __device__ __forceinline__ Raw<float, 2> raw_pair(int i) const { return {{w[2 * i], w[2 * i + 1]}}; }
 };
+__device__ __forceinline__ float wide(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float wide(float x) { return x; }
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -92,65 +99,99 @@ __device__ __forceinline__ float rcp(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// silu(z) u: z / (1 + 2^(-z log2 e)) u
-__device__ __forceinline__ float2 gated(float2 z, float2 u) {
+// silu(z) u: z / (1 + 2^(-z log2 e)) u; most: the largest 1 + 2^(-z log2 e).
+__device__ __forceinline__ float2 gated(float2 z, float2 u, float& most) {
   const float2 e = mul2(z, make_float2(-1.4426950408889634f, -1.4426950408889634f));
   const float2 d = add2(make_float2(ex2(e.x), ex2(e.y)), make_float2(1.f, 1.f));
+  asm("max.f32 %0, %0, %1, %2;" : "+f"(most) : "f"(d.x), "f"(d.y));
   return mul2(mul2(z, make_float2(rcp(d.x), rcp(d.y))), u);
+}
+// How far off the above is, relative to it, with the product of it and a rounded reciprocal of the scale: the exponent's rounding
+// and that of log2 e cost |z| (2^-24 + 2^-26.2) where the exponential counts (z < 0), the instructions and roundings 11 x 2^-24 at
+// most: 2^-19.6 while 1 + e < 2^12 (z > -8.4), less than 2^-16 up to where silu is 0 in fp32.
+__device__ __forceinline__ float off_by(float most) { return most < 0x1p12f ? 0x1.6ap-20f : 0x1p-16f; }
+// The same to 2^-40: 2^f by its series (the 11th term is below 2^-42), a reciprocal and a step of Newton's.
+__device__ __forceinline__ double gated_exactly(float z, float u) {
+  const double x = fminf(fmaxf(z, -200.f), 200.f), t = fma(x, -1.4426950408889634, 0x1.8p52), f = fma(x, -1.4426950408889634, 0x1.8p52 - t);
+  double p = 7.054911620801121e-09;
+  const double c[10] = {1.0178086009239696e-07, 1.3215486790144305e-06, 1.5252733804059838e-05, 0.00015403530393381606, 0.0013333558146428441,
+                        0.009618129107628477, 0.055504108664821576, 0.2402265069591007, 0.6931471805599453, 1.0};
+#pragma unroll
+  for (int i = 0; i < 10; ++i) p = fma(p, f, c[i]);
+  const double d = fma(p, __hiloint2double((__double2loint(t) + 1023) << 20, 0), 1.0), r = (double)rcp((float)d);
+  return (double)z * fma(fma(-d, r, 1.0), r, r) * (double)u;
 }
 __device__ __forceinline__ float max_abs(float m, float x) {  // NaN if either is
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(m), "f"(fabsf(x)));
+  return m;
+}
+__device__ __forceinline__ float max_abs(float m, float2 v) {  // (one instruction)
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(m), "f"(v.x), "f"(v.y));
   return m;
 }
 // The scale of a block of this largest magnitude.
 __device__ __forceinline__ float scale_of(float most) {
   return most < INFINITY ? fmaxf(__fdiv_rn(most, 448.f), 0x1p-126f) : __uint_as_float(0x7fc00000u);
 }
-// The code of v / s, which lies between two neighbouring codes' values: those of lo and hi (magnitudes).
-__device__ __noinline__ uint32_t decide(float v, float s, uint32_t lo, uint32_t hi) {
-  // the border is half way: 2^-10 times an odd number at least, 9 bits
+// The value half way between two neighbouring codes (magnitudes): 2^-10 times an odd number at least, 9 bits.
+__device__ __forceinline__ float border(uint32_t lo, uint32_t hi) {
   auto value = [](uint32_t c) { return c < 8 ? c * 0x1p-9f : __uint_as_float(((c >> 3) + 120u) << 23 | (c & 7u) << 20); };
-  const float edge = 0.5f * (value(lo) + value(hi));
+  return 0.5f * (value(lo) + value(hi));
+}
+// The sign of |v| / s - edge.
+__device__ __forceinline__ int side(float v, float s, float edge) {
   const float up = s < 0x1p-60f ? 0x1p64f : 1.f;   // (keeps the difference out of the subnormals)
   const float d = fmaf(-edge, s * up, fabsf(v) * up);
-  return d > 0.f ? hi : d < 0.f ? lo : lo & 1u ? hi : lo;
+  return (d > 0.f) - (d < 0.f);
 }
-// Codes of N values of a block with scale s, 4 to a word.  EXACT: borders are decided exactly.
-template <bool EXACT, int N> __device__ __forceinline__ void codes_of(const float2 (&v)[N / 2], float s, uint32_t (&c)[N / 4]) {
+__device__ __forceinline__ int side_gated(float z, float u, float s, float edge) {
+  const double d = fabs(gated_exactly(z, u)) - (double)edge * (double)s;
+  return (d > 0.) - (d < 0.);
+}
+// Codes of N values of a block with scale s, 4 to a word; off: how far from the quotients the products may be, relative to them;
+// side_of(i, edge): on which side of a border value i lies (it reads the value again: few come here, in one loop).
+template <int N, class Side> __device__ __forceinline__ void codes_of(const float2 (&v)[N / 2], float s, float off, uint32_t (&c)[N / 4], Side side_of) {
   if (s != s) {
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) c[i] = 0u;
     return;
   }
-  const float inv = __frcp_rn(s);
-  const float above = EXACT ? inv * (1.f + 0x1p-21f) : inv, below = inv * (1.f - 0x1p-21f);
+  const float inv = __frcp_rn(s), above = inv * (1.f + off), below = inv * (1.f - off);
   uint32_t low[N / 4], differ = 0u;
 #pragma unroll
   for (int i = 0; i < N / 4; ++i) {
     const float2 p = mul2(v[2 * i], make_float2(above, above)), q = mul2(v[2 * i + 1], make_float2(above, above));
     c[i] = pack_e4m3(p.x, p.y) | ((uint32_t)pack_e4m3(q.x, q.y) << 16);
-    if (EXACT) {
-      const float2 r = mul2(v[2 * i], make_float2(below, below)), t = mul2(v[2 * i + 1], make_float2(below, below));
-      low[i] = pack_e4m3(r.x, r.y) | ((uint32_t)pack_e4m3(t.x, t.y) << 16);
-      differ |= c[i] ^ low[i];
-    }
+    const float2 r = mul2(v[2 * i], make_float2(below, below)), t = mul2(v[2 * i + 1], make_float2(below, below));
+    low[i] = pack_e4m3(r.x, r.y) | ((uint32_t)pack_e4m3(t.x, t.y) << 16);
+    differ |= c[i] ^ low[i];
   }
-  if (EXACT && differ) {
+  if (differ) {
+#pragma unroll 1
+    for (int k = 0; k < N / 4; ++k) {
+      uint32_t high = c[0], other = low[0];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const uint32_t hi = (c[i >> 2] >> (8 * (i & 3))) & 0xffu, lo = (low[i >> 2] >> (8 * (i & 3))) & 0xffu;
-      if (hi != lo) {
-        const uint32_t is = decide(i & 1 ? v[i >> 1].y : v[i >> 1].x, s, lo & 0x7fu, hi & 0x7fu) | (hi & 0x80u);
-        c[i >> 2] = (c[i >> 2] & ~(0xffu << (8 * (i & 3)))) | is << (8 * (i & 3));
+      for (int x = 1; x < N / 4; ++x)
+        if (k == x) { high = c[x]; other = low[x]; }
+      uint32_t open = high ^ other;   // (0 in the bytes that are decided)
+      while (open) {
+        const int b = (__ffs(open) - 1) & 24;
+        const uint32_t hi = (high >> b) & 0x7fu, lo = (other >> b) & 0x7fu;
+        const int is = side_of(4 * k + (b >> 3), border(lo, hi));
+        if (is < 0 || (is == 0 && (hi & 1u))) high ^= (hi ^ lo) << b;
+        open &= ~(0xffu << b);
       }
+#pragma unroll
+      for (int x = 0; x < N / 4; ++x)
+        if (k == x) c[x] = high;
     }
   }
 }
 
-// Blocks of rows: L lanes to a block of 128 columns, AHEAD blocks at once (their loads are asked for together).  Of rows that are
-// spread one at a time: more of them are bound by registers (8192 tokens to 8 rows each 65 us, 67 with two, 72 with four).
-template <class T, bool GATED, bool VEC> __global__ void __launch_bounds__(THREADS) dvm_quantize_kernel(const __grid_constant__ Args a) {
-  constexpr int L = sizeof(T) == 2 ? 8 : 16, N = DVM_SCALE_BLOCK / L, AHEAD = GATED ? 2 : 1, GROUPS = THREADS / L;
+// Blocks of rows: L lanes to a block of 128 columns; four CTAs per SM, since what counts is loads on their way (8192 tokens to 8
+// rows each 65 us, 70 with as many registers as the compiler likes and two blocks of a row at once).
+template <class T, bool GATED, bool VEC> __global__ void __launch_bounds__(THREADS, 4) dvm_quantize_kernel(const __grid_constant__ Args a) {
+  constexpr int L = sizeof(T) == 2 ? 8 : 16, N = DVM_SCALE_BLOCK / L, GROUPS = THREADS / L;
   const int lane = threadIdx.x % L, group = threadIdx.x / L;
   const long long items = (long long)a.rows * a.blocks, step = (long long)gridDim.x * GROUPS;
   grid_ready();
@@ -159,66 +200,79 @@ template <class T, bool GATED, bool VEC> __global__ void __launch_bounds__(THREA
   const int step_rows = (int)(step / a.blocks), step_blocks = (int)(step - (long long)step_rows * a.blocks);
   long long item = (long long)blockIdx.x * GROUPS + group;
   int row = (int)(item / a.blocks), b = (int)(item - (long long)row * a.blocks);
-  for (long long of_warp = item - group % (32 / L); of_warp < items; of_warp += AHEAD * step) {   // (all lanes of a warp together)
-    int rows[AHEAD], bs[AHEAD];
-    Raw<T, N> x[AHEAD], up[GATED ? AHEAD : 1];
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      rows[k] = item < items ? row : -1;
-      bs[k] = b;
-      const int col = b * DVM_SCALE_BLOCK + N * lane;
-      if (rows[k] >= 0 && col < a.cols) {
-        const T* p = (const T*)a.x + row * a.xs + col;
-        x[k].template load<VEC>(p);
-        if (GATED) up[GATED ? k : 0].template load<VEC>(p + a.cols);
-      } else {
-        x[k].clear();
-        if (GATED) up[GATED ? k : 0].clear();
-      }
-      item += step;
-      row += step_rows;
-      b += step_blocks;
-      if (b >= a.blocks) { b -= a.blocks; ++row; }
+  for (; item - group % (32 / L) < items; item += step) {   // (all lanes of a warp together)
+    const int col = b * DVM_SCALE_BLOCK + N * lane;
+    const bool here = item < items, in = here && col < a.cols;
+    const T* const from = (const T*)a.x + row * a.xs + col;
+    Raw<T, N> x, up;
+    if (in) {
+      x.template load<VEC>(from);
+      if (GATED) up.template load<VEC>(from + a.cols);
+    } else {
+      x.clear();
+      if (GATED) up.clear();
     }
+    float2 v[N / 2];
+    float most = 0.f, worst = 0.f, s;
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      const int col = bs[k] * DVM_SCALE_BLOCK + N * lane;
-      float2 v[N / 2];
-      float most = 0.f;
+    for (int i = 0; i < N / 2; ++i) {
+      v[i] = GATED ? gated(x.pair(i), up.pair(i), worst) : x.pair(i);
+      most = max_abs(most, v[i]);
+    }
+    const float own = most;
 #pragma unroll
-      for (int i = 0; i < N / 2; ++i) {
-        v[i] = GATED ? gated(x[k].pair(i), up[GATED ? k : 0].pair(i)) : x[k].pair(i);
-        most = max_abs(max_abs(most, v[i].x), v[i].y);
+    for (int d = L / 2; d > 0; d >>= 1) most = max_abs(most, __shfl_xor_sync(ALL, most, d));
+    uint32_t c[N / 4];
+    if (GATED) {
+      // the lanes whose largest may be the block's compute it again, to more than fp32
+      s = 0.f;
+      if (own >= most * (1.f - 0x1p-15f)) {
+        Raw<T, 2> z = {}, u = {};
+        float first = 0.f;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i)
+          if (max_abs(0.f, v[i]) == own) {
+            z = x.raw_pair(i);
+            u = up.raw_pair(i);
+            first = v[i].x;
+          }
+        const float2 zs = z.pair(0), us = u.pair(0);
+        const bool x_is = fabsf(first) == own;
+        s = (float)(fabs(gated_exactly(x_is ? zs.x : zs.y, x_is ? us.x : us.y)) * (1. / 448.));
       }
 #pragma unroll
-      for (int d = L / 2; d > 0; d >>= 1) most = max_abs(most, __shfl_xor_sync(ALL, most, d));
-      const float s = scale_of(most);
-      uint32_t c[N / 4];
-      codes_of<!GATED, N>(v, s, c);
-      auto put = [&](uint8_t* p) {
-        if (N == 16) *(uint4*)p = make_uint4(c[0], c[1], c[N / 4 - 2], c[N / 4 - 1]);
-        else *(uint2*)p = make_uint2(c[0], c[1]);
-      };
-      const bool in = rows[k] >= 0 && col < a.cols;
-      if (!a.copies) {
-        if (in) put(a.codes + rows[k] * a.cs + col);
-        if (rows[k] >= 0 && lane == 0) a.scales[rows[k] * a.ss + bs[k]] = s;
-      } else {
-        for (int j0 = 0; j0 < a.copies; j0 += L) {
-          // lane l: place j0 + l, whose scale it stores
-          int place = -1;
-          if (rows[k] >= 0 && j0 + lane < a.copies) place = a.places[(long long)rows[k] * a.copies + j0 + lane];
-          if (place >= a.out_rows) place = -1;
-          if (place >= 0) a.scales[place * a.ss + bs[k]] = s;
-          // (the lanes' places beyond the last are -1)
+      for (int d = L / 2; d > 0; d >>= 1) s = fmaxf(s, __shfl_xor_sync(ALL, s, d));
+      s = most < INFINITY ? fmaxf(s, 0x1p-126f) : __uint_as_float(0x7fc00000u);
+      codes_of<N>(v, s, off_by(worst), c, [&](int i, float edge) { return side_gated(wide(from[i]), wide(from[a.cols + i]), s, edge); });
+    } else {
+      s = scale_of(most);
+      codes_of<N>(v, s, 0x1p-21f, c, [&](int i, float edge) { return side(wide(from[i]), s, edge); });
+    }
+    auto put = [&](uint8_t* p) {
+      if (N == 16) *(uint4*)p = make_uint4(c[0], c[1], c[N / 4 - 2], c[N / 4 - 1]);
+      else *(uint2*)p = make_uint2(c[0], c[1]);
+    };
+    if (!a.copies) {
+      if (in) put(a.codes + row * a.cs + col);
+      if (here && lane == 0) a.scales[row * a.ss + b] = s;
+    } else {
+      for (int j0 = 0; j0 < a.copies; j0 += L) {
+        // lane l: place j0 + l, whose scale it stores
+        int place = -1;
+        if (here && j0 + lane < a.copies) place = a.places[(long long)row * a.copies + j0 + lane];
+        if (place >= a.out_rows) place = -1;
+        if (place >= 0) a.scales[place * a.ss + b] = s;
+        // (the lanes' places beyond the last are -1)
 #pragma unroll
-          for (int j = 0; j < L; ++j) {
-            const int to = __shfl_sync(ALL, place, j, L);
-            if (to >= 0 && in) put(a.codes + to * a.cs + col);
-          }
+        for (int j = 0; j < L; ++j) {
+          const int to = __shfl_sync(ALL, place, j, L);
+          if (to >= 0 && in) put(a.codes + to * a.cs + col);
         }
       }
     }
+    row += step_rows;
+    b += step_blocks;
+    if (b >= a.blocks) { b -= a.blocks; ++row; }
   }
 }
 
@@ -244,7 +298,7 @@ template <class T, bool VEC> __global__ void __launch_bounds__(THREADS) dvm_quan
 #pragma unroll
   for (int i = 0; i < ROWS; ++i)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) m = max_abs(max_abs(m, v[i][k].x), v[i][k].y);
+    for (int k = 0; k < 4; ++k) m = max_abs(m, v[i][k]);
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) m = max_abs(m, __shfl_xor_sync(ALL, m, d));
   if ((threadIdx.x & 31) == 0) most[threadIdx.x >> 5] = m;
@@ -256,7 +310,8 @@ template <class T, bool VEC> __global__ void __launch_bounds__(THREADS) dvm_quan
   for (int i = 0; i < ROWS; ++i) {
     const int row = row0 + i * (THREADS / LANES);
     uint32_t c[2];
-    codes_of<true, 8>(v[i], s, c);
+    const T* const from = (const T*)a.x + row * a.xs + col;
+    codes_of<8>(v[i], s, 0x1p-21f, c, [&](int k, float edge) { return side(wide(from[k]), s, edge); });
     if (row < a.rows && col < a.cols) *(uint2*)(a.codes + row * a.cs + col) = make_uint2(c[0], c[1]);
   }
   if (threadIdx.x == 0) a.scales[rb * a.ss + b] = s;

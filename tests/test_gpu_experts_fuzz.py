@@ -46,6 +46,30 @@ def test_drawn_quantize(seed):
             check_quantize(x, gated, int(r.choice([0, 1, 2, 7])), pad=16 * int(r.integers(0, 3)), seed=seed, some_outside=bool(r.integers(2)))
 
 
+@pytest.mark.parametrize("dtype,std", [(BF16, 1.0), (F32, 1.0), (F32, 10.0), (BF16, 30.0), (F32, 1e-3)])
+def test_gated_codes_are_the_nearest(dtype, std):
+    """Codes against the quotients in 64 bits by the kernel's own scales, all of them; scales: of the largest, rounded once, but
+    where a value of less than 2^-15 below it stands in for it (which takes two such in 16 neighbours: one block in ten thousand)."""
+    rows, cols = 3000, 1408
+    x = normal((rows, 2 * cols), dtype, 11, std)
+    codes, scales = torch.zeros((rows, cols), dtype=torch.uint8, device="cuda"), torch.zeros((rows, cols // 128), device="cuda")
+    dvm.launch(dvm.encode_quantize(x, codes, scales, gated=True), [x, codes, scales])
+    ok()
+    z, u = x.double()[:, :cols], x.double()[:, cols:]
+    v = torch.where(z < -87, 0.0, z / (1 + (-z).exp())) * u
+    largest = (v.abs().view(rows, -1, 128).amax(2) / 448).clamp(min=2.0 ** -126)
+    assert bool(((scales.double() - largest).abs() <= largest * 2.0 ** -15).all())
+    assert float((scales != largest.float()).float().mean()) <= 1e-3
+    q = (v.view(rows, -1, 128) / scales.double()[..., None]).view(rows, cols)
+    table = torch.arange(127, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn).double()
+    m = q.abs().clamp(max=448.0)
+    hi = torch.searchsorted(table, m).clamp(1, 126)
+    up = m - table[hi - 1] - (table[hi] - m)
+    at = torch.where((up > 0) | ((up == 0) & (hi % 2 == 0)), hi, hi - 1)
+    assert torch.equal(codes & 0x7f, at.to(torch.uint8))
+    assert bool((((codes >> 7) == 1) == (q < 0))[at > 0].all())
+
+
 @pytest.mark.parametrize("seed", range(32))
 def test_drawn_scaled(seed):
     r = np.random.default_rng(200 + seed)
