@@ -8,12 +8,13 @@
 // Quotients lie on the border between two codes often (bf16 values over their maximum are quotients of small numbers),
 // so a rounded quotient would decide by its rounding.  Each value is multiplied by a reciprocal a little too large and by one a
 // little too small: where both products have one code, it is the quotient's; where not, the sign of v - border * scale, one
-// exact multiply-add, decides (the value is read again, in a loop: kept in registers and called for each of the 16, that cost
-// 4 us of the weights' 40).  A gated value is fp32 within a bound; its products take the bound in, and the largest of a block and
+// exact multiply-add, decides, in a loop over the few that want it (nearly every warp has one in bf16 rows), which reads the value
+// again: decided where each of the 16 stands, 8192 rows of 4096 without copies took 33 us, so 27.  A gated value is fp32 within a bound; its products take the bound in, and the largest of a block and
 // the values at a border are computed again to 2^-40: in fp32 alone 1 of 600000 codes was the neighbour of the right one.
-// 8192 tokens of 4096 to 8 rows each: 65 us, 5.3 TB/s; 49157 rows of 1408 gated: 73 us, 4.7 (the largest again 9 us, the second
+// 8192 tokens of 4096 to 8 rows each: 64 us, 5.4 TB/s; 49157 rows of 1408 gated: 73 us, 4.7 (the largest again 9 us, the second
 // product 4; bound by instructions and by their unit for exponentials and reciprocals); weights of 11008 x 4096 from fp32: 36 us, 6.2.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <math.h>
 
@@ -133,10 +134,12 @@ __device__ __forceinline__ float max_abs(float m, float2 v) {  // (one instructi
 __device__ __forceinline__ float scale_of(float most) {
   return most < INFINITY ? fmaxf(__fdiv_rn(most, 448.f), 0x1p-126f) : __uint_as_float(0x7fc00000u);
 }
-// The value half way between two neighbouring codes (magnitudes): 2^-10 times an odd number at least, 9 bits.
+// The magnitude half way between the values of two neighbouring codes: 2^-10 times an odd number at least, 9 bits.
 __device__ __forceinline__ float border(uint32_t lo, uint32_t hi) {
-  auto value = [](uint32_t c) { return c < 8 ? c * 0x1p-9f : __uint_as_float(((c >> 3) + 120u) << 23 | (c & 7u) << 20); };
-  return 0.5f * (value(lo) + value(hi));
+  uint32_t both;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(both) : "h"((uint16_t)(lo | hi << 8)));
+  const float2 f = __half22float2(*(const __half2*)&both);
+  return fabsf(0.5f * (f.x + f.y));
 }
 // The sign of |v| / s - edge.
 __device__ __forceinline__ int side(float v, float s, float edge) {
@@ -167,29 +170,32 @@ template <int N, class Side> __device__ __forceinline__ void codes_of(const floa
     differ |= c[i] ^ low[i];
   }
   if (differ) {
-#pragma unroll 1
+    uint32_t open = 0u;   // bit 8 b + 7 - k: byte b of word k differs
+#pragma unroll
     for (int k = 0; k < N / 4; ++k) {
+      const uint32_t x = c[k] ^ low[k];
+      open |= ((((x & 0x7f7f7f7fu) + 0x7f7f7f7fu) | x) & 0x80808080u) >> k;
+    }
+#pragma unroll 1
+    do {
+      const int bit = __ffs(open) - 1, k = 7 - (bit & 7), b = bit & 24;
+      open &= open - 1u;
       uint32_t high = c[0], other = low[0];
 #pragma unroll
       for (int x = 1; x < N / 4; ++x)
         if (k == x) { high = c[x]; other = low[x]; }
-      uint32_t open = high ^ other;   // (0 in the bytes that are decided)
-      while (open) {
-        const int b = (__ffs(open) - 1) & 24;
-        const uint32_t hi = (high >> b) & 0x7fu, lo = (other >> b) & 0x7fu;
-        const int is = side_of(4 * k + (b >> 3), border(lo, hi));
-        if (is < 0 || (is == 0 && (hi & 1u))) high ^= (hi ^ lo) << b;
-        open &= ~(0xffu << b);
-      }
+      const uint32_t hi = (high >> b) & 0xffu, lo = (other >> b) & 0xffu;
+      const int is = side_of(4 * k + (b >> 3), border(lo, hi));
+      const uint32_t flip = is < 0 || (is == 0 && (hi & 1u)) ? (hi ^ lo) << b : 0u;
 #pragma unroll
       for (int x = 0; x < N / 4; ++x)
-        if (k == x) c[x] = high;
-    }
+        if (k == x) c[x] ^= flip;
+    } while (open);
   }
 }
 
 // Blocks of rows: L lanes to a block of 128 columns; four CTAs per SM, since what counts is loads on their way (8192 tokens to 8
-// rows each 65 us, 70 with as many registers as the compiler likes and two blocks of a row at once).
+// rows each 64 us, 70 with as many registers as the compiler likes and two blocks of a row at once).
 template <class T, bool GATED, bool VEC> __global__ void __launch_bounds__(THREADS, 4) dvm_quantize_kernel(const __grid_constant__ Args a) {
   constexpr int L = sizeof(T) == 2 ? 8 : 16, N = DVM_SCALE_BLOCK / L, GROUPS = THREADS / L;
   const int lane = threadIdx.x % L, group = threadIdx.x / L;
