@@ -50,7 +50,7 @@ extern "C" {
  *   ids[t, 0 .. top_k)    the experts of the largest c among those, largest first, of equal ones the lowest index
  *   weights[t, j]         s of expert ids[t, j]; with `renormalise` divided by the sum over j; times `factor`
  * The order is that of exact values: where 32 bits cannot tell two apart, they are computed in 64.  A NaN counts less than
- * anything else (a NaN logit under softmax makes the token's weights NaN).
+ * anything else (a NaN or +inf logit under softmax makes the token's weights NaN).
  * The plan, over all (t, j):
  *   starts[e]     first row of expert e: rows starts[e] <= r < starts[e + 1] are its tokens, in their order;
  *                 starts[experts] rows are in use

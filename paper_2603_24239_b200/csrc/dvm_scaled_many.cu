@@ -9,7 +9,7 @@
 // thread r holds row r and 128 of the columns, in registers -- and add them up with the row's scale times the weight's: 128
 // multiply-adds a thread to a block, two to an instruction, 290 cycles of an SM, 500 with the loads from tensor memory.  Two
 // warps copy the scales of four blocks at a time into shared memory, ahead of all that.  At a tile's end rows leave by TMA from
-// shared memory, beside the next tile's sums; rows of a warp that are not all the group's are stored one by one.
+// shared memory, beside the next tile's sums; of a warp whose rows are not all the group's each thread stores its own.
 // A place in tensor memory is taken for the products (512 cycles), their end's arrival (190), the loads and sums (500) and the
 // way back (200), and there are two: 950 to 1000 cycles a block are what it takes.  8192 rows, 4096 to 11008: 360 us in bursts,
 // 2.05 PFLOP/s (1.7 GHz), 407 in calls in a row at the power cap (1.42 GHz).
@@ -290,17 +290,31 @@ dvm_scaled_many_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_co
           __syncwarp();
           if (lane == 0) tma_store_2d(&tm_out, box + (c & 1) * S::OUT_BOX, c0 + c * PER_LINE, tile.first + quarter * 32);
         }
-      } else if (row < tile.rows) {
-        T* const out = (T*)a.out + (long long)(tile.first + row) * a.out_stride + c0;
-        if (a.out_tma && cols == HALF) {
+      } else if (a.out_tma && cols == HALF) {
+        if (row < tile.rows) {
+          T* const out = (T*)a.out + (long long)(tile.first + row) * a.out_stride + c0;
 #pragma unroll
           for (int i = 0; i < HALF / PIECE; ++i) *(uint4*)(out + i * PIECE) = Out<T>::pack(acc + i * (PIECE / 2));
-        } else {
+        }
+      } else if (cols > 0 && quarter * 32 < tile.rows) {
+        // results that no copy out takes: the same lines through shared memory, so that a store has neighbours of one row
+        const int rows = min(32, tile.rows - quarter * 32);
+        uint8_t* const boxes = sm + S::OUT + (warp - 4) * 2 * S::OUT_BOX;
+        T* const out = (T*)a.out + (long long)(tile.first + quarter * 32) * a.out_stride + c0;
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
 #pragma unroll
-          for (int i = 0; i < 64; ++i) {
-            if (2 * i < cols) out[2 * i] = (T)acc[i].x;
-            if (2 * i + 1 < cols) out[2 * i + 1] = (T)acc[i].y;
-          }
+        for (int c = 0; c < HALF / PER_LINE; ++c) {
+          uint8_t* const box = boxes + (c & 1) * S::OUT_BOX;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) *(uint4*)(box + lane * 128 + ((i ^ (lane & 7)) << 4)) = Out<T>::pack(acc + (8 * c + i) * (PIECE / 2));
+          __syncwarp();
+          for (int r = 0; r < rows; ++r)
+#pragma unroll
+            for (int e = lane; e < PER_LINE; e += 32)
+              if (c * PER_LINE + e < cols)
+                out[r * a.out_stride + c * PER_LINE + e] = *(const T*)(box + r * 128 + (((e / PIECE) ^ (r & 7)) << 4) + e % PIECE * sizeof(T));
+          __syncwarp();
         }
       }
     }
