@@ -12,12 +12,14 @@
 // choices are a bit per token in a word per expert: a token's rank at its expert is the number of bits below its own, plus what
 // earlier rounds of the chunk counted.  Up to 32 tokens are one round of one CTA, which does it all; else every CTA leaves its
 // chunk's counts in the workspace, a byte each, and a second launch adds up those of the chunks before.
-// 8191 tokens of 256 experts in 8 groups with a bias: 32 us (19 without both), 64 tokens 9.7, one token 3.9.  Bound by
+// 8191 tokens of 256 experts in 8 groups with a bias: 29 us (19 without both), 64 tokens 9.8, one token 3.9.  Bound by
 // instructions: 2.1 us would read the logits, but a token costs 870 instructions without groups or bias (a load, a score, a sort of
 // 8 keys and 8 rounds of two reductions) and 1530 with both, 13 and 20 us of the first launch.  A warp per token was taken over a
-// CTA per token (whose barriers made 8191 tokens 96 us) and over a thread per token (64 tokens leave the GPU empty).  The second
-// launch, 8 us, reads every chunk's counts per 4 chunks; 16 bytes to a load and additions of two counts to an instruction took it
-// there from 20.
+// CTA per token (whose barriers made 8191 tokens 96 us) and over a thread per token (64 tokens leave the GPU empty).  One token in
+// a CTA that goes to 64 bits keeps the others waiting: with all of it done again there, groups included, 8191 tokens took 29 to 36
+// us by what they held, now 27 to 31 (25.7 if none did).  Sorting by merges of odd and even places (38 instructions for 56) made
+// no difference for 8 keys and lost registers for 16.  The second launch, 8 us, reads every chunk's counts per 4 chunks; 16 bytes
+// to a load and additions of two counts to an instruction took it there from 20.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -69,16 +71,18 @@ template <class T> __device__ __forceinline__ T warp_sum(T v) {
 }
 
 // How near two values c are when 32 bits may have swapped them: twice what each may be off, in units of 2^-24.  A sigmoid: the
-// exponential's error, 2 ulp and 1.2 per unit of its argument, times s (1 - s), a sum and a reciprocal (1 ulp): less than 10.  Of a
-// softmax every score is at most 1 / sum; exponentials (at most 5), up to 16 + 5 additions and the quotient are less than 36
-// of that.  The bias adds a rounding of c itself.
-__device__ __forceinline__ float doubt(float unit, float c) { return 0x1p-23f * (unit + 2.f * fabsf(c)); }
+// exponential's error, 4 (2 ulp) and 1.25 |x| of it (its argument and log2 e are rounded), times s (1 - s): at most 1.05; the sum
+// before the reciprocal 1; the reciprocal 2 (1 ulp): less than 4.2.  Of a softmax every score is at most 1 / sum; exponentials (at most
+// 5), up to 16 + 5 additions and the quotient are less than 36 of that.  The bias adds a rounding of c itself.
+constexpr float SIGMOID_UNIT = 4.2f, SOFTMAX_UNIT = 36.f;
+// Of two sums of two values, at most most in magnitudes: four values and both sums' roundings.
+__device__ __forceinline__ float doubt_of_sums(float unit, float most) { return 0x1p-23f * 2.f * (unit + most); }
 // ... and of two keys without their lowest bits, which are less than V units in the last place (of at most 2^-23 of the value).
 // Values by logits are not rounded (unit 0).
 template <int V> __device__ __forceinline__ bool near_keys(uint32_t more, uint32_t less, float unit) {
   if (less < 2 * NAN_KEY) return false;   // (NaN, or nothing)
   const float x = of_key(more & ~(uint32_t)(V - 1)), y = of_key(less & ~(uint32_t)(V - 1));
-  return x - y <= fmaxf(fabsf(x), fabsf(y)) * (V * 0x1p-22f) + 0x1p-23f * unit;   // (infinite minus infinite: not near, the index decides)
+  return x - y <= fmaxf(fabsf(x), fabsf(y)) * ((V + 1) * 0x1p-23f) + 0x1p-23f * unit;   // (infinite minus infinite: not near, the index decides)
 }
 __device__ __forceinline__ float exp_near(float x) {
   float y;
@@ -106,12 +110,12 @@ template <class T> __device__ __forceinline__ void merge2(T& first, T& second, T
   else second = second > of ? second : of;
 }
 
-// The token again in 64 bits; returns lane j's choice.
-template <int V> __device__ __noinline__ int choose_exactly(const Args& a, long long t) {
-  const int lane = threadIdx.x & 31, per = a.experts / a.groups;
-  double v[V], sum = 0.0, top = -INFINITY;
+// c of this lane's experts in 64 bits.
+template <int V> __device__ __noinline__ void scores_exactly(const Args& a, long long t, double* v) {
+  const int lane = threadIdx.x & 31;
+  double sum = 0.0, top = -INFINITY;
   bool nan = false;
-#pragma unroll
+#pragma unroll 1
   for (int i = 0; i < V; ++i) {
     const int e = 32 * i + lane;
     v[i] = e < a.experts ? (double)logit_at(a, t, e) : -INFINITY;
@@ -123,18 +127,54 @@ template <int V> __device__ __noinline__ int choose_exactly(const Args& a, long 
     for (int d = 16; d > 0; d >>= 1) top = fmax(top, __shfl_xor_sync(ALL, top, d));
     if (__any_sync(ALL, nan)) top = NAN;
   }
-#pragma unroll
+#pragma unroll 1
   for (int i = 0; i < V; ++i) {
-    v[i] = a.sigmoid ? 1.0 / (1.0 + exp(-v[i])) : exp(v[i] - top);
+    v[i] = exp(a.sigmoid ? -v[i] : v[i] - top);
+    if (a.sigmoid) v[i] = 1.0 / (1.0 + v[i]);
     if (32 * i + lane < a.experts) sum += v[i];
   }
   if (!a.sigmoid) sum = warp_sum(sum);
-#pragma unroll
+#pragma unroll 1
   for (int i = 0; i < V; ++i) {
     const int e = 32 * i + lane;
     if (!a.sigmoid) v[i] /= sum;
     if (a.bias && e < a.experts) v[i] += (double)a.bias[e];
   }
+}
+// Of the groups `open`, the `places` that count most, by their sums in 64 bits (which are numbers).
+template <int V> __device__ __noinline__ uint32_t groups_exactly(const Args& a, long long t, uint32_t open, int places) {
+  const int lane = threadIdx.x & 31, per = a.experts / a.groups;
+  double v[V], mine = 0.0;   // mine: of group `lane`
+  int group[V];
+  scores_exactly<V>(a, t, v);
+  groups_of<V>(a, group);
+  for (uint32_t m = open; m; m &= m - 1u) {
+    const int g = __ffs(m) - 1;
+    double first = -INFINITY, second = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (group[i] == g) merge2(first, second, v[i], (double)-INFINITY);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+      const double of = __shfl_xor_sync(ALL, first, d), os = __shfl_xor_sync(ALL, second, d);
+      merge2(first, second, of, os);
+    }
+    if (lane == g) mine = per > 1 ? first + second : first;
+  }
+  int before = 0;
+  for (uint32_t m = open; m; m &= m - 1u) {
+    const int g = __ffs(m) - 1;
+    const double other = __shfl_sync(ALL, mine, g);
+    before += g != lane && (other > mine || (other == mine && g < lane));
+  }
+  return __ballot_sync(ALL, ((open >> lane) & 1u) && before < places);
+}
+
+// The token again in 64 bits; returns lane j's choice.
+template <int V> __device__ __noinline__ int choose_exactly(const Args& a, long long t) {
+  const int lane = threadIdx.x & 31, per = a.experts / a.groups;
+  double v[V];
+  scores_exactly<V>(a, t, v);
   uint32_t stay = ALL;
   int group[V];
   groups_of<V>(a, group);
@@ -270,7 +310,7 @@ template <int V, bool SCORED> __device__ __forceinline__ int choose(const Args& 
     sum = warp_sum(sum);
   }
   bool unsure = false;
-  const float unit = a.sigmoid ? 10.f : 36.f / sum;
+  const float unit = a.sigmoid ? SIGMOID_UNIT : SOFTMAX_UNIT / sum;
   if (SCORED) {
     const float inv_sum = rcp_near(sum);
     float c[V];
@@ -314,6 +354,7 @@ template <int V, bool SCORED> __device__ __forceinline__ int choose(const Args& 
         second = fmaxf(fmaxf(second, os), fminf(first, of));
         first = fmaxf(first, of);
       }
+      const float size = per > 1 ? fabsf(first) + fabsf(second) : fabsf(first);
       // (every lane of a group has its key; lanes of no group the lowest)
       const uint32_t mine = g < a.groups ? (bad ? NAN_KEY : key_of(per > 1 ? first + second : first)) : 0u;
       int before = 0;
@@ -321,16 +362,27 @@ template <int V, bool SCORED> __device__ __forceinline__ int choose(const Args& 
         const uint32_t other = __shfl_sync(ALL, mine, o * a.lanes);
         before += other > mine || (other == mine && o < g);
       }
-      const bool in = g < a.groups && before < a.top_groups;
-      const uint32_t stay = __ballot_sync(ALL, in);
+      bool in = g < a.groups && before < a.top_groups;
       if (a.top_groups < a.groups) {
         const uint32_t least = __reduce_min_sync(ALL, in ? mine : ALL), most = __reduce_max_sync(ALL, in ? 0u : mine);
-        if (most > NAN_KEY) {
-          const float x = of_key(least), y = of_key(most);
-          // (a sum of two values: both may be off, and their sum is rounded)
-          unsure = x - y <= 2.f * doubt(unit, fmaxf(fabsf(x), fabsf(y)));
+        const float sizes = __uint_as_float(__reduce_max_sync(ALL, __float_as_uint(g < a.groups && !bad && size < INFINITY ? size : 0.f)));
+        const float x = of_key(least), y = of_key(most), far = doubt_of_sums(unit, sizes);
+        if (most > NAN_KEY && x - y <= far) {
+          // those that may lie on either side of the border
+          const float sum = of_key(mine);
+          const bool may = g < a.groups && mine > NAN_KEY && sum - y <= far && x - sum <= far;
+          uint32_t open = 0u;
+          int sure = 0;
+          for (int o = 0; o < a.groups; ++o) {
+            const bool o_may = __shfl_sync(ALL, (int)may, o * a.lanes) != 0, o_in = __shfl_sync(ALL, (int)in, o * a.lanes) != 0;
+            open |= (uint32_t)o_may << o;
+            sure += o_in && !o_may;
+          }
+          open = groups_exactly<V>(a, t, open, a.top_groups - sure);
+          if (may) in = (open >> g) & 1u;
         }
       }
+      const uint32_t stay = __ballot_sync(ALL, in);
       const float inv = (float)a.groups / (float)a.experts;   // (e + 1/2 is half an expert away from any border, e < 512)
 #pragma unroll
       for (int i = 0; i < V; ++i)

@@ -32,6 +32,31 @@ def test_drawn_routing(seed):
         check_routing(logits, k, str(r.choice(["softmax", "sigmoid"])), bias, groups, top_groups, bool(r.integers(2)), float(r.choice([1.0, 0.1, 16.0])), positions)
 
 
+@pytest.mark.parametrize("scoring", ["sigmoid", "softmax"])
+def test_groups_whose_sums_32_bits_cannot_tell_apart(scoring):
+    """Biases that cancel in a group's sum, equal groups, groups a step of fp32 apart, experts and whole groups that are switched off."""
+    e, groups, per = 64, 8, 8
+    g = torch.Generator("cuda").manual_seed(3)
+    logits = torch.randn((400, e), generator=g, device="cuda") * 0.01
+    bias = torch.zeros(e, device="cuda")
+    bias[0::per], bias[1::per], bias[2::per] = 50.0, -49.99, -49.98   # sums near 0 of values near 50, rounded to 2^-18
+    for i in range(3, per):
+        bias[i::per] = -60.0
+    for top_groups in (1, 4, 7):
+        check_routing(logits, 4, scoring, bias, groups, top_groups)
+    same = logits.view(400, groups, per)[:, :1].expand(400, groups, per).reshape(400, e).contiguous()
+    for top_groups in (1, 3, 7):
+        check_routing(same, 5, scoring, None, groups, top_groups)   # equal groups: the first ones
+        check_routing(same, 5, scoring, torch.zeros(e, device="cuda"), groups, top_groups)
+    step = same.view(torch.int32) + torch.randint(-1, 2, same.shape, generator=g, device="cuda", dtype=torch.int32)
+    check_routing(step.view(torch.float32), 6, scoring, None, groups, 4, True, 2.0)
+    off = torch.zeros(e, device="cuda")
+    off[8:16], off[17], off[33:40] = -float("inf"), -float("inf"), -float("inf")   # a group, one expert, all but one of a group
+    off[48] = float("inf")
+    check_routing(step.view(torch.float32), 6, scoring, off, groups, 3)
+    check_routing(logits, 6, scoring, off, groups, 7)
+
+
 @pytest.mark.parametrize("seed", range(16))
 def test_drawn_quantize(seed):
     r = np.random.default_rng(100 + seed)
