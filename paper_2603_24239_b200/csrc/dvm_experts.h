@@ -29,9 +29,9 @@ int dvm_launch_experts(const uint32_t* w, void* const* tensors, int n_tensors, c
 
 inline int64_t dvm_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Routing: tokens are taken in rounds, a warp to each, by chunks of whole rounds; a chunk is one CTA.  Up to DVM_ROUTE_ONE tokens
-// are one round; more go in rounds of DVM_ROUTE_ROUND, and a chunk has at most 15 of these: its counts are bytes.
-#define DVM_ROUTE_ONE 32
+// Routing: up to DVM_ROUTE_ONE tokens are one launch of a cluster.  More are taken in rounds of DVM_ROUTE_ROUND, a warp to each, by
+// chunks of whole rounds; a chunk is one CTA and has at most 15 of these: its counts are bytes.
+#define DVM_ROUTE_ONE 128
 #define DVM_ROUTE_ROUND 16
 #define DVM_ROUTE_CHUNKS 592
 inline int64_t dvm_route_rounds(const dvm_routing_desc& d) {  // rounds of one chunk

@@ -10,9 +10,10 @@
 //
 // The plan is a counting sort without atomics whose order could change it.  Tokens go in rounds, a warp to each, and a round's
 // choices are a bit per token in a word per expert: a token's rank at its expert is the number of bits below its own, plus what
-// earlier rounds of the chunk counted.  Up to 32 tokens are one round of one CTA, which does it all; else every CTA leaves its
-// chunk's counts in the workspace, a byte each, and a second launch adds up those of the chunks before.
-// 8191 tokens of 256 experts in 8 groups with a bias: 29 us (19 without both), 64 tokens 9.8, one token 3.9.  Bound by
+// earlier rounds of the chunk counted.  Up to 128 tokens are dealt to the 8 CTAs of a cluster, which read one another's counts;
+// else every CTA leaves its chunk's counts in the workspace, a byte each, and a second launch adds up those of the chunks before.
+// 8191 tokens of 256 experts in 8 groups with a bias: 29 us (19 without both), 64 tokens 6.1 (4.2), one token of 64
+// experts 3.4 in a chain of launches (two launches of CTAs of 16 tokens took 9.8 for 64; one CTA of 32 took 6.6 for 32, 5.8 now).  Bound by
 // instructions: 2.1 us would read the logits, but a token costs 870 instructions without groups or bias (a load, a score, a sort of
 // 8 keys and 8 rounds of two reductions) and 1530 with both, 13 and 20 us of the first launch.  A warp per token was taken over a
 // CTA per token (whose barriers made 8191 tokens 96 us) and over a thread per token (64 tokens leave the GPU empty).  One token in
@@ -30,6 +31,7 @@ namespace dvm {
 namespace routing {
 
 constexpr int PLAN = 4, PLAN_THREADS = 512;   // of the second launch: chunks of a CTA
+constexpr int JOINT = 8, JOINT_WARPS = DVM_ROUTE_ONE / JOINT;   // of the one launch for few tokens: CTAs of a cluster, warps of each
 constexpr uint32_t ALL = 0xffffffffu;
 
 struct Args {
@@ -458,9 +460,10 @@ template <int WARPS> __device__ __forceinline__ uint32_t block_scan(uint32_t cou
   return before + upto - count;
 }
 
-template <int V, bool SCORED, int WARPS> __global__ void __launch_bounds__(WARPS * 32, 32 / WARPS) dvm_routing_kernel(const __grid_constant__ Args a) {
-  constexpr int THREADS = WARPS * 32;
-  __shared__ uint32_t chosen[DVM_MAX_EXPERTS], carry[DVM_MAX_EXPERTS], sums[WARPS];
+// A chunk of many tokens; its counts go to the second launch.
+template <int V, bool SCORED> __global__ void __launch_bounds__(DVM_ROUTE_ROUND * 32, 2) dvm_routing_kernel(const __grid_constant__ Args a) {
+  constexpr int WARPS = DVM_ROUTE_ROUND, THREADS = WARPS * 32;
+  __shared__ uint32_t chosen[DVM_MAX_EXPERTS], carry[DVM_MAX_EXPERTS];
   __shared__ float bias[DVM_MAX_EXPERTS];
   extern __shared__ float rows[];   // V * 33 to a warp, where there are groups
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -493,31 +496,65 @@ template <int V, bool SCORED, int WARPS> __global__ void __launch_bounds__(WARPS
     }
     __syncthreads();
   }
-  if (a.chunks > 1) {   // (the counts of experts behind the last are 0)
-    const int words = (a.experts + 15) / 16 * 4;
-    for (int q = threadIdx.x; q < words; q += THREADS)
-      a.counts[(long long)blockIdx.x * words + q] = carry[4 * q] | (carry[4 * q + 1] << 8) | (carry[4 * q + 2] << 16) | (carry[4 * q + 3] << 24);
-    return;
-  }
-  // one CTA: the starts, thread e expert e (up to 32 experts more to a warp than it has threads: a loop over the lanes' carries)
-  uint32_t before = 0u;
-  for (int e0 = 0; e0 < a.experts; e0 += THREADS) {
-    const int e = e0 + (int)threadIdx.x;
-    uint32_t total;
-    const uint32_t start = before + block_scan<WARPS>(e < a.experts ? carry[e] : 0u, sums, &total);
-    if (e < a.experts) {
-      a.starts[e] = (int)start;
-      chosen[e] = start;
-    }
-    before += total;
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) a.starts[a.experts] = (int)before;
-  for (int i = threadIdx.x; i < a.tokens * a.top_k; i += THREADS) {
-    const int e = a.ids[i];
-    if (e >= 0) a.places[i] += (int)chosen[e];
-  }
+  const int words = (a.experts + 15) / 16 * 4;   // (the counts of experts behind the last are 0)
+  for (int q = threadIdx.x; q < words; q += THREADS)
+    a.counts[(long long)blockIdx.x * words + q] = carry[4 * q] | (carry[4 * q + 1] << 8) | (carry[4 * q + 2] << 16) | (carry[4 * q + 3] << 24);
 }
+
+// Few tokens, in one launch: the CTAs of a cluster share them, a warp to each, and read one another's counts.
+template <int V, bool SCORED> __global__ void __cluster_dims__(JOINT) __launch_bounds__(JOINT_WARPS * 32, 1) dvm_routing_joint_kernel(const __grid_constant__ Args a) {
+  constexpr int THREADS = JOINT_WARPS * 32;
+  __shared__ uint32_t chosen[DVM_MAX_EXPERTS], counts[DVM_MAX_EXPERTS], sums[JOINT_WARPS];
+  __shared__ float bias[DVM_MAX_EXPERTS];
+  extern __shared__ float rows[];   // V * 33 to a warp, where there are groups
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, e = threadIdx.x;
+  uint32_t rank;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  chosen[e] = 0u;
+  grid_ready();
+  grid_wait();
+  if (SCORED && a.bias && e < a.experts) bias[e] = a.bias[e];
+  __syncthreads();
+  const int per = (a.tokens + JOINT - 1) / JOINT, t = (int)rank * per + warp;
+  const bool here = warp < per && t < a.tokens;
+  int mine = -1;
+  if (here) {
+    float l[V], weight = 0.f;
+    load_logits<V>(a, t, l);
+    if (!a.positions || a.positions[t] >= 0) mine = choose<V, SCORED>(a, t, l, bias, rows + warp * (V * 33), &weight);
+    if (mine >= 0) atomicOr(&chosen[mine], 1u << warp);
+    if (lane < a.top_k) {
+      a.ids[t * a.top_k + lane] = mine;
+      a.weights[t * a.top_k + lane] = weight;
+    }
+  }
+  __syncthreads();
+  const uint32_t place = mine >= 0 ? __popc(chosen[mine] & ((1u << warp) - 1u)) : 0u;
+  counts[e] = __popc(chosen[e]);
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  uint32_t of_all = 0u, before = 0u;
+  const uint32_t at = (uint32_t)__cvta_generic_to_shared(&counts[e]);
+#pragma unroll
+  for (uint32_t c = 0; c < JOINT; ++c) {
+    uint32_t there, n;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(c));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(n) : "r"(there) : "memory");
+    of_all += n;
+    before += c < rank ? n : 0u;
+  }
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // (no CTA goes before its counts have been read)
+  uint32_t total;
+  const uint32_t start = block_scan<JOINT_WARPS>(e < a.experts ? of_all : 0u, sums, &total);
+  if (rank == 0) {
+    if (e < a.experts) a.starts[e] = (int)start;
+    if (e == 0) a.starts[a.experts] = (int)total;
+  }
+  chosen[e] = start + before;
+  __syncthreads();
+  if (here && lane < a.top_k) a.places[t * a.top_k + lane] = mine < 0 ? -1 : (int)(chosen[mine] + place);
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+static_assert(JOINT_WARPS * 32 == DVM_MAX_EXPERTS, "a thread per expert");
 
 // The plan of several chunks, for PLAN of them: thread (s, q) adds up the counts of experts 16 q ... 16 q + 15 (16 bytes) over
 // every s-th chunk, two to a word; the threads of a warp that share q add theirs up by exchange, the warps by atomics in shared
@@ -620,16 +657,19 @@ __global__ void __launch_bounds__(PLAN_THREADS) dvm_routing_plan_kernel(const __
 }
 static_assert(PLAN_THREADS == DVM_MAX_EXPERTS, "a thread per expert");
 
-template <int V, bool SCORED, int WARPS> int launch(const Args& a, int device, cudaStream_t stream) {
-  static std::atomic<uint64_t> allowed{0};
-  constexpr int BYTES = WARPS * V * 33 * 4;
-  const int st = dvm_allow_smem((const void*)dvm_routing_kernel<V, SCORED, WARPS>, BYTES, device, &allowed);
-  return st != DVM_OK ? st : dvm_launch_next(dvm_routing_kernel<V, SCORED, WARPS>, a.chunks, WARPS * 32, a.groups > 1 ? BYTES : 0, stream, a);
+template <int V, bool SCORED> int launch(const Args& a, int device, cudaStream_t stream) {
+  static std::atomic<uint64_t> allowed{0}, allowed_joint{0};
+  const bool few = a.tokens <= DVM_ROUTE_ONE;
+  const int bytes = (few ? JOINT_WARPS : DVM_ROUTE_ROUND) * V * 33 * 4, smem = a.groups > 1 ? bytes : 0;
+  if (few) {
+    const int st = dvm_allow_smem((const void*)dvm_routing_joint_kernel<V, SCORED>, bytes, device, &allowed_joint);
+    return st != DVM_OK ? st : dvm_launch_next(dvm_routing_joint_kernel<V, SCORED>, JOINT, JOINT_WARPS * 32, smem, stream, a);
+  }
+  const int st = dvm_allow_smem((const void*)dvm_routing_kernel<V, SCORED>, bytes, device, &allowed);
+  return st != DVM_OK ? st : dvm_launch_next(dvm_routing_kernel<V, SCORED>, a.chunks, DVM_ROUTE_ROUND * 32, smem, stream, a);
 }
 template <int V> int launch(const Args& a, int device, cudaStream_t stream) {
-  const bool scored = a.bias || a.groups > 1;
-  if (a.chunks == 1) return scored ? launch<V, true, DVM_ROUTE_ONE>(a, device, stream) : launch<V, false, DVM_ROUTE_ONE>(a, device, stream);
-  return scored ? launch<V, true, DVM_ROUTE_ROUND>(a, device, stream) : launch<V, false, DVM_ROUTE_ROUND>(a, device, stream);
+  return a.bias || a.groups > 1 ? launch<V, true>(a, device, stream) : launch<V, false>(a, device, stream);
 }
 
 }  // namespace routing
@@ -658,6 +698,6 @@ int dvm_launch_routing(const dvm_routing_desc& d, void* const* t, cudaStream_t s
   if (st != DVM_OK) return st;
   st = d.experts <= 64 ? launch<2>(a, dev.device, stream) : d.experts <= 128 ? launch<4>(a, dev.device, stream) : d.experts <= 256 ? launch<8>(a, dev.device, stream)
        : launch<16>(a, dev.device, stream);
-  if (st != DVM_OK || a.chunks == 1) return st;
+  if (st != DVM_OK || a.tokens <= DVM_ROUTE_ONE) return st;
   return dvm_launch_next(dvm_routing_plan_kernel, (a.chunks + PLAN - 1) / PLAN, PLAN_THREADS, 0, stream, a);
 }

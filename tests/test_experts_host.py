@@ -127,7 +127,7 @@ def test_extents():
         return dvm.tensor_extents(binding.Code(buf, size, []))
     assert of("routing") == [10 * 16 * 4, 64, 40, 160, 160, 160, 68, 0]
     assert of("routing", biased=0, masked=0, dtype=1, logits_stride=20) == [2 * (9 * 20 + 16), 160, 160, 160, 68, 0]
-    assert of("routing", tokens=32)[-1] == 0 and of("routing", tokens=33)[-1] == 3 * 16 and of("routing", tokens=16 * 592 + 1, experts=18, logits_stride=18, groups=1, top_groups=1)[-1] == 297 * 32
+    assert of("routing", tokens=128)[-1] == 0 and of("routing", tokens=129)[-1] == 9 * 16 and of("routing", tokens=16 * 592 + 1, experts=18, logits_stride=18, groups=1, top_groups=1)[-1] == 297 * 32
     assert of("quantize") == [10 * 272 * 2, 120, 30 * 272, 30 * 3 * 4]
     assert of("quantize", gated=1, x_stride=600) == [2 * (9 * 600 + 544), 120, 30 * 272, 30 * 3 * 4]
     assert of("quantize", copies=0, rows=300, out_rows=300, block_rows=128, dtype=0) == [300 * 272 * 4, 300 * 272, 3 * 3 * 4]

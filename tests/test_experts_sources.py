@@ -18,9 +18,10 @@ def bodies(name):
 
 @pytest.mark.skipif(not os.path.exists(NVCC), reason="nvcc not found")
 @pytest.mark.parametrize("source,kernel,count,least,most,spilled", [
-    ("dvm_routing.cu", "routing_kernelILi2E", 4, 1, 64, 0),     # one CTA of 1024 threads per SM, or two of 512
-    ("dvm_routing.cu", "routing_kernelILi4E", 4, 1, 64, 0),
-    ("dvm_routing.cu", "routing_kernelILi8E", 4, 1, 64, 64),    # (off the keys' sort: what a warp keeps of the chunk)
+    ("dvm_routing.cu", "routing_kernelILi2E", 2, 1, 64, 0),     # two CTAs of 512 threads per SM
+    ("dvm_routing.cu", "routing_kernelILi4E", 2, 1, 64, 0),
+    ("dvm_routing.cu", "routing_kernelILi8E", 2, 1, 64, 64),    # (off the keys' sort: what a warp keeps of the chunk)
+    ("dvm_routing.cu", "routing_joint_kernel", 8, 1, 128, 0),   # one
     ("dvm_routing.cu", "routing_plan_kernel", 1, 1, 128, 0),
     ("dvm_quantize.cu", "quantize_kernel", 8, 1, 64, 0),        # four CTAs of 256 threads per SM
     ("dvm_quantize.cu", "quantize_block_kernel", 4, 1, 128, 0),

@@ -32,6 +32,15 @@ def test_drawn_routing(seed):
         check_routing(logits, k, str(r.choice(["softmax", "sigmoid"])), bias, groups, top_groups, bool(r.integers(2)), float(r.choice([1.0, 0.1, 16.0])), positions)
 
 
+@pytest.mark.parametrize("tokens", [1, 2, 7, 8, 9, 15, 16, 17, 63, 64, 65, 112, 113, 120, 121, 127, 128, 129, 143, 144, 145])
+def test_routing_of_few_tokens(tokens):
+    """Both sides of the border between one launch and two, and tokens that the CTAs of a cluster do not share evenly."""
+    for experts, groups, top_groups, k in ((5, 1, 1, 3), (512, 1, 1, 8), (96, 3, 2, 32)):
+        positions = ints(np.where(np.arange(tokens) % 5 == 3, -1, np.arange(tokens)))
+        check_routing(normal((tokens, experts), F32, tokens, 1.5), k, "sigmoid", normal((experts,), F32, 1, 0.1), groups, top_groups, True, 1.0, positions)
+        check_routing(normal((1, experts), F32, 3).expand(tokens, experts).contiguous(), k, "softmax", None, groups, top_groups)   # all tokens alike
+
+
 @pytest.mark.parametrize("scoring", ["sigmoid", "softmax"])
 def test_groups_whose_sums_32_bits_cannot_tell_apart(scoring):
     """Biases that cancel in a group's sum, equal groups, groups a step of fp32 apart, experts and whole groups that are switched off."""
