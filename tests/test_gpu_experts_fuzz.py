@@ -6,7 +6,7 @@ import torch
 
 import paper_2603_24239_b200 as dvm
 from tests import experts_oracle as orc
-from tests.test_gpu_experts import BF16, F32, check_combine, check_quantize, check_routing, check_scaled, ints, normal, ok, small_codes, small_scales, uneven, values, workspace
+from tests.test_gpu_experts import BF16, F32, check_combine, check_quantize, check_routing, check_scaled, ints, normal, ok, run_routing, small_codes, small_scales, uneven, values, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -222,3 +222,53 @@ def test_offsets_past_32_bits_in_the_weights():
             a, b = int(first[g]), int(first[g + 1])
             want = values(x[a:b], xs[a:b], 1) @ values(w[g].view(torch.float8_e4m3fn), ws[g], 128).T
             assert torch.equal(out[a:b].double(), want), g
+
+
+def test_a_dense_product_right_behind_what_writes_its_weight():
+    """The weight's codes are written by the launch just before, other ones each time: none of the last ones are read."""
+    n, k = 11008, 1024
+    x, xs = small_codes((3, k), 1), small_scales((3, 8), 2)
+    values_of = [normal((n, k), BF16, seed) for seed in (3, 4)]
+    w, ws = torch.zeros((n, k), dtype=torch.uint8, device="cuda"), torch.zeros((n // 128, 8), device="cuda")
+    out = [torch.empty((3, n), device="cuda") for _ in range(40)]
+    quantize = dvm.encode_quantize(values_of[0], w, ws, block_rows=128)
+    product = dvm.encode_scaled_matmul(x, xs, w[None], ws[None], out[0])
+    work, want = workspace(product), []
+    for v in values_of:
+        dvm.launch(quantize, [v, w, ws])
+        torch.cuda.synchronize()
+        dvm.launch(product, [x, xs, w, ws, out[0], work])
+        ok()
+        want.append(out[0].clone())
+    assert not torch.equal(want[0], want[1])
+    for i in range(40):
+        dvm.launch(quantize, [values_of[i % 2], w, ws])
+        dvm.launch(product, [x, xs, w, ws, out[i], work])
+    ok()
+    for i in range(40):
+        assert torch.equal(out[i], want[i % 2]), i
+
+
+def test_routing_on_two_streams_at_once():
+    """Clusters of two calls side by side, and calls of one launch between calls of two."""
+    a, b = normal((128, 256), F32, 1, 1.5), normal((300, 512), F32, 2, 1.5)
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def call(logits):
+        t, e = logits.shape
+        out = [torch.full((t, 8), 77, dtype=dt, device="cuda") for dt in (torch.int32, F32, torch.int32)] + [ints(np.full(e + 1, 77))]
+        code = dvm.encode_routing(logits, 8)
+        return code, [logits] + out + [workspace(code)]
+
+    calls = [(call(a), call(b), call(a[: i + 1])) for i in range(30)]
+    torch.cuda.synchronize()                                        # (the tensors are there before the other streams use them)
+    for x, y, z in calls:
+        dvm.launch(*x, one)
+        dvm.launch(*y, two)
+        dvm.launch(*z, two)
+    ok()
+    of_a, of_b = run_routing(a, 8), run_routing(b, 8)
+    ok()
+    for i, (x, y, z) in enumerate(calls):
+        assert all(torch.equal(p, q) for p, q in zip(x[1][1:5] + y[1][1:5], of_a + of_b)), i
+        assert all(torch.equal(p, q[: i + 1]) for p, q in zip(z[1][1:3], of_a[:2])), i
