@@ -48,7 +48,8 @@ extern "C" {
  *   with groups > 1: the experts form `groups` groups of neighbours; a group counts the sum of its two largest c (its only
  *   one, where a group is one expert); the top_groups groups that count most stay, of equal ones the first
  *   ids[t, 0 .. top_k)    the experts of the largest c among those, largest first, of equal ones the lowest index
- *   weights[t, j]         s of expert ids[t, j]; with `renormalise` divided by the sum over j; times `factor`
+ *   weights[t, j]         s of expert ids[t, j]; with `renormalise` divided by the sum over j (the quotient itself, also of scores
+ *                         that are below fp32's range: only where all of them are those of -inf is it 0 / 0, NaN); times `factor`
  * The order is that of exact values: where 32 bits cannot tell two apart, they are computed in 64.  A NaN counts less than
  * anything else (a NaN or +inf logit under softmax makes the token's weights NaN).
  * The plan, over all (t, j):

@@ -278,6 +278,16 @@ template <int V> __device__ __noinline__ int order_exactly(const Args& a, long l
   return lane < a.top_k ? result : -1;
 }
 
+// The chosen scores over their sum, lane j's of logit l, where scores may lie below what fp32 holds: relative to the largest of them
+// (m: its logit), which changes no quotient: exp(l - m) of a softmax; exp(-m) / (1 + exp(-l)) of a sigmoid, none of which is above
+// 1/2 here.
+__device__ __noinline__ float share_of_small(const Args& a, float l) {
+  const bool chosen = (threadIdx.x & 31) < a.top_k;
+  const float m = of_key(__reduce_max_sync(ALL, chosen ? key_of(l) : 0u));   // (-inf: 0 / 0)
+  const float s = a.sigmoid ? expf(l - m) / (1.f + expf(l)) : expf(l - m);
+  return s / warp_sum(chosen ? s : 0.f);
+}
+
 // A lane's keys in descending order.  Neighbours of every other pair trade places in turn.
 template <int V> __device__ __forceinline__ void sort_keys(uint32_t (&key)[V]) {
 #pragma unroll
@@ -429,7 +439,8 @@ template <int V, bool SCORED> __device__ __forceinline__ int choose(const Args& 
   float s = a.sigmoid ? 1.f / (1.f + expf(-mine_l)) : expf(mine_l - top) / sum;
   if (a.renormalise) {
     const float total = warp_sum(lane < a.top_k ? s : 0.f);
-    s = s / total;
+    // (2^-128 is lost of a sigmoid whose logit is below -88, 2^-150 of a softmax: nothing that counts, but in a small total)
+    s = total < (a.sigmoid ? 0.25f : 0x1p-23f) ? share_of_small(a, mine_l) : s / total;
   }
   *weight = s * a.factor;
   return lane < a.top_k ? mine : -1;

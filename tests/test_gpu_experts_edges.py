@@ -1,0 +1,80 @@
+"""The operators of a layer of experts where their numbers are at the ends of what fp32 holds, and at sizes near 2^31."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2603_24239_b200 as dvm
+from tests import experts_oracle as orc
+from tests.experts_oracle import f64
+from tests.test_gpu_experts import F32, check_routing, ints, normal, ok, run_routing
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------------ routing
+
+def check_renormalised(logits, top_k, scoring, bias=None, groups=1, top_groups=1, factor=1.0):
+    """As check_routing, the weights by logarithms of the scores, of finite logits: quotients of the scores themselves are 0 / 0 in 64 bits
+    too from logits of -746 down (exp(746) passes 2^1024)."""
+    ids, weights, places, starts = (x.cpu().numpy() for x in run_routing(logits, top_k, scoring, bias, groups, top_groups, True, factor))
+    ok()
+    want = orc.routing(f64(logits), top_k, scoring, None if bias is None else f64(bias), groups, top_groups, False, 1.0, None)
+    assert np.array_equal(ids, want[0]) and np.array_equal(places, want[2]) and np.array_equal(starts, want[3])
+    chosen = np.take_along_axis(f64(logits), ids.astype(np.int64), 1)
+    log_s = chosen if scoring == "softmax" else -np.logaddexp(0.0, -chosen)    # (a softmax's common denominator left out)
+    w = np.exp(log_s - np.logaddexp.reduce(log_s, 1, keepdims=True)) * factor
+    assert (np.abs(weights - w) <= w * orc.weights_bound(logits.shape[1]) + 2.0 ** -126).all()
+
+
+@pytest.mark.parametrize("tokens", [5, 200])
+@pytest.mark.parametrize("top_k", [1, 4])
+def test_renormalised_weights_of_scores_below_fp32(tokens, top_k):
+    """The definition's quotients are ordinary numbers however small the scores are.  (weights_bound: differences of the chosen logits are
+    below 30 here too.)"""
+    e = 64
+    base = normal((tokens, e), F32, 1, 3.0)
+    for shift in (-60.0, -85.0, -88.0, -100.0, -120.0, -400.0, -650.0):
+        for groups, top_groups in ((1, 1), (8, 3)):
+            check_renormalised(base + shift, top_k, "sigmoid", None, groups, top_groups, 2.5)
+        check_renormalised(base + shift, top_k, "sigmoid", normal((e,), F32, 2, 0.3))
+    # a bias that chooses experts far below the top
+    for below in (60.0, 90.0, 95.0, 104.0, 120.0, 400.0, 650.0):
+        logits, bias = base.clone(), torch.zeros(e, device="cuda")
+        bias[8:16] = 2.0
+        logits[:, 8:16] -= below
+        check_renormalised(logits, top_k, "softmax", bias)
+        check_renormalised(logits, top_k, "softmax", bias, 8, 2, 0.5)
+        check_renormalised(logits - 300.0, top_k, "sigmoid", bias, 8, 2)
+    # one chosen score of ordinary size beside ones that are not
+    logits = base - 130.0
+    logits[:, 3] = 1.0
+    check_renormalised(logits, top_k, "sigmoid")
+    check_renormalised(logits, top_k, "softmax")
+    logits[:, 3] = -50.0
+    check_renormalised(logits, top_k, "sigmoid")
+
+
+def test_renormalised_weights_of_values_that_are_not_finite():
+    """A NaN or +inf logit under softmax makes the weights NaN, whatever is chosen; so do chosen scores that are all zero, those of -inf."""
+    e, inf, nan = 64, float("inf"), float("nan")
+    base, zeros, high = normal((40, e), F32, 5), torch.zeros(e, device="cuda"), torch.zeros(e, device="cuda")
+    high[10:20] = 3.0
+    for bad in (nan, inf, -inf):
+        x = base.clone()
+        x[1, 5], x[3, :], x[7, 12:], x[9, 10:20] = bad, bad, bad, bad
+        for bias in (zeros, high):
+            check_routing(x, 6, "softmax", bias, renormalise=True)
+            check_routing(x, 6, "sigmoid", bias, renormalise=True)
+        check_routing(x, 6, "softmax", renormalise=True)
+        if bad != bad:
+            continue
+        check_routing(x, 6, "sigmoid", renormalise=True)
+        check_routing(x, 6, "sigmoid", None, 8, 5, True)
+    # the lowest finite logits are numbers like any others: alike ones share alike (exact arithmetic: 64 bits have 0 / 0 here)
+    x = base.clone()
+    x[::2] = torch.finfo(F32).min
+    for positions in (None, ints(np.arange(40) % 3 - 1)):
+        _, weights, _, _ = run_routing(x, 4, "sigmoid", renormalise=True, positions=positions)
+        ok()
+        takes_part = torch.ones(40, dtype=torch.bool, device="cuda") if positions is None else positions >= 0
+        assert bool((weights[::2] == torch.where(takes_part, 0.25, 0.0)[::2, None]).all())
