@@ -211,7 +211,7 @@ dvm_scaled_few_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_con
           next = scale_at(kb + S::AHEAD);
         }
         const float* const s = scales + (half * S::AHEAD + in) * ROWS + j_first;
-        const bool ok = mbar_wait(bar_done + 8 * buffer, b_phase, abort_flag);
+        const bool ok = __all_sync(ALL, mbar_wait(bar_done + 8 * buffer, b_phase, abort_flag));   // (its lanes alike: what follows is for whole warps)
         if (ok) {   // (a warp that gave up goes on without work, so that the warps still meet)
           tc_fence_after();
 #pragma unroll
