@@ -65,7 +65,7 @@ template <class T, int W> __global__ void __launch_bounds__(THREADS) dvm_combine
   grid_ready();
   grid_wait();
   // a warp's item: RUNS * 32 runs of a token
-  const int parts = (a.runs + RUNS * 32 - 1) / (RUNS * 32);
+  const int parts = (int)(((uint32_t)a.runs + (RUNS * 32 - 1)) / (RUNS * 32));   // (a row may have 2^31 - 1 columns)
   const long long items = (long long)a.tokens * parts, step = (long long)gridDim.x * (THREADS / 32);
   for (long long item = (long long)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5); item < items; item += step) {
     const int t = (int)(item / parts), run0 = (int)(item - (long long)t * parts) * (RUNS * 32) + lane;

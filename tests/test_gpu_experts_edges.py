@@ -78,3 +78,19 @@ def test_renormalised_weights_of_values_that_are_not_finite():
         ok()
         takes_part = torch.ones(40, dtype=torch.bool, device="cuda") if positions is None else positions >= 0
         assert bool((weights[::2] == torch.where(takes_part, 0.25, 0.0)[::2, None]).all())
+
+
+# ------------------------------------------------------------------------------------------------------ sizes near 2^31
+
+@pytest.mark.parametrize("cols", [2 ** 31 - 1, 2 ** 31 - 61])
+def test_combine_of_as_many_columns_as_a_size_can_name(cols):
+    """Odd numbers of columns, one to a thread: the last ones, and those on both sides of the last whole piece of 64, are written too."""
+    torch.cuda.empty_cache()
+    y = torch.empty((1, cols), dtype=torch.bfloat16, device="cuda").fill_(3.0)
+    out = torch.full((1, cols), 7.0, dtype=torch.bfloat16, device="cuda")
+    places, weights = ints([[0]]), torch.ones((1, 1), device="cuda")
+    dvm.launch(dvm.encode_combine(y, places, weights, out), [y, places, weights, out])
+    ok()
+    assert bool((out == 3.0).all())
+    del y, out
+    torch.cuda.empty_cache()
