@@ -110,7 +110,8 @@ int dvm_encode_quantize(const dvm_quantize_desc* d, void* code, size_t code_capa
  * The products run on the tensor cores.  x and w start at multiples of 16 bytes (DVM_ERR_INVALID_ARG at launch otherwise).
  * Which of a row's partial sums are added first may depend on the numbers of rows of all groups, never on what they hold:
  * the same sizes and starts give the same bits.
- * DVM_ERR_UNSUPPORTED: k or a stride of x or w not a multiple of 16.  DVM_ERR_TOO_LARGE: more groups than above. */
+ * DVM_ERR_UNSUPPORTED: k or a stride of x or w not a multiple of 16.  DVM_ERR_TOO_LARGE: more groups than above, or more than 2^31 -
+ * 256 rows or columns of the result. */
 typedef struct {
   int64_t rows, n, k, groups;
   int64_t x_stride, x_scales_stride, out_stride;  /* row */

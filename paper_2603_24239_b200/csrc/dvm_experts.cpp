@@ -35,7 +35,8 @@ int check(const dvm_quantize_desc& d) {
 int check(const dvm_scaled_matmul_desc& d) {
   if (!dim_ok(d.rows) || !dim_ok(d.n, 1) || !dim_ok(d.k, 1) || !dim_ok(d.groups, 1) || !float_type(d.out_dtype) || (d.grouped & ~1)) return DVM_ERR_INVALID_ARG;
   if (!d.grouped && d.groups != 1) return DVM_ERR_SHAPE_MISMATCH;
-  if (d.groups > DVM_MAX_WEIGHT_GROUPS) return DVM_ERR_TOO_LARGE;
+  // (the kernels add a tile's rows or columns, 256 at most, less one to these in 32 bits)
+  if (d.groups > DVM_MAX_WEIGHT_GROUPS || d.rows > kMaxDim - 255 || d.n > kMaxDim - 255) return DVM_ERR_TOO_LARGE;
   const int64_t r[1] = {d.rows}, w[2] = {d.groups, d.n}, kb = dvm_up(d.k, DVM_SCALE_BLOCK), nb = dvm_up(d.n, DVM_SCALE_BLOCK);
   if (extent(r, &d.x_stride, 1, d.k, 1) < 0 || extent(r, &d.x_scales_stride, 1, kb, 4) < 0 || extent(w, d.w_stride, 2, d.k, 1) < 0 ||
       extent(r, &d.out_stride, 1, d.n, es_of(d.out_dtype)) < 0 || !distinct(r, &d.out_stride, 1, d.n) || (__int128)d.groups * nb * kb * 4 > kMaxBytes)
