@@ -101,17 +101,20 @@ __device__ __forceinline__ float rcp(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// silu(z) u: z / (1 + 2^(-z log2 e)) u; most: the largest 1 + 2^(-z log2 e).
+// silu(z) u: z (u / (1 + 2^(-z log2 e))); most: the largest 1 + 2^(-z log2 e).  (The quotient first: what it loses as a subnormal number
+// is lost of a value below 2^-119, while a small z before a large u would lose bits of values of any size.)
 __device__ __forceinline__ float2 gated(float2 z, float2 u, float& most) {
   const float2 e = mul2(z, make_float2(-1.4426950408889634f, -1.4426950408889634f));
   const float2 d = add2(make_float2(ex2(e.x), ex2(e.y)), make_float2(1.f, 1.f));
   asm("max.f32 %0, %0, %1, %2;" : "+f"(most) : "f"(d.x), "f"(d.y));
-  return mul2(mul2(z, make_float2(rcp(d.x), rcp(d.y))), u);
+  return mul2(z, mul2(make_float2(rcp(d.x), rcp(d.y)), u));
 }
 // How far off the above is, relative to it, with the product of it and a rounded reciprocal of the scale: the exponent's rounding
 // and that of log2 e cost |z| (2^-24 + 2^-26.2) where the exponential counts (z < 0), the instructions and roundings 11 x 2^-24 at
 // most: 2^-19.6 while 1 + e < 2^12 (z > -8.4), less than 2^-16 up to where silu is 0 in fp32.
-__device__ __forceinline__ float off_by(float most) { return most < 0x1p12f ? 0x1.6ap-20f : 0x1p-16f; }
+// In blocks of a small scale s what subnormal quotients lose may count: |z| 2^-150 < 2^-143.5 (|z| < 88, beyond 17 for z < 0 alone), 2^-7.5 of
+// the least border, 2^-10 s >= 2^-136; from s = 2^-96 on it is 2^-37 of that.  (2^-6 to both sides still has one border at most.)
+__device__ __forceinline__ float off_by(float most, float s) { return s < 0x1p-96f ? 0x1p-6f : most < 0x1p12f ? 0x1.6ap-20f : 0x1p-16f; }
 // The same to 2^-40: 2^f by its series (the 11th term is below 2^-42), a reciprocal and a step of Newton's.
 __device__ __forceinline__ double gated_exactly(float z, float u) {
   const double x = fminf(fmaxf(z, -200.f), 200.f), t = fma(x, -1.4426950408889634, 0x1.8p52), f = fma(x, -1.4426950408889634, 0x1.8p52 - t);
@@ -250,7 +253,7 @@ template <class T, bool GATED, bool VEC> __global__ void __launch_bounds__(THREA
 #pragma unroll
       for (int d = L / 2; d > 0; d >>= 1) s = fmaxf(s, __shfl_xor_sync(ALL, s, d));
       s = most < INFINITY ? fmaxf(s, 0x1p-126f) : __uint_as_float(0x7fc00000u);
-      codes_of<N>(v, s, off_by(worst), c, [&](int i, float edge) { return side_gated(wide(from[i]), wide(from[a.cols + i]), s, edge); });
+      codes_of<N>(v, s, off_by(worst, s), c, [&](int i, float edge) { return side_gated(wide(from[i]), wide(from[a.cols + i]), s, edge); });
     } else {
       s = scale_of(most);
       codes_of<N>(v, s, 0x1p-21f, c, [&](int i, float edge) { return side(wide(from[i]), s, edge); });

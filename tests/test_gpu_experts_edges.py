@@ -94,3 +94,49 @@ def test_combine_of_as_many_columns_as_a_size_can_name(cols):
     assert bool((out == 3.0).all())
     del y, out
     torch.cuda.empty_cache()
+
+
+# ------------------------------------------------------------------------------------------------------ gated codes
+
+def spread_values(shape, lo, hi, dtype, seed, signed=True):
+    """Magnitudes 2^lo .. 2^hi, evenly in their logarithms."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    v = torch.exp2(torch.rand(shape, generator=g, device="cuda") * (hi - lo) + lo)
+    return (v * torch.sign(torch.randn(shape, generator=g, device="cuda")) if signed else v).to(dtype)
+
+
+def check_gated(z, u):
+    """Codes nearest to the quotients in 64 bits by the kernel's own scales, all of them; scales of the largest value, or of one less than
+    2^-15 below it.  Values of 2^128 and more are infinities (as near to 2^128 as the kernel's fp32 may be off, 2^-16, they may be or not)."""
+    rows, cols = z.shape
+    x = torch.cat([z, u], 1)
+    codes, scales = torch.full((rows, cols), 0x11, dtype=torch.uint8, device="cuda"), torch.full((rows, -(-cols // 128)), 7.0, device="cuda")
+    dvm.launch(dvm.encode_quantize(x, codes, scales, gated=True), [x, codes, scales])
+    ok()
+    z, u = z.double(), u.double()
+    v = torch.where(z < -87.336544, 0.0, z / (1 + (-z).exp())) * u          # (126 ln 2)
+    v = torch.nn.functional.pad(v, (0, -cols % 128)).view(rows, -1, 128)
+    largest = (v.abs().amax(2) / 448).clamp(min=2.0 ** -126)
+    top = largest * 448
+    infinite = torch.where((top / 2.0 ** 128 - 1).abs() < 2.0 ** -16, scales.isnan(), top >= 2.0 ** 128)
+    assert torch.equal(scales.isnan(), infinite)
+    assert bool(((scales.double() - largest).abs() <= largest * 2.0 ** -15)[~infinite].all())
+    q = torch.where(infinite[..., None], 0.0, v / scales.double()[..., None]).view(rows, -1)[:, :cols]
+    want = torch.from_numpy(orc.encode(q.cpu().numpy())).cuda()
+    assert torch.equal(codes & 0x7f, want & 0x7f)
+    assert bool(((codes >> 7) == (q < 0))[(want & 0x7f) > 0].all())
+
+
+@pytest.mark.parametrize("dtype", [F32, torch.bfloat16])
+@pytest.mark.parametrize("z_lo,z_hi,u_lo,u_hi", [
+    (-149, -124, 90, 127),      # gates among fp32's subnormals, values that are not
+    (-149, -100, 60, 127), (-126, 6, 0, 20),
+    (-1, 1, -149, -105),        # the other way round
+    (-20, 3, -130, -118),       # blocks of the least scale and a little above
+    (-10, 6, -149, -100), (-149, 6, -149, 100), (3, 6.4, -149, -120), (3, 6.4, 60, 125)])
+def test_gated_codes_of_small_and_large_factors(dtype, z_lo, z_hi, u_lo, u_hi):
+    for seed, n in ((1, 3000), (2, 500)):
+        z, u = spread_values((n, 272), z_lo, z_hi, dtype, seed), spread_values((n, 272), u_lo, u_hi, dtype, seed + 10)
+        check_gated(z, u)
+        check_gated(-z.abs(), u)
+        check_gated(z.abs(), u)
