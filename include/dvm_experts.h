@@ -79,8 +79,8 @@ int dvm_encode_routing(const dvm_routing_desc* d, void* code, size_t code_capaci
  *   scale = max(max |v| / 448, 2^-126)        rounded to fp32
  *   code  = the e4m3 value nearest to the quotient v / scale, of two the even one
  * (not of a rounded quotient, so the codes of an input are the same everywhere; with `gated` v is taken to 2^-40 where that
- * decides, silu(z) counts as zero for z < -87, v of 2^128 and more is an infinity, and the scale may be that of a value less than
- * 2^-15 below the largest.)
+ * decides, silu(z) counts as zero where exp(-z) passes 2^126 -- z below -87.3365 --, v of 2^128 and more is an infinity, and the
+ * scale may be that of a value less than 2^-15 below the largest.)
  * A block that holds an infinity or a NaN has the scale NaN and codes of zero.
  * block_rows 1: a scale for 128 columns of a row; 128: for 128 x 128 (weights; neither gated nor with copies).
  * copies = 0: row t of x is row t of the codes (out_rows = rows).  copies > 0: it is written to the rows places[t, j], 0 <= j <

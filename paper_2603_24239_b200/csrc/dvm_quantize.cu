@@ -115,7 +115,8 @@ __device__ __forceinline__ float2 gated(float2 z, float2 u, float& most) {
 // In blocks of a small scale s what subnormal quotients lose may count: |z| 2^-150 < 2^-143.5 (|z| < 88, beyond 17 for z < 0 alone), 2^-7.5 of
 // the least border, 2^-10 s >= 2^-136; from s = 2^-96 on it is 2^-37 of that.  (2^-6 to both sides still has one border at most.)
 __device__ __forceinline__ float off_by(float most, float s) { return s < 0x1p-96f ? 0x1p-6f : most < 0x1p12f ? 0x1.6ap-20f : 0x1p-16f; }
-// The same to 2^-40: 2^f by its series (the 11th term is below 2^-42), a reciprocal and a step of Newton's.
+// The same to 2^-40: 2^f by its series (the 11th term is below 2^-42), a reciprocal and a step of Newton's.  By a quarter of 1 + 2^(-z log2 e):
+// where the above is zero, its reciprocal below 2^-126, is for the above alone to say, so that scale and codes see one place.
 __device__ __forceinline__ double gated_exactly(float z, float u) {
   const double x = fminf(fmaxf(z, -200.f), 200.f), t = fma(x, -1.4426950408889634, 0x1.8p52), f = fma(x, -1.4426950408889634, 0x1.8p52 - t);
   double p = 7.054911620801121e-09;
@@ -123,8 +124,8 @@ __device__ __forceinline__ double gated_exactly(float z, float u) {
                         0.009618129107628477, 0.055504108664821576, 0.2402265069591007, 0.6931471805599453, 1.0};
 #pragma unroll
   for (int i = 0; i < 10; ++i) p = fma(p, f, c[i]);
-  const double d = fma(p, __hiloint2double((__double2loint(t) + 1023) << 20, 0), 1.0), r = (double)rcp((float)d);
-  return (double)z * fma(fma(-d, r, 1.0), r, r) * (double)u;
+  const double d = fma(p, __hiloint2double((__double2loint(t) + 1021) << 20, 0), 0.25), r = (double)rcp((float)d);
+  return (double)z * fma(fma(-d, r, 1.0), r, r) * ((double)u * 0.25);
 }
 __device__ __forceinline__ float max_abs(float m, float x) {  // NaN if either is
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(m), "f"(fabsf(x)));
@@ -236,7 +237,7 @@ template <class T, bool GATED, bool VEC> __global__ void __launch_bounds__(THREA
     if (GATED) {
       // the lanes whose largest may be the block's compute it again, to more than fp32
       s = 0.f;
-      if (own >= most * (1.f - 0x1p-15f)) {
+      if (own > most * (1.f - 0x1p-15f)) {   // (not where all are zero)
         Raw<T, 2> z = {}, u = {};
         float first = 0.f;
 #pragma unroll

@@ -140,3 +140,39 @@ def test_gated_codes_of_small_and_large_factors(dtype, z_lo, z_hi, u_lo, u_hi):
         check_gated(z, u)
         check_gated(-z.abs(), u)
         check_gated(z.abs(), u)
+
+
+def test_gated_where_silu_becomes_zero():
+    """At one place (-126 ln 2, -87.3365) for what the scale is of and for the codes, whatever stands beside it; values that count are those
+    before large ones.  In fp32 the place is off by 2^-16 at most: half a step of the exponent 126 (2^-18) and log2 e's rounding (2^-19), the
+    exponential's 2 ulp and the sum's rounding (2^-21)."""
+    at = -126 * np.log(2.0)
+    near = np.float32(at).view(np.int32) + np.arange(-300, 301)                      # steps of fp32 on both sides
+    z = np.concatenate([near.astype(np.int32).view(np.float32), np.float32([-86.9, -87.0, -87.1, -87.25, -87.3, -87.33, -87.34, -87.4, -87.5, -88, -89, -100, -1e4, -3e38])])
+    z = torch.tensor(np.repeat(z, 3), device="cuda")
+    for u in (3e38, -1e37, 1e30):
+        for beside in ((0.0, 0.0), (1.0, 1e-3), (-87.0, 1e38)):                      # the rest of its block: nothing, small, large
+            for lane in (0, 5, 127):
+                x = torch.zeros((len(z), 256), device="cuda")
+                x[:, 1:128:3], x[:, 129::3] = beside
+                x[:, lane], x[:, 128 + lane] = z, u
+                codes, scales = torch.zeros((len(z), 128), dtype=torch.uint8, device="cuda"), torch.zeros((len(z), 1), device="cuda")
+                dvm.launch(dvm.encode_quantize(x, codes, scales, gated=True), [x, codes, scales])
+                ok()
+                zz, uu = f64(x[:, :128]), f64(x[:, 128:])
+                with np.errstate(over="ignore"):
+                    full = zz / (1 + np.exp(-zz)) * uu
+                # either side of the place, to 2^-16 of it, both answers are one: the whole block's
+                got_c, got_s = codes.cpu().numpy(), f64(scales)
+                for zero_from in (at - 2.0 ** -16, at + 2.0 ** -16):
+                    v = np.where(zz < zero_from, 0.0, full)
+                    top = np.maximum(np.abs(v).max(1, keepdims=True) / 448, 2.0 ** -126)
+                    right = (np.abs(got_s - top) <= top * 2.0 ** -15) & ((got_c & 0x7f) == (orc.encode(v / got_s) & 0x7f))
+                    both = right.all(1) if zero_from < at else both | right.all(1)
+                    if zero_from < at:
+                        never_zero = right.all(1)
+                    else:
+                        zero = right.all(1)
+                own = zz[:, lane]
+                assert both.all()
+                assert never_zero[own >= at + 2.0 ** -16].all() and zero[own < at - 2.0 ** -16].all()
