@@ -50,8 +50,10 @@ extern "C" {
  *   ids[t, 0 .. top_k)    the experts of the largest c among those, largest first, of equal ones the lowest index
  *   weights[t, j]         s of expert ids[t, j]; with `renormalise` divided by the sum over j (the quotient itself, also of scores
  *                         that are below fp32's range: only where all of them are those of -inf is it 0 / 0, NaN); times `factor`
- * The order is that of exact values: where 32 bits cannot tell two apart, they are computed in 64.  A NaN counts less than
- * anything else (a NaN or +inf logit under softmax makes the token's weights NaN).
+ * The order is that of exact values: where 32 bits cannot tell two apart, they are computed in 64.  Without `biased` experts (not
+ * groups) are ordered by their logits, whose order is that of the scores.  A NaN counts less than anything else.  Under softmax a
+ * NaN or +inf logit, or logits of -inf alone, make all of the token's scores and weights NaN: groups, and biased experts, are then
+ * taken by index, others by their logits.
  * The plan, over all (t, j):
  *   starts[e]     first row of expert e: rows starts[e] <= r < starts[e + 1] are its tokens, in their order;
  *                 starts[experts] rows are in use
@@ -101,7 +103,8 @@ int dvm_encode_quantize(const dvm_quantize_desc* d, void* code, size_t code_capa
 
 /* ---- scaled matmul: product of 8-bit matrices with a scale per block, one weight or one per group of rows --------------
  *   out[r, n] = sum over blocks b of x_scales[r, b] w_scales[g, n / 128, b] (sum over k in b of x[r, k] w[g, n, k])
- * fp32 accumulation, rounded once when stored.  With `grouped`, g is the group with starts[g] <= r < starts[g + 1] (starts as
+ * fp32 accumulation, rounded once when stored.  The two scales are multiplied first, in fp32: a product below 2^-126 has fewer
+ * bits than others, one of 2^128 and more is infinite.  With `grouped`, g is the group with starts[g] <= r < starts[g + 1] (starts as
  * routing gives them: ascending; values outside [0, rows] are cut); rows of no group stay as they were.  Without, groups is
  * 1 and every row meets that weight.
  * Tensors: x codes [rows, k], x_scales [rows, k / 128 rounded up] fp32, w codes [groups, n, k], w_scales [groups, n / 128, k /

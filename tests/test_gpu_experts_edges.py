@@ -80,6 +80,23 @@ def test_renormalised_weights_of_values_that_are_not_finite():
         assert bool((weights[::2] == torch.where(takes_part, 0.25, 0.0)[::2, None]).all())
 
 
+def test_softmax_without_a_number():
+    """All of a token's scores are NaN: groups, and experts with a bias, are taken by index, experts without one by their logits."""
+    e, inf, nan = 96, float("inf"), float("nan")
+    x = normal((150, e), F32, 7)
+    x[::3, 40], x[1::3, 90], x[2::6, 5], x[5::6] = nan, inf, nan, -inf
+    high = normal((e,), F32, 8)
+    for groups, top_groups in ((1, 1), (8, 5)):
+        for renormalise in (False, True):
+            check_routing(x, 6, "softmax", None, groups, top_groups, renormalise)
+            check_routing(x, 6, "softmax", high, groups, top_groups, renormalise)
+    ids, weights, _, _ = run_routing(x, 6, "softmax", high)
+    ok()
+    assert bool(weights.isnan().all()) and bool((ids == torch.arange(6, device="cuda")).all())
+    ids, _, _, _ = run_routing(x[:1], 6, "softmax")
+    assert torch.equal(ids[0].long(), x[0].nan_to_num(-inf).sort(descending=True, stable=True)[1][:6])
+
+
 # ------------------------------------------------------------------------------------------------------ sizes near 2^31
 
 @pytest.mark.parametrize("cols", [2 ** 31 - 1, 2 ** 31 - 61])
