@@ -1,8 +1,9 @@
 // Combine meta-kernel: every token's rows added up by weight, out[t] = base[t] + sum_j weights[t, j] y[places[t, j]].
 //
 // Bound by memory: each row is read once.  A thread takes twice 16 bytes of columns of one token and asks for up to 8 rows at
-// once; sums are fp32, in the order of j, rounded once.  8192 tokens of 8 rows of 4096, with a base: 112 us, 6.0 TB/s (124 with one
-// run of 16 bytes to a thread); 64 tokens of 6: 2.5 us in a chain of launches.
+// once; sums are fp32, in the order of j, rounded once.  8192 tokens of 8 rows of 4096, with a base: 113 us, 5.9 TB/s (124 with one
+// run of 16 bytes to a thread); rows at odd places, a column to a load, 237 without a base (100 at even ones); 64 tokens of 6: 2.5 us in a
+// chain of launches.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

@@ -208,8 +208,10 @@ CombineSlots dvm_slots(const dvm_combine_desc& d) {
 }
 
 // Which kernel takes a scaled product, by the rows of a group if they were dealt out evenly and by the tiles that gives.
-//  16  the weights' bytes are all that counts: up to 12 rows to a group (1024 rows of 128 experts, 4096 to 2816: 244 us, 277 in
-//      tiles of 64, 302 in the kernel for many), or up to 32 where the tiles do not fill the device (32 rows, 4096 to 4096: 9.9,
+//  16  the weights' bytes are all that counts: up to 12 rows to a group (of 128 experts, 4096 to 2816, drawn evenly, so that they have
+//      more and fewer: 8 rows on average 235 us, 250 in tiles of 64, 280 in the kernel for many; 12: 253, 276, 285; 13: 262, 279, 294;
+//      14: 283, 279, 293; 16: 317, 286, 285; of 64, 2048 to 4096: 12: 97, 109, 105; 14: 110, 110, 109; 16: 116, 112, 110; groups of just
+//      16: 245, 258, 276, of just 20: 401, 290, 281), or up to 32 where the tiles do not fill the device (32 rows, 4096 to 4096: 9.9,
 //      10.0, 17.7)
 //  64  more rows, and still no more tiles than CTAs (128 rows, 4096 to 4096: 20.8, 13.0, 18.9; 256: 37, 18.4, 19.1)
 //  else the kernel for many (128 rows, 4096 to 11008: 50, 26, 19.6; 2048 rows of 64 experts, 4096 to 2816: 256, 169, 157; 512 of

@@ -12,8 +12,8 @@
 // value again: with a place in the code for each of the 16, 8192 rows of 4096 without copies took 33 us, now 27.
 // A gated value is fp32 within a bound; its products take the bound in, and the largest of a block and the values at a border
 // are computed again to 2^-40: in fp32 alone 1 of 600000 codes was the neighbour of the right one.
-// 8192 tokens of 4096 to 8 rows each: 64 us, 5.4 TB/s; 49157 rows of 1408 gated: 73 us, 4.7 (the largest again 9 us, the second
-// product 4; 330 instructions to a warp's four blocks, one step after another); weights of 11008 x 4096 from fp32: 36 us, 6.2.
+// 8192 tokens of 4096 to 8 rows each: 64 us, 5.4 TB/s; 49157 rows of 1408 gated: 73 us in a chain, 77 in calls, 4.8 and 4.5 (the largest
+// again 9 us, the second product 4; 330 instructions to a warp's four blocks, one step after another); weights of 11008 x 4096 from fp32: 36 us, 6.2.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>

@@ -12,8 +12,8 @@
 // choices are a bit per token in a word per expert: a token's rank at its expert is the number of bits below its own, plus what
 // earlier rounds of the chunk counted.  Up to 128 tokens are dealt to the 8 CTAs of a cluster, which read one another's counts;
 // else every CTA leaves its chunk's counts in the workspace, a byte each, and a second launch adds up those of the chunks before.
-// 8191 tokens of 256 experts in 8 groups with a bias: 29 us (19 without both), 64 tokens 6.1 (4.2), one token of 64
-// experts 3.4 in a chain of launches (two launches of CTAs of 16 tokens took 9.8 for 64; one CTA of 32 took 6.6 for 32, 5.8 now).  Bound by
+// 8191 tokens of 256 experts in 8 groups with a bias: 28 us (19 without both), 64 tokens 6.0 (4.2), one token of 64
+// experts 3.8 in a chain of launches (two launches of CTAs of 16 tokens took 9.8 for 64; one CTA of 32 took 6.6 for 32, 5.8 now).  Bound by
 // instructions: 2.1 us would read the logits, but a token costs 870 instructions without groups or bias (a load, a score, a sort of
 // 8 keys and 8 rounds of two reductions) and 1530 with both, 13 and 20 us of the first launch.  A warp per token was taken over a
 // CTA per token (whose barriers made 8191 tokens 96 us) and over a thread per token (64 tokens leave the GPU empty).  One token in

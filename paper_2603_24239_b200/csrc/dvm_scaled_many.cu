@@ -11,8 +11,10 @@
 // warps copy the scales of four blocks at a time into shared memory, ahead of all that.  At a tile's end rows leave by TMA from
 // shared memory, beside the next tile's sums; of a warp whose rows are not all the group's each thread stores its own.
 // A place in tensor memory is taken for the products (512 cycles), their end's arrival (190), the loads and sums (500) and the
-// way back (200), and there are two: 950 to 1000 cycles a block are what it takes.  8192 rows, 4096 to 11008: 360 us in bursts,
-// 2.05 PFLOP/s (1.7 GHz), 407 in calls in a row at the power cap (1.42 GHz).
+// way back (200), and there are two: 700 cycles a block, or L2's 768.  It takes 950 (4096 rows, 4096 to 5632: cycles of the SMs over
+// their blocks) to 1000; which of the ends of tiles, where rows are packed, and of what else holds the other 200 is not known.  8192
+// rows, 4096 to 11008: 360 us in bursts, 2.05 PFLOP/s (1.7 GHz), 407 to 417 in calls in a row at the power cap (1.42 GHz).
+// (The compiler keeps some values of a tile in memory: 9 loads a warp and tile, none to a block, by the counters.)
 // Built and not faster: pairs of CTAs (cta_group::2; half the weight's bytes from L2, but a commit to both CTAs and an arrival at
 // the other take 800 cycles more); places of half the columns each (416 us: x is read from shared memory twice); 32 columns at a time from tensor memory
 // (spilled registers: 430 to 520 us); all waits polled without sleep (no change).
